@@ -112,6 +112,8 @@ typedef struct tri_cache {
                                      each already rotated by its own position (Section 2.1 Eq. 1), as serving
                                      stacks usually store them; the scores are the same, the rotation of the key
                                      in the score kernel is skipped and pos is read by tri_compact only */
+    int32_t n_blocks;             /* paged, read by tri_append and tri_attend / tri_attend_shared only: block ids outside [0, n_blocks)
+                                     name no block; 0: not given, only negative ids name no block */
 } tri_cache;
 
 const char *tri_last_error(void);
@@ -243,6 +245,78 @@ size_t tri_static_scratch_size(void);
 tri_status tri_compress_step_static(const tri_model *model, const float *centers, const tri_cache *src,
                                     const tri_cache *dst, int32_t budget, int32_t *kept_idx,
                                     int32_t *kept_cnt, int32_t *new_seq_len, void *stream);
+
+/*
+ * ---- What a serving step does with the cache between two compressions: it appends its tokens' keys and values, and its
+ * queries attend to what is cached.  Both work on one layer per call (a model's layers depend on one another) and on caches as
+ * the compression leaves them: slots in any order, a position per head and slot, pre- or post-RoPE keys, lengths per sequence or
+ * per head.  Rotation means Section 2.1 Eq. 1 with the model's rope_theta and pair layout; angles are exact for every int32 position.
+ *
+ * The step's tokens, sequence by sequence.  max_tokens bounds the tokens of one sequence (it sizes grids; tokens beyond it: output
+ * unspecified).  Device values are read into their ranges: no token range leaves [0, n_tokens], no length [0, max_seq_len].
+ */
+typedef struct tri_tokens {
+    int32_t n_tokens;         /* T >= 0 */
+    int32_t max_tokens;       /* host bound on the tokens of one sequence, 1 to n_tokens (not read where start is NULL) */
+    const int32_t *start;     /* device [n_seqs + 1], ascending from 0 to n_tokens: sequence s has the tokens start[s] to start[s + 1] - 1.
+                                 NULL: one token per sequence (n_tokens == n_seqs), token s being sequence s's */
+    const int32_t *pos;       /* device [n_tokens]: positions; NULL (only where start is NULL): the cache's cur_pos */
+    const int32_t *head_len;  /* NULL: sequence s has seq_len[s] occupied slots in every head.  Else device
+                                 [n_layers][n_seqs][n_kv_heads], as kept_cnt: the occupied slots of every head-instance
+                                 (after a compression with head_budgets); seq_len is not read then */
+    int32_t rotated;          /* 0: the step's q and k rows are pre-RoPE and are rotated by pos where needed; 1: already rotated */
+} tri_tokens;
+
+/*
+ * Appends the step's keys, values and positions to layer `layer` of a cache: token i of sequence s goes to slot len + i of every
+ * head, len being the sequence's (head's) length before the step.  Keys are rotated by their position on the way where the cache holds
+ * post-RoPE keys (k_rotated) and the rows are not rotated yet (one rounding, to the cache's type); rotated rows for a cache of
+ * pre-RoPE keys are TRI_ERR_UNSUPPORTED.
+ *   k_new, v_new  device rows of head_dim elements of the cache's dtype: token t, KV head h at t*stride_token + h*stride_head elements
+ *                 (the same strides for both: views of a fused projection's output will do); 16-byte aligned
+ *   new_seq_len   NULL or device [n_seqs] int32 <- min(len + tokens, max_seq_len) (of KV head 0 with head_len); must not be seq_len
+ *                 or head_len, which other workgroups of the call still read
+ * Tokens whose slot lies at or beyond max_seq_len, or in a block that there is not (n_blocks), are not written.
+ */
+tri_status tri_append(const tri_model *model, const tri_cache *cache, int32_t layer, const tri_tokens *tokens, const void *k_new,
+                      const void *v_new, int64_t stride_token, int64_t stride_head, int32_t *new_seq_len, void *stream);
+
+/* Queries in, attention out: rows of head_dim elements of the cache's dtype, token t, query head h at t*stride_token + h*stride_head
+ * elements; 16-byte aligned.  Query head h attends with KV head h / G.  out must not overlap q. */
+typedef struct tri_attention {
+    const void *q;
+    void *out;
+    int64_t q_stride_token, q_stride_head;
+    int64_t out_stride_token, out_stride_head;
+    float scale;              /* of the products q . k; finite, > 0 */
+    int32_t causal;           /* 1: a token attends to the keys whose position is at most its own; 0: to all */
+} tri_attention;
+
+/*
+ * out = sum_n p_n v_n, p = softmax over the attended keys n of scale * (q . k_n), both rotated by their positions: the keys of layer `layer` in the
+ * occupied slots of the token's own sequence (the step's own tokens among them once tri_append has written them and the lengths count them).
+ * A token that attends to no key gets zeros.  What lies in slots that are not occupied is never used, whatever it is; a key or value that is not a
+ * number reaches the tokens that attend to it only.  Occupied slots in blocks that there are not (n_blocks) hold no key.  Scores, softmax and sums are
+ * held in fp32; results do not depend on anything but the arguments (no atomics).
+ * workspace as for tri_score, of tri_attend_workspace_size() bytes (which may be 0: NULL will do then).
+ */
+tri_status tri_attend(const tri_model *model, const tri_cache *cache, int32_t layer, const tri_tokens *tokens,
+                      const tri_attention *attention, void *workspace, size_t ws_bytes, void *stream);
+
+/*
+ * The same for sequences behind shared prefixes: `prefix` is a cache of its own (dtype as the cache's, everything else may differ) whose "sequences" are the prefixes,
+ * and the tokens of sequences group[g] to group[g + 1] - 1 attend to prefix g's keys too, by the same rule.  The prefix is read once for all
+ * their tokens, not once per sequence.
+ *   group  device [prefix->n_seqs + 1], ascending from 0 to cache->n_seqs; NULL: one prefix (prefix->n_seqs == 1) for all sequences
+ * tokens->head_len says the lengths of the sequences' own heads; prefixes have prefix->seq_len keys in every head.
+ */
+tri_status tri_attend_shared(const tri_model *model, const tri_cache *prefix, const int32_t *group, const tri_cache *cache,
+                             int32_t layer, const tri_tokens *tokens, const tri_attention *attention, void *workspace,
+                             size_t ws_bytes, void *stream);
+
+/* Bytes of workspace of tri_attend (prefix NULL) or tri_attend_shared for these geometries (bounds count, not lengths on the device); (size_t)-1 on
+ * invalid arguments. */
+size_t tri_attend_workspace_size(const tri_model *model, const tri_cache *prefix, const tri_cache *cache, const tri_tokens *tokens);
 
 /*
  * Measurement hook for benchmark harnesses (no counterpart in the paper).  After attaching, the

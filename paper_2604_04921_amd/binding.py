@@ -19,7 +19,7 @@ TRI_SCORE_FULL, TRI_SCORE_TRIG_ONLY, TRI_SCORE_NORM_ONLY, TRI_SCORE_NORM_UNWEIGH
 
 EXPORTS = ["tri_last_error", "tri_build_centers", "tri_centers_accumulate", "tri_centers_finalize", "tri_band_diagnostics", "tri_workspace_size", "tri_score", "tri_select_topk",
            "tri_compact", "tri_compact_fill", "tri_compress_step", "tri_static_scratch_size", "tri_compress_step_static",
-           "tri_timing_attach", "tri_timing_detach"]
+           "tri_append", "tri_attend", "tri_attend_shared", "tri_attend_workspace_size", "tri_timing_attach", "tri_timing_detach"]
 
 
 class TriModel(ctypes.Structure):
@@ -38,7 +38,18 @@ class TriCache(ctypes.Structure):
                 ("stride_layer", ctypes.c_int64), ("stride_seq_or_block", ctypes.c_int64),
                 ("stride_head", ctypes.c_int64), ("stride_slot", ctypes.c_int64),
                 ("pos_stride_layer", ctypes.c_int64), ("pos_stride_seq_or_block", ctypes.c_int64),
-                ("pos_stride_head", ctypes.c_int64), ("k_rotated", ctypes.c_int32)]
+                ("pos_stride_head", ctypes.c_int64), ("k_rotated", ctypes.c_int32), ("n_blocks", ctypes.c_int32)]
+
+
+class TriTokens(ctypes.Structure):
+    _fields_ = [("n_tokens", ctypes.c_int32), ("max_tokens", ctypes.c_int32), ("start", ctypes.c_void_p), ("pos", ctypes.c_void_p),
+                ("head_len", ctypes.c_void_p), ("rotated", ctypes.c_int32)]
+
+
+class TriAttention(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("out", ctypes.c_void_p), ("q_stride_token", ctypes.c_int64), ("q_stride_head", ctypes.c_int64),
+                ("out_stride_token", ctypes.c_int64), ("out_stride_head", ctypes.c_int64), ("scale", ctypes.c_float),
+                ("causal", ctypes.c_int32)]
 
 
 class TriError(RuntimeError):
@@ -88,6 +99,17 @@ def lib():
         L.tri_compress_step_static.restype = i32
         L.tri_compress_step_static.argtypes = [ctypes.POINTER(TriModel), vp, ctypes.POINTER(TriCache),
                                                ctypes.POINTER(TriCache), i32, vp, vp, vp, vp]
+        L.tri_append.restype = i32
+        L.tri_append.argtypes = [ctypes.POINTER(TriModel), ctypes.POINTER(TriCache), i32, ctypes.POINTER(TriTokens), vp, vp, i64, i64, vp, vp]
+        L.tri_attend.restype = i32
+        L.tri_attend.argtypes = [ctypes.POINTER(TriModel), ctypes.POINTER(TriCache), i32, ctypes.POINTER(TriTokens),
+                                 ctypes.POINTER(TriAttention), vp, ctypes.c_size_t, vp]
+        L.tri_attend_shared.restype = i32
+        L.tri_attend_shared.argtypes = [ctypes.POINTER(TriModel), ctypes.POINTER(TriCache), vp, ctypes.POINTER(TriCache), i32,
+                                        ctypes.POINTER(TriTokens), ctypes.POINTER(TriAttention), vp, ctypes.c_size_t, vp]
+        L.tri_attend_workspace_size.restype = ctypes.c_size_t
+        L.tri_attend_workspace_size.argtypes = [ctypes.POINTER(TriModel), ctypes.POINTER(TriCache), ctypes.POINTER(TriCache),
+                                                ctypes.POINTER(TriTokens)]
         L.tri_timing_attach.restype = i32
         L.tri_timing_attach.argtypes = [vp, i32]
         L.tri_timing_detach.restype = i32
@@ -156,13 +178,80 @@ class Cache:
                           0 if block_table is None else block_table.data_ptr(),
                           0 if block_table is None else block_table.shape[1],
                           k.stride(0), k.stride(1), k.stride(2), k.stride(3),
-                          pos.stride(0), pos.stride(1), pos.stride(2), int(bool(k_rotated)))
+                          pos.stride(0), pos.stride(1), pos.stride(2), int(bool(k_rotated)),
+                          0 if block_table is None else k.shape[1])
         if block_table is not None:
             assert block_table.dtype == torch.int32 and block_table.is_contiguous()
 
     @property
     def ref(self):
         return ctypes.byref(self.c)
+
+
+class Tokens:
+    """tri_tokens over torch tensors: a step's new tokens, sequence by sequence.
+
+    pos int32 [T]; start int32 [S + 1] (None: one token per sequence); max_tokens bounds the tokens of one sequence (default T);
+    head_len int32 [L][S][Hkv] or None; rotated: the q and k rows given are post-RoPE already."""
+
+    def __init__(self, pos, start=None, max_tokens=None, head_len=None, rotated=False):
+        for t in (pos, start, head_len):
+            assert t is None or (t.dtype == torch.int32 and t.is_contiguous())
+        self.tensors = (pos, start, head_len)
+        n = pos.numel()
+        self.c = TriTokens(n, n if max_tokens is None else int(max_tokens), None if start is None else start.data_ptr(), pos.data_ptr(),
+                           None if head_len is None else head_len.data_ptr(), int(bool(rotated)))
+
+    @property
+    def ref(self):
+        return ctypes.byref(self.c)
+
+
+def _rows(t, heads, tokens, cache, name):
+    """Rows [T][heads][d] of the cache's type, d dense; any strides of the other two."""
+    if t.dim() != 3 or tuple(t.shape) != (tokens.c.n_tokens, heads, 128) or t.stride(2) != 1:
+        raise ValueError("%s: [%d][%d][128] with dense rows, got %s" % (name, tokens.c.n_tokens, heads, tuple(t.shape)))
+    if t.dtype != cache.tensors[0].dtype:
+        raise TypeError("%s: %s, the cache holds %s" % (name, t.dtype, cache.tensors[0].dtype))
+    return t.stride(0), t.stride(1)
+
+
+def tri_append(model, cache, layer, tokens, k_new, v_new, new_seq_len=None, stream=None):
+    """k_new, v_new [T][Hkv][d], with the same strides, to the end of every sequence of layer `layer`."""
+    strides = _rows(k_new, model.c.n_kv_heads, tokens, cache, "k_new")
+    if _rows(v_new, model.c.n_kv_heads, tokens, cache, "v_new") != strides:
+        raise ValueError("k_new and v_new must have the same strides")
+    _check(lib().tri_append(model.ref, cache.ref, layer, tokens.ref, k_new.data_ptr(), v_new.data_ptr(), strides[0], strides[1],
+                            _p(new_seq_len), _stream(stream)))
+
+
+def _attention(model, cache, tokens, q, out, scale, causal):
+    heads = model.c.n_q_heads
+    qs, os_ = _rows(q, heads, tokens, cache, "q"), _rows(out, heads, tokens, cache, "out")
+    return TriAttention(q.data_ptr(), out.data_ptr(), qs[0], qs[1], os_[0], os_[1], model.c.head_dim ** -0.5 if scale is None else scale,
+                        int(bool(causal)))
+
+
+def tri_attend(model, cache, layer, tokens, q, out, scale=None, causal=True, workspace=None, stream=None):
+    """out [T][Hq][d] <- attention of q [T][Hq][d] over layer `layer` of the cache.  scale None: 1 / sqrt(d)."""
+    at = _attention(model, cache, tokens, q, out, scale, causal)
+    _check(lib().tri_attend(model.ref, cache.ref, layer, tokens.ref, ctypes.byref(at), _p(workspace),
+                            0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)))
+
+
+def tri_attend_shared(model, prefix, group, cache, layer, tokens, q, out, scale=None, causal=True, workspace=None, stream=None):
+    """tri_attend with the keys of shared prefixes: group int32 [P + 1] (first sequence of every prefix's), None for one prefix."""
+    assert group is None or (group.dtype == torch.int32 and group.is_contiguous() and group.numel() == prefix.c.n_seqs + 1)
+    at = _attention(model, cache, tokens, q, out, scale, causal)
+    _check(lib().tri_attend_shared(model.ref, prefix.ref, _p(group), cache.ref, layer, tokens.ref, ctypes.byref(at), _p(workspace),
+                                   0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)))
+
+
+def tri_attend_workspace_size(model, cache, tokens, prefix=None):
+    n = int(lib().tri_attend_workspace_size(model.ref, None if prefix is None else prefix.ref, cache.ref, tokens.ref))
+    if n == ctypes.c_size_t(-1).value:
+        raise TriError(TRI_ERR_INVALID_ARG, lib().tri_last_error().decode())
+    return n
 
 
 def tri_build_centers(model, q_samples, centers_out, stream=None):

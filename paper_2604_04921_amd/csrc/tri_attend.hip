@@ -1,0 +1,326 @@
+// Attention of a step's tokens over a cache (tri_attend, tri_attend_shared): the general kernel (fp32 matrix instructions, any type, any number of rows) and the
+// joining of partial results.
+#include <algorithm>
+
+#include "tri_serve.h"
+
+namespace tri {
+
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kRowTile = 16;        // rows (token, query head of the group) of a workgroup of the general kernel
+constexpr int kAttendThreads = 256;
+constexpr float kNoScore = -__builtin_inff();
+
+template <typename T>
+__device__ __forceinline__ void load4(const char *p, float *x);
+template <>
+__device__ __forceinline__ void load4<float>(const char *p, float *x)
+{
+    const f32x4 u = *reinterpret_cast<const f32x4 *>(p);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = u[e];
+}
+template <>
+__device__ __forceinline__ void load4<__bf16>(const char *p, float *x)
+{
+    const uint2 u = *reinterpret_cast<const uint2 *>(p);
+    x[0] = __uint_as_float(u.x << 16), x[1] = __uint_as_float(u.x & 0xffff0000u);
+    x[2] = __uint_as_float(u.y << 16), x[3] = __uint_as_float(u.y & 0xffff0000u);
+}
+__device__ __forceinline__ void store8(float *p, const float *x)
+{
+    *reinterpret_cast<f32x4 *>(p) = f32x4{x[0], x[1], x[2], x[3]};
+    *reinterpret_cast<f32x4 *>(p + 4) = f32x4{x[4], x[5], x[6], x[7]};
+}
+__device__ __forceinline__ void store8(__bf16 *p, const float *x)
+{
+    typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+    bf16x8 b;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) b[e] = (__bf16)x[e];
+    *reinterpret_cast<bf16x8 *>(p) = b;
+}
+
+// Rotates a lane's 32 elements of a row: x[c][e] is dimension 16 c + 4 kq + e, so both parts of a band lie in one lane in either pair layout.
+__device__ __forceinline__ void rotate32(float (*x)[4], int32_t pos, int kq, int half, const uint64_t *turns)
+{
+    if (half) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint64_t w = turns[16 * c + 4 * kq + e];
+                float cs, sn;
+                turn_exact(phase_of(pos, (uint32_t)w, (uint32_t)(w >> 32)), &cs, &sn);
+                const float re = x[c][e], im = x[c + 4][e];
+                x[c][e] = fmaf(re, cs, -(im * sn));
+                x[c + 4][e] = fmaf(re, sn, im * cs);
+            }
+    } else {
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const uint64_t w = turns[8 * c + 2 * kq + e];
+                float cs, sn;
+                turn_exact(phase_of(pos, (uint32_t)w, (uint32_t)(w >> 32)), &cs, &sn);
+                const float re = x[c][2 * e], im = x[c][2 * e + 1];
+                x[c][2 * e] = fmaf(re, cs, -(im * sn));
+                x[c][2 * e + 1] = fmaf(re, sn, im * cs);
+            }
+    }
+}
+
+// One wave takes 16 keys at a time against 16 rows.  S^T[key][row] = K Q^T and O^T[dim][row] = V^T P^T run on v_mfma_f32_16x16x4_f32, whose lane (m = lane & 15,
+// kq = lane >> 4) holds one element of either operand: contractions may take their terms in any order, so a lane feeds the four dimensions (QK) of a 16-byte piece of
+// its key's row in turn, and O's rows are numbered so that the V rows it loads whole are operands as they are (dimension 64 b + 4 m + e is row m of tile (b, e)).
+// S^T leaves key 4 kq + i of row (lane & 15) in register i, which is where the second product wants it: no data crosses lanes but the
+// maximum and, at the end, the sum over kq.  The maximum is that of the products before the scale, which their differences are multiplied
+// by (a score of 30 powers of two rounded as such is off by 2^-20).  The workgroup's four waves take every fourth tile of the range and join in LDS.
+template <typename T>
+__global__ __launch_bounds__(kAttendThreads) void attend_general_kernel(AttendArgs a)
+{
+    __shared__ uint64_t turns[kBands];
+    __shared__ float wave_m[4][kRowTile], wave_l[4][kRowTile];
+    __shared__ __align__(16) float wave_o[4][kRowTile][kHeadDim + 4];
+    const CacheView &c = a.src.cache;
+    const int H = c.n_kv_heads, G = a.group_size, Hq = H * G;
+    uint32_t w = blockIdx.x;
+    const int rt = w % a.row_tiles;
+    w /= a.row_tiles;
+    const int split = w % a.src.n_split;
+    w /= a.src.n_split;
+    const int h = w % H, s = w / H;
+    const TokenRange tr = tokens_of(a, s);
+    const int rows = tr.n * G, r0 = rt * kRowTile;
+    if (r0 >= rows) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane & 15, kq = lane >> 4;
+    if (tid < kBands) turns[tid] = a.turns.w[tid];
+    __syncthreads();
+    const int n_all = keys_of(a, s, h);
+    const int per = ((n_all + a.src.n_split - 1) / a.src.n_split + 63) & ~63;
+    const int k_lo = min((int64_t)split * per, (int64_t)n_all), k_hi = min(k_lo + per, n_all);
+
+    // this lane's row: column m of S^T and O^T
+    const int r = min(r0 + m, rows - 1), t = tr.t0 + r / G, hq = h * G + r % G;
+    const bool real = r0 + m < rows;
+    const int32_t t_pos = a.pos ? a.pos[t] : 0;
+    float q[8][4];
+    {
+        const char *p = a.q + ((int64_t)t * a.q_stride_token + (int64_t)hq * a.q_stride_head) * (int64_t)sizeof(T);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) load4<T>(p + (16 * j + 4 * kq) * sizeof(T), q[j]);
+        if (a.rotate_q) rotate32(q, t_pos, kq, a.half, turns);
+    }
+    f32x4 o[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float top = kNoScore, sum = 0.f;
+    const int64_t base = (int64_t)a.layer * c.stride_layer + (int64_t)h * c.stride_head;
+    const int64_t pbase = (int64_t)a.layer * c.pos_stride_layer + (int64_t)h * c.pos_stride_head;
+    const int in_block = c.block_shift < 0 ? 0x7fffffff : (1 << c.block_shift) - 1;
+    for (int k0 = k_lo + 16 * wave; k0 < k_hi; k0 += 64) {
+        // lane: key k0 + m of the tile for K, its position and whether it is there
+        const int key = k0 + m;
+        int b = key < k_hi ? s : -1;
+        if (b >= 0 && c.block_shift >= 0) b = block_of(c, a.src.n_blocks, s, key);
+        const int at = key & in_block;
+        float k[8][4];
+        int32_t k_pos = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) k[j][e] = 0.f;
+        if (b >= 0) {
+            const char *p = (const char *)c.k + row_of(c, base, b, at) * (int64_t)sizeof(T);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) load4<T>(p + (16 * j + 4 * kq) * sizeof(T), k[j]);
+            if (a.causal || !c.k_rotated) k_pos = c.pos[pbase + (int64_t)b * c.pos_stride_sb + at];
+            if (!c.k_rotated) rotate32(k, k_pos, kq, a.half, turns);
+        }
+        f32x4 sc = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sc = __builtin_amdgcn_mfma_f32_16x16x4f32(k[j][e], q[j][e], sc, 0, 0, 0);
+        // the keys this lane has scores of (and whose V rows it loads): 4 kq + i
+        bool keep[4];
+        float v[4][2][4];
+        bool hole = false, odd = false;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int from = 4 * kq + i;
+            const int vb = __shfl(b, from);
+            const int32_t vp = __shfl(k_pos, from);
+            keep[i] = vb >= 0 && (!a.causal || vp <= t_pos);
+            hole |= real && vb >= 0 && !keep[i];
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[i][j][e] = 0.f;
+            if (vb >= 0) {
+                const char *p = (const char *)c.v + row_of(c, base, vb, (k0 + from) & in_block) * (int64_t)sizeof(T);
+                load4<T>(p + 4 * m * sizeof(T), v[i][0]);
+                load4<T>(p + (64 + 4 * m) * sizeof(T), v[i][1]);
+            }
+        }
+        float best = kNoScore;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            sc[i] = keep[i] ? sc[i] : kNoScore;
+            best = fmaxf(best, sc[i]);
+        }
+        best = fmaxf(best, __shfl_xor(best, 16));
+        best = fmaxf(best, __shfl_xor(best, 32));
+        const float next = fmaxf(top, best), ref = next == kNoScore ? 0.f : next;
+        const float shrink = __builtin_amdgcn_exp2f((top - ref) * a.scale_log2);   // (no score yet: 2^-inf = 0)
+        top = next;
+        sum *= shrink;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) o[j] *= shrink;
+        float p[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            p[i] = keep[i] ? __builtin_amdgcn_exp2f((sc[i] - ref) * a.scale_log2) : 0.f;
+            sum += p[i];
+        }
+        // A value that is not finite must not reach rows that do not attend to its key (0 times it is no 0).  Where a row of the tile leaves a key out, such values
+        // are taken out of the product and added as what they are, by products of "attends" with "is +inf or NaN" and "is -inf or NaN".
+        if (__ballot(hole)) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) odd |= !(fabsf(v[i][j][e]) < __builtin_inff());
+            if (__ballot(odd)) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        f32x4 up = f32x4{0.f, 0.f, 0.f, 0.f}, down = up;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float x = v[i][j][e], on = keep[i] ? 1.f : 0.f;
+                            up = __builtin_amdgcn_mfma_f32_16x16x4f32(x < __builtin_inff() ? 0.f : 1.f, on, up, 0, 0, 0);
+                            down = __builtin_amdgcn_mfma_f32_16x16x4f32(x > -__builtin_inff() ? 0.f : 1.f, on, down, 0, 0, 0);
+                            if (!(fabsf(x) < __builtin_inff())) v[i][j][e] = 0.f;
+                        }
+#pragma unroll
+                        for (int d = 0; d < 4; ++d) o[4 * j + e][d] += (up[d] > 0.f ? __builtin_inff() : 0.f) + (down[d] > 0.f ? -__builtin_inff() : 0.f);
+                    }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[4 * j + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[i][j][e], p[i], o[4 * j + e], 0, 0, 0);
+    }
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+    if (kq == 0) wave_m[wave][m] = top, wave_l[wave][m] = sum;
+    __syncthreads();
+    float all = kNoScore;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) all = fmaxf(all, wave_m[j][m]);
+    const float mine = __builtin_amdgcn_exp2f((top - (all == kNoScore ? 0.f : all)) * a.scale_log2);
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int d = 0; d < 4; ++d)   // dimensions 64 j + 16 kq + 4 d + e
+            *reinterpret_cast<f32x4 *>(&wave_o[wave][m][64 * j + 16 * kq + 4 * d]) =
+                f32x4{o[4 * j][d], o[4 * j + 1][d], o[4 * j + 2][d], o[4 * j + 3][d]} * mine;
+    __syncthreads();
+    const int row = tid >> 4, d0 = 8 * (tid & 15);
+    if (r0 + row >= rows) return;
+    float best = kNoScore, total = 0.f, x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) best = fmaxf(best, wave_m[j][row]);
+    const float ref = best == kNoScore ? 0.f : best;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        total += wave_l[j][row] * __builtin_amdgcn_exp2f((wave_m[j][row] - ref) * a.scale_log2);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] += wave_o[j][row][d0 + e];
+    }
+    const int ot = tr.t0 + (r0 + row) / G, oh = h * G + (r0 + row) % G;
+    if (a.part_o) {
+        const int64_t at = ((int64_t)(a.src.part0 + split) * a.n_tokens + ot) * Hq + oh;
+        if (d0 == 0) a.part_ml[at] = make_float2(best, total);
+        store8(a.part_o + at * kHeadDim + d0, x);
+        return;
+    }
+    const float inv = 1.f / total;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = total != 0.f ? x[e] * inv : 0.f;   // (no key: zeros; scores that are no number: NaN)
+    store8(reinterpret_cast<T *>(a.out) + (int64_t)ot * a.out_stride_token + (int64_t)oh * a.out_stride_head + d0, x);
+}
+
+// Joins the parts of a row: sixteen threads a row, 8 dimensions each.
+template <typename T>
+__global__ __launch_bounds__(kAttendThreads) void join_kernel(const float *part_o, const float2 *part_ml, char *out, int64_t out_stride_token,
+                                                              int64_t out_stride_head, int32_t n_q_heads, int64_t n_rows, int32_t parts, float scale_log2)
+{
+    const int64_t row = (int64_t)blockIdx.x * (kAttendThreads / 16) + (threadIdx.x >> 4);
+    const int d0 = 8 * (threadIdx.x & 15);
+    if (row >= n_rows) return;
+    float best = kNoScore;
+    for (int p = 0; p < parts; ++p) best = fmaxf(best, part_ml[p * n_rows + row].x);
+    float total = 0.f, x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    const float ref = best == kNoScore ? 0.f : best;
+    for (int p = 0; p < parts; ++p) {
+        const float2 ml = part_ml[p * n_rows + row];
+        if (ml.y != 0.f) {   // (a part without a key has nothing to bring)
+            const float f = __builtin_amdgcn_exp2f((ml.x - ref) * scale_log2);
+            total += f * ml.y;
+            const f32x4 *po = reinterpret_cast<const f32x4 *>(part_o + (p * n_rows + row) * kHeadDim + d0);
+            const f32x4 lo = po[0], hi = po[1];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] += f * lo[e], x[4 + e] += f * hi[e];
+        }
+    }
+    const float inv = 1.f / total;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = total != 0.f ? x[e] * inv : 0.f;
+    const int64_t t = row / n_q_heads, h = row - t * n_q_heads;
+    store8(reinterpret_cast<T *>(out) + t * out_stride_token + h * out_stride_head + d0, x);
+}
+
+}  // namespace
+
+int32_t attend_splits(const tri_model &m, const tri_cache &c, int32_t max_tokens, int32_t n_tokens)
+{
+    (void)n_tokens;
+    const int64_t G = m.n_q_heads / m.n_kv_heads;
+    const int64_t tiles = ((int64_t)max_tokens * G + kRowTile - 1) / kRowTile;
+    const int64_t units = std::max<int64_t>((int64_t)c.n_seqs * m.n_kv_heads * tiles, 1);
+    const int64_t most = std::max<int64_t>(((int64_t)c.max_seq_len + 255) / 256, 1);
+    return (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(most, 256), (1024 + units - 1) / units));
+}
+
+tri_status launch_attend(AttendArgs a, int32_t dtype, hipStream_t st)
+{
+    a.row_tiles = (int32_t)(((int64_t)a.src.max_tokens * a.group_size + kRowTile - 1) / kRowTile);
+    const int64_t blocks = (int64_t)a.row_tiles * a.src.n_split * a.src.cache.n_kv_heads * a.src.cache.n_seqs;
+    if (dtype == TRI_BF16) attend_general_kernel<__bf16><<<(uint32_t)blocks, kAttendThreads, 0, st>>>(a);
+    else attend_general_kernel<float><<<(uint32_t)blocks, kAttendThreads, 0, st>>>(a);
+    return hip_status("attend_general_kernel");
+}
+
+tri_status launch_join(const AttendArgs &a, int32_t parts, int32_t n_q_heads, int32_t dtype, hipStream_t st)
+{
+    const int64_t rows = (int64_t)a.n_tokens * n_q_heads;
+    const uint32_t blocks = (uint32_t)((rows + kAttendThreads / 16 - 1) / (kAttendThreads / 16));
+    if (dtype == TRI_BF16)
+        join_kernel<__bf16><<<blocks, kAttendThreads, 0, st>>>(a.part_o, a.part_ml, a.out, a.out_stride_token, a.out_stride_head, n_q_heads, rows, parts, a.scale_log2);
+    else
+        join_kernel<float><<<blocks, kAttendThreads, 0, st>>>(a.part_o, a.part_ml, a.out, a.out_stride_token, a.out_stride_head, n_q_heads, rows, parts, a.scale_log2);
+    return hip_status("join_kernel");
+}
+
+}  // namespace tri
