@@ -2,17 +2,18 @@
 // joining of partial results.
 #include <algorithm>
 
-#include "tri_serve.h"
+#include "tri_attend_common.h"
 
 namespace tri {
 
 namespace {
 
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-
 constexpr int kRowTile = 16;        // rows (token, query head of the group) of a workgroup of the general kernel
 constexpr int kAttendThreads = 256;
-constexpr float kNoScore = -__builtin_inff();
+#ifndef WANTED
+#define WANTED 3072
+#endif
+constexpr int64_t kWantedGroups = WANTED;
 
 template <typename T>
 __device__ __forceinline__ void load4(const char *p, float *x);
@@ -30,20 +31,6 @@ __device__ __forceinline__ void load4<__bf16>(const char *p, float *x)
     x[0] = __uint_as_float(u.x << 16), x[1] = __uint_as_float(u.x & 0xffff0000u);
     x[2] = __uint_as_float(u.y << 16), x[3] = __uint_as_float(u.y & 0xffff0000u);
 }
-__device__ __forceinline__ void store8(float *p, const float *x)
-{
-    *reinterpret_cast<f32x4 *>(p) = f32x4{x[0], x[1], x[2], x[3]};
-    *reinterpret_cast<f32x4 *>(p + 4) = f32x4{x[4], x[5], x[6], x[7]};
-}
-__device__ __forceinline__ void store8(__bf16 *p, const float *x)
-{
-    typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-    bf16x8 b;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) b[e] = (__bf16)x[e];
-    *reinterpret_cast<bf16x8 *>(p) = b;
-}
-
 // Rotates a lane's 32 elements of a row: x[c][e] is dimension 16 c + 4 kq + e, so both parts of a band lie in one lane in either pair layout.
 __device__ __forceinline__ void rotate32(float (*x)[4], int32_t pos, int kq, int half, const uint64_t *turns)
 {
@@ -100,9 +87,8 @@ __global__ __launch_bounds__(kAttendThreads) void attend_general_kernel(AttendAr
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane & 15, kq = lane >> 4;
     if (tid < kBands) turns[tid] = a.turns.w[tid];
     __syncthreads();
-    const int n_all = keys_of(a, s, h);
-    const int per = ((n_all + a.src.n_split - 1) / a.src.n_split + 63) & ~63;
-    const int k_lo = min((int64_t)split * per, (int64_t)n_all), k_hi = min(k_lo + per, n_all);
+    const KeyRange range = keys_of_split(a, s, h, split);
+    const int k_lo = range.lo, k_hi = range.hi;
 
     // this lane's row: column m of S^T and O^T
     const int r = min(r0 + m, rows - 1), t = tr.t0 + r / G, hq = h * G + r % G;
@@ -248,17 +234,7 @@ __global__ __launch_bounds__(kAttendThreads) void attend_general_kernel(AttendAr
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] += wave_o[j][row][d0 + e];
     }
-    const int ot = tr.t0 + (r0 + row) / G, oh = h * G + (r0 + row) % G;
-    if (a.part_o) {
-        const int64_t at = ((int64_t)(a.src.part0 + split) * a.n_tokens + ot) * Hq + oh;
-        if (d0 == 0) a.part_ml[at] = make_float2(best, total);
-        store8(a.part_o + at * kHeadDim + d0, x);
-        return;
-    }
-    const float inv = 1.f / total;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = total != 0.f ? x[e] * inv : 0.f;   // (no key: zeros; scores that are no number: NaN)
-    store8(reinterpret_cast<T *>(a.out) + (int64_t)ot * a.out_stride_token + (int64_t)oh * a.out_stride_head + d0, x);
+    finish_row<T>(a, split, tr.t0 + (r0 + row) / G, h * G + (r0 + row) % G, Hq, d0, best, total, x);
 }
 
 // Joins the parts of a row: sixteen threads a row, 8 dimensions each.
@@ -293,21 +269,29 @@ __global__ __launch_bounds__(kAttendThreads) void join_kernel(const float *part_
 
 }  // namespace
 
+// Which kernel takes a call: the bf16 ones need pages of sixteen slots, and 32 rows' addresses within 32 bits.
+static bool rows_kernel(const tri_cache &c, int64_t rows)
+{
+    return c.dtype == TRI_BF16 && (c.block_size == 0 || c.block_size >= 16) && c.stride_slot < (1 << 24) && rows <= 32;
+}
+
 int32_t attend_splits(const tri_model &m, const tri_cache &c, int32_t max_tokens, int32_t n_tokens)
 {
     (void)n_tokens;
-    const int64_t G = m.n_q_heads / m.n_kv_heads;
-    const int64_t tiles = ((int64_t)max_tokens * G + kRowTile - 1) / kRowTile;
+    const int64_t rows = (int64_t)max_tokens * (m.n_q_heads / m.n_kv_heads);
+    const int64_t tiles = rows_kernel(c, rows) ? 1 : (rows + kRowTile - 1) / kRowTile;
     const int64_t units = std::max<int64_t>((int64_t)c.n_seqs * m.n_kv_heads * tiles, 1);
     const int64_t most = std::max<int64_t>(((int64_t)c.max_seq_len + 255) / 256, 1);
-    return (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(most, 256), (1024 + units - 1) / units));
+    return (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(most, 256), (kWantedGroups + units - 1) / units));
 }
 
-tri_status launch_attend(AttendArgs a, int32_t dtype, hipStream_t st)
+tri_status launch_attend(AttendArgs a, const tri_cache &c, hipStream_t st)
 {
-    a.row_tiles = (int32_t)(((int64_t)a.src.max_tokens * a.group_size + kRowTile - 1) / kRowTile);
+    const int64_t rows = (int64_t)a.src.max_tokens * a.group_size;
+    if (rows_kernel(c, rows)) return launch_attend_rows(a, (int32_t)rows, st);
+    a.row_tiles = (int32_t)((rows + kRowTile - 1) / kRowTile);
     const int64_t blocks = (int64_t)a.row_tiles * a.src.n_split * a.src.cache.n_kv_heads * a.src.cache.n_seqs;
-    if (dtype == TRI_BF16) attend_general_kernel<__bf16><<<(uint32_t)blocks, kAttendThreads, 0, st>>>(a);
+    if (c.dtype == TRI_BF16) attend_general_kernel<__bf16><<<(uint32_t)blocks, kAttendThreads, 0, st>>>(a);
     else attend_general_kernel<float><<<(uint32_t)blocks, kAttendThreads, 0, st>>>(a);
     return hip_status("attend_general_kernel");
 }

@@ -1,0 +1,118 @@
+// What the attention kernels share.
+#pragma once
+
+#include "tri_serve.h"
+
+namespace tri {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+constexpr float kNoScore = -__builtin_inff();
+constexpr int kNonTemporal = 2;   // the cache policy operand of buffer loads
+
+__device__ __forceinline__ void store8(float *p, const float *x)
+{
+    *reinterpret_cast<f32x4 *>(p) = f32x4{x[0], x[1], x[2], x[3]};
+    *reinterpret_cast<f32x4 *>(p + 4) = f32x4{x[4], x[5], x[6], x[7]};
+}
+__device__ __forceinline__ void store8(__bf16 *p, const float *x)
+{
+    bf16x8 b;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) b[e] = (__bf16)x[e];
+    *reinterpret_cast<bf16x8 *>(p) = b;
+}
+template <typename U>
+__device__ __forceinline__ uint4 as_uint4(const U &u) { return __builtin_bit_cast(uint4, u); }
+__device__ __forceinline__ void widen8(const uint4 &u, float *x)
+{
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(w[i] << 16), x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+}
+
+// The keys of a part: split's share of the sequence's keys, in whole groups of 128 (pages of sixteen and more are not cut by a tile of 32 or 16).
+struct KeyRange {
+    int lo, hi;
+};
+__device__ __forceinline__ KeyRange keys_of_split(const AttendArgs &a, int s, int h, int split)
+{
+    const int n = keys_of(a, s, h);
+    const int64_t per = (((int64_t)n + a.src.n_split - 1) / a.src.n_split + 127) & ~(int64_t)127;
+    const int lo = (int)min(split * per, (int64_t)n);
+    return KeyRange{lo, (int)min(lo + per, (int64_t)n)};
+}
+
+// lane ^ 8 of each sixteen
+__device__ __forceinline__ float across_8(float x) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x128, 0xf, 0xf, false)); }
+// the maximum over the four lanes that share lane & 15
+__device__ __forceinline__ float max_over_kq(float x)
+{
+    auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
+// Element e of eight rows' pieces: v[i][j] is the piece of key 4 i + j of the lane's eight.
+__device__ __forceinline__ bf16x8 column(const uint4 (&v)[2][4], int e)
+{
+    const uint32_t pick = e & 1 ? 0x07060302u : 0x05040100u;
+    auto word = [&](const uint4 &u) { return e < 4 ? (e < 2 ? u.x : u.y) : (e < 6 ? u.z : u.w); };
+    uint4 r;
+    r.x = __builtin_amdgcn_perm(word(v[0][1]), word(v[0][0]), pick);
+    r.y = __builtin_amdgcn_perm(word(v[0][3]), word(v[0][2]), pick);
+    r.z = __builtin_amdgcn_perm(word(v[1][1]), word(v[1][0]), pick);
+    r.w = __builtin_amdgcn_perm(word(v[1][3]), word(v[1][2]), pick);
+    return __builtin_bit_cast(bf16x8, r);
+}
+__device__ __forceinline__ bool not_finite(const uint4 &u)
+{
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) odd |= (w[i] & 0x7f80u) == 0x7f80u || (w[i] & 0x7f800000u) == 0x7f800000u;
+    return odd;
+}
+__device__ __forceinline__ uint4 finite_only(const uint4 &u)
+{
+    uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if ((w[i] & 0x7f80u) == 0x7f80u) w[i] &= 0xffff0000u;
+        if ((w[i] & 0x7f800000u) == 0x7f800000u) w[i] &= 0xffffu;
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// 1 where an element is the infinity `which` (0x7f80 or 0xff80) or NaN, else 0
+__device__ __forceinline__ bf16x8 where_not_below(const bf16x8 &x, uint32_t which)
+{
+    bf16x8 r;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const uint32_t b = __builtin_bit_cast(uint16_t, (__bf16)x[e]);
+        r[e] = b == which || (b & 0x7fffu) > 0x7f80u ? (__bf16)1.f : (__bf16)0.f;
+    }
+    return r;
+}
+
+// Eight dimensions of a row whose keys are all seen to: to the output, or as a part.
+template <typename T>
+__device__ __forceinline__ void finish_row(const AttendArgs &a, int split, int t, int hq, int Hq, int d0, float best, float total, float *x)
+{
+    if (a.part_o) {
+        const int64_t at = ((int64_t)(a.src.part0 + split) * a.n_tokens + t) * Hq + hq;
+        if (d0 == 0) a.part_ml[at] = make_float2(best, total);
+        store8(a.part_o + at * kHeadDim + d0, x);
+        return;
+    }
+    const float inv = 1.f / total;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = total != 0.f ? x[e] * inv : 0.f;   // (no key: zeros; scores that are no number: NaN)
+    store8(reinterpret_cast<T *>(a.out) + (int64_t)t * a.out_stride_token + (int64_t)hq * a.out_stride_head + d0, x);
+}
+
+tri_status launch_attend_rows(AttendArgs a, int32_t rows, hipStream_t st);
+
+}  // namespace tri

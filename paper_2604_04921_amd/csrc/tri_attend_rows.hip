@@ -1,0 +1,384 @@
+// Attention with few rows per KV head (decoding): bf16, contiguous caches or pages of at least sixteen slots, up to 32 rows (token, query head of the group).
+#include <algorithm>
+
+#include "tri_attend_common.h"
+
+namespace tri {
+
+namespace {
+
+constexpr int kRowsThreads = 256;
+constexpr int kRowsTile = 32;   // keys a wave takes at a time
+
+// Both halves of a wave's 64-byte pieces of a K row lie with one lane: x[c][e] is dimension 32 c + 8 kq + e.
+template <bool EXACT>
+__device__ __forceinline__ void rotate_row(float (*x)[8], int32_t pos, int kq, int half, const uint64_t *turns)
+{
+    if (half) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint64_t w = turns[32 * c + 8 * kq + e];
+                float cs, sn;
+                const uint32_t phase = phase_of(pos, (uint32_t)w, (uint32_t)(w >> 32));
+                if (EXACT) turn_exact(phase, &cs, &sn);
+                else turn_fast(phase, &cs, &sn);
+                const float re = x[c][e], im = x[c + 2][e];
+                x[c][e] = fmaf(re, cs, -(im * sn));
+                x[c + 2][e] = fmaf(re, sn, im * cs);
+            }
+    } else {
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint64_t w = turns[16 * c + 4 * kq + e];
+                float cs, sn;
+                const uint32_t phase = phase_of(pos, (uint32_t)w, (uint32_t)(w >> 32));
+                if (EXACT) turn_exact(phase, &cs, &sn);
+                else turn_fast(phase, &cs, &sn);
+                const float re = x[c][2 * e], im = x[c][2 * e + 1];
+                x[c][2 * e] = fmaf(re, cs, -(im * sn));
+                x[c][2 * e + 1] = fmaf(re, sn, im * cs);
+            }
+    }
+}
+
+// NT column tiles of sixteen rows against 32 keys at a time.  S^T[key][row] = K Q^T and O^T[dim][row] = V^T P^T run on v_mfma_f32_16x16x32_bf16; a lane (m = lane & 15,
+// kq = lane >> 4) holds eight terms of either operand, and since a contraction may take its terms in any order, it loads what is whole in memory: K operands are 16-byte
+// pieces of the key's row; of V it loads pieces m of the rows of the eight keys whose weights it holds (4 kq + r of both halves of the tile: where the first product
+// leaves them), and 32 byte permutations turn the 8 x 8 block in registers, row m of the product's tile e then being dimension 8 m + e.  Nothing passes through LDS
+// or between lanes until the end but the maximum, so waves run on their own, 16 KB of loads under way each, and what bounds the kernel is the cache's bytes.
+// LO: columns 8 to 15 of a tile hold what the rounding to bf16 takes off the rows 0 to 7 (of q turned by its position, and of the weights): the matrix
+// instructions have that room where rows are at most eight to a tile, and both products are as good as in 16 bits of fraction.  Keys turned on the way (TURN)
+// are multiplied as two bf16 numbers for the same reason.  Without LO, q and the weights are rounded to bf16 once.
+template <int NT, bool LO, bool PAGED, bool TURN>
+__global__ __launch_bounds__(kRowsThreads, 2) void attend_rows_kernel(AttendArgs a)
+{
+    constexpr int kCols = LO ? 8 : 16, kRows = kCols * NT;
+    __shared__ __align__(16) uint64_t turns[kBands];
+    __shared__ float wave_m[4][kRows], wave_l[4][kRows];
+    __shared__ __align__(16) float wave_o[4][kRows][kHeadDim + 4];
+    const CacheView &c = a.src.cache;
+    const int H = c.n_kv_heads, G = a.group_size, Hq = H * G;
+    uint32_t w = blockIdx.x;
+    const int rt = w % a.row_tiles;
+    w /= a.row_tiles;
+    const int split = w % a.src.n_split;
+    w /= a.src.n_split;
+    const int h = w % H, s = w / H;
+    const TokenRange tr = tokens_of(a, s);
+    const int rows = tr.n * G, r0 = rt * kRows;
+    if (r0 >= rows) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15, kq = lane >> 4;
+    if (tid < kBands) turns[tid] = a.turns.w[tid];
+    __syncthreads();
+    const KeyRange range = keys_of_split(a, s, h, split);
+    const int k_hi = __builtin_amdgcn_readfirstlane(range.hi);   // (what buffer descriptors are made of stays in scalar registers)
+
+    // this lane's rows: columns m of the column tiles
+    bf16x8 q[NT][4];
+    int32_t t_pos[NT], first_pos = 0x7fffffff;
+    bool real[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const int at = r0 + n * kCols + (LO ? m & 7 : m), r = min(at, rows - 1), t = tr.t0 + r / G, hq = h * G + r % G;
+        real[n] = at < rows;
+        t_pos[n] = a.causal ? a.pos[t] : 0x7fffffff;
+        first_pos = min(first_pos, t_pos[n]);
+        const char *p = a.q + ((int64_t)t * a.q_stride_token + (int64_t)hq * a.q_stride_head) * 2;
+        float x[4][8];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) widen8(*reinterpret_cast<const uint4 *>(p + 64 * j + 16 * kq), x[j]);
+        if (a.rotate_q) rotate_row<true>(x, a.pos[t], kq, a.half, turns);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const __bf16 hi = (__bf16)x[j][e];
+                q[n][j][e] = LO && m >= 8 ? (__bf16)(x[j][e] - (float)hi) : hi;
+            }
+    }
+#pragma unroll
+    for (int x = 1; x < 16; x *= 2) first_pos = min(first_pos, __shfl_xor(first_pos, x));
+    first_pos = __builtin_amdgcn_readfirstlane(first_pos);
+
+    f32x4 o[NT][8];
+    float top[NT], sum[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        top[n] = kNoScore;
+        sum[n] = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[n][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    const int64_t base = (int64_t)a.layer * c.stride_layer + (int64_t)h * c.stride_head;
+    const int64_t pbase = (int64_t)a.layer * c.pos_stride_layer + (int64_t)h * c.pos_stride_head;
+    const uint32_t sb = (uint32_t)c.stride_slot * 2u;
+    const uint32_t lane_k = m * sb + kq * 16;
+    uint32_t lane_v[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) lane_v[j] = (4 * kq + j) * sb + m * 16;
+    const bool need_pos = a.causal || TURN;
+
+    // Sixteen keys: where their rows begin and how many there are (0: none, or their block is not there).  Lanes beyond the last row lie beyond the buffer and load zeros.
+    struct Rows {
+        int64_t kv, pos;
+        int n;
+    };
+    auto find = [&](int k0, int block) {
+        Rows r;
+        const int left = min(max(k_hi - k0, 0), 16);
+        if (PAGED) {
+            const int in = k0 & ((1 << c.block_shift) - 1);
+            r.n = block < 0 || (a.src.n_blocks > 0 && block >= a.src.n_blocks) ? 0 : left;
+            const int b = r.n ? block : 0;
+            r.kv = base + (int64_t)b * c.stride_sb + (int64_t)in * c.stride_slot;
+            r.pos = pbase + (int64_t)b * c.pos_stride_sb + in;
+        } else {
+            r.n = left;
+            r.kv = base + (int64_t)s * c.stride_sb + (int64_t)k0 * c.stride_slot;
+            r.pos = pbase + (int64_t)s * c.pos_stride_sb + k0;
+        }
+        return r;
+    };
+    auto block_at = [&](int k0) {
+        return PAGED ? __builtin_amdgcn_readfirstlane(c.block_table[(int64_t)s * c.max_blocks + (min(k0, max(k_hi - 1, 0)) >> c.block_shift)]) : 0;
+    };
+    auto rsrc = [&](const void *p, int64_t at, int n) {
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>((const char *)p) + at * 2, 0, n > 0 ? (n - 1) * sb + kHeadDim * 2 : 0, 0x00027000);
+    };
+    uint4 k[2][4], v[2][4];
+    int32_t k_pos[2];
+    auto load_k = [&](const Rows (&r)[2]) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const auto b = rsrc(c.k, r[i].kv, r[i].n);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) k[i][j] = as_uint4(__builtin_amdgcn_raw_buffer_load_b128(b, lane_k + 64 * j, 0, kNonTemporal));
+            const auto p = __builtin_amdgcn_make_buffer_rsrc(const_cast<int32_t *>(c.pos) + r[i].pos, 0, need_pos ? r[i].n * 4 : 0, 0x00027000);
+            k_pos[i] = __builtin_amdgcn_raw_buffer_load_b32(p, m * 4, 0, 0);
+        }
+    };
+    auto load_v = [&](const Rows (&r)[2]) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const auto b = rsrc(c.v, r[i].kv, r[i].n);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[i][j] = as_uint4(__builtin_amdgcn_raw_buffer_load_b128(b, lane_v[j], 0, kNonTemporal));
+        }
+    };
+    constexpr int kStep = 4 * kRowsTile;
+    int k0 = __builtin_amdgcn_readfirstlane(range.lo) + kRowsTile * wave;
+    Rows here[2] = {find(k0, block_at(k0)), find(k0 + 16, block_at(k0 + 16))};
+    int ahead[2] = {block_at(k0 + kStep), block_at(k0 + kStep + 16)};
+    load_k(here);
+    load_v(here);
+    for (; k0 < k_hi; k0 += kStep) {
+        const Rows next[2] = {find(k0 + kStep, ahead[0]), find(k0 + kStep + 16, ahead[1])};
+        ahead[0] = block_at(k0 + 2 * kStep);
+        ahead[1] = block_at(k0 + 2 * kStep + 16);
+        f32x4 sc[2][NT];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) sc[i][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (TURN) {
+                float x[4][8];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) widen8(k[i][j], x[j]);
+                rotate_row<false>(x, k_pos[i], kq, a.half, turns);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    bf16x8 hi, lo;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) hi[e] = (__bf16)x[j][e], lo[e] = (__bf16)(x[j][e] - (float)hi[e]);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        sc[i][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi, q[n][j], sc[i][n], 0, 0, 0);
+                        sc[i][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lo, q[n][j], sc[i][n], 0, 0, 0);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+                        sc[i][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[i][j]), q[n][j], sc[i][n], 0, 0, 0);
+            }
+        }
+        const int32_t pos_here[2] = {k_pos[0], k_pos[1]};
+        load_k(next);
+        if (LO) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int d = 0; d < 4; ++d) sc[i][n][d] += across_8(sc[i][n][d]);
+        }
+        // keys that are not there, or behind the position of one of the rows
+        const bool late = a.causal && __ballot(pos_here[0] > first_pos || pos_here[1] > first_pos);
+        uint32_t keep[NT];   // bit 4 i + d: key 16 i + 4 kq + d is attended to
+        bool hole = false;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) keep[n] = 0xffu;
+        if (late || here[0].n < 16 || here[1].n < 16) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int d = 0; d < 4; ++d) {
+                    const bool there = 4 * kq + d < here[i].n;
+                    const int32_t p = __shfl(pos_here[i], 4 * kq + d);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        const bool on = there && (!a.causal || p <= t_pos[n]);
+                        if (!on) keep[n] &= ~(1u << (4 * i + d)), sc[i][n][d] = kNoScore;
+                        hole |= there && !on && real[n];
+                    }
+                }
+        }
+        bf16x8 weight[NT];
+        float best[NT];
+        bool higher = false;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            best[n] = kNoScore;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int d = 0; d < 4; ++d) best[n] = fmaxf(best[n], sc[i][n][d]);
+            best[n] = max_over_kq(best[n]);
+            higher |= best[n] > top[n];
+        }
+        if (__ballot(higher)) {   // (rare after the first tiles)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const float next_top = fmaxf(top[n], best[n]);
+                const float shrink = next_top == kNoScore ? 1.f : __builtin_amdgcn_exp2f((top[n] - next_top) * a.scale_log2);
+                top[n] = next_top;
+                sum[n] *= shrink;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) o[n][e] *= shrink;
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const float ref = top[n] == kNoScore ? 0.f : top[n];
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int d = 0; d < 4; ++d) {
+                    const float p = __builtin_amdgcn_exp2f((sc[i][n][d] - ref) * a.scale_log2);
+                    sum[n] += p;
+                    const __bf16 hi = (__bf16)p;
+                    weight[n][4 * i + d] = LO && m >= 8 ? (__bf16)(p - (float)hi) : hi;
+                }
+        }
+        if (__ballot(hole)) {   // (see attend_general_kernel: values that are not finite and not everyone's)
+            bool odd = false;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) odd |= not_finite(v[i][j]);
+            if (__ballot(odd)) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const bf16x8 x = column(v, e), up_at = where_not_below(x, 0x7f80), down_at = where_not_below(x, 0xff80);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        bf16x8 on;
+#pragma unroll
+                        for (int d = 0; d < 8; ++d) on[d] = (keep[n] >> d) & 1 ? (__bf16)1.f : (__bf16)0.f;
+                        const f32x4 none = f32x4{0.f, 0.f, 0.f, 0.f};
+                        const f32x4 up = __builtin_amdgcn_mfma_f32_16x16x32_bf16(up_at, on, none, 0, 0, 0);
+                        const f32x4 down = __builtin_amdgcn_mfma_f32_16x16x32_bf16(down_at, on, none, 0, 0, 0);
+#pragma unroll
+                        for (int d = 0; d < 4; ++d) o[n][e][d] += (up[d] > 0.f ? __builtin_inff() : 0.f) + (down[d] > 0.f ? -__builtin_inff() : 0.f);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) v[i][j] = finite_only(v[i][j]);
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const bf16x8 x = column(v, e);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) o[n][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, weight[n], o[n][e], 0, 0, 0);
+        }
+        load_v(next);
+        here[0] = next[0];
+        here[1] = next[1];
+    }
+    // join the waves: O's lane has dimensions 32 kq + 8 d + e of its row
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        sum[n] += __shfl_xor(sum[n], 16);
+        sum[n] += __shfl_xor(sum[n], 32);
+        if (kq == 0 && (!LO || m < 8)) wave_m[wave][n * kCols + m] = top[n], wave_l[wave][n * kCols + m] = sum[n];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const int at = n * kCols + (LO ? m & 7 : m);
+        float all = kNoScore;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) all = fmaxf(all, wave_m[j][at]);
+        const float mine = __builtin_amdgcn_exp2f((top[n] - (all == kNoScore ? 0.f : all)) * a.scale_log2);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+#pragma unroll
+            for (int d = 0; d < 4; ++d) o[n][e][d] = (LO ? o[n][e][d] + across_8(o[n][e][d]) : o[n][e][d]) * mine;
+        if (!LO || m < 8)
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+#pragma unroll
+                for (int e = 0; e < 8; e += 4)
+                    *reinterpret_cast<f32x4 *>(&wave_o[wave][at][32 * kq + 8 * d + e]) = f32x4{o[n][e][d], o[n][e + 1][d], o[n][e + 2][d], o[n][e + 3][d]};
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kRows / 16 + (kRows < 16); ++i) {
+        const int row = 16 * i + (tid >> 4), d0 = 8 * (tid & 15);
+        if (row >= kRows || r0 + row >= rows) break;
+        float best = kNoScore, total = 0.f, x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) best = fmaxf(best, wave_m[j][row]);
+        const float ref = best == kNoScore ? 0.f : best;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            total += wave_l[j][row] * __builtin_amdgcn_exp2f((wave_m[j][row] - ref) * a.scale_log2);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] += wave_o[j][row][d0 + e];
+        }
+        finish_row<__bf16>(a, split, tr.t0 + (r0 + row) / G, h * G + (r0 + row) % G, Hq, d0, best, total, x);
+    }
+}
+
+template <int NT, bool LO>
+void launch_rows_of(const AttendArgs &a, uint32_t blocks, hipStream_t st)
+{
+    const bool paged = a.src.cache.block_shift >= 0, turn = !a.src.cache.k_rotated;
+    if (paged && turn) attend_rows_kernel<NT, LO, true, true><<<blocks, kRowsThreads, 0, st>>>(a);
+    else if (paged) attend_rows_kernel<NT, LO, true, false><<<blocks, kRowsThreads, 0, st>>>(a);
+    else if (turn) attend_rows_kernel<NT, LO, false, true><<<blocks, kRowsThreads, 0, st>>>(a);
+    else attend_rows_kernel<NT, LO, false, false><<<blocks, kRowsThreads, 0, st>>>(a);
+}
+
+}  // namespace
+
+tri_status launch_attend_rows(AttendArgs a, int32_t rows, hipStream_t st)
+{
+    a.row_tiles = 1;
+    const uint32_t blocks = (uint32_t)((int64_t)a.src.n_split * a.src.cache.n_kv_heads * a.src.cache.n_seqs);
+    if (rows <= 8) launch_rows_of<1, true>(a, blocks, st);
+    else if (rows <= 16) launch_rows_of<2, true>(a, blocks, st);
+    else launch_rows_of<2, false>(a, blocks, st);
+    return hip_status("attend_rows_kernel");
+}
+
+}  // namespace tri
