@@ -11,38 +11,21 @@ constexpr int kRowsThreads = 256;
 constexpr int kRowsTile = 32;   // keys a wave takes at a time
 
 // Both halves of a wave's 64-byte pieces of a K row lie with one lane: x[c][e] is dimension 32 c + 8 kq + e.
-template <bool EXACT>
-__device__ __forceinline__ void rotate_row(float (*x)[8], int32_t pos, int kq, int half, const uint64_t *turns)
+template <bool HALF>
+__device__ __forceinline__ void rotate_row(float (*x)[8], int32_t pos, int kq, const uint64_t *turns)
 {
-    if (half) {
 #pragma unroll
-        for (int c = 0; c < 2; ++c)
+    for (int c = 0; c < (HALF ? 2 : 4); ++c)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const uint64_t w = turns[32 * c + 8 * kq + e];
-                float cs, sn;
-                const uint32_t phase = phase_of(pos, (uint32_t)w, (uint32_t)(w >> 32));
-                if (EXACT) turn_exact(phase, &cs, &sn);
-                else turn_fast(phase, &cs, &sn);
-                const float re = x[c][e], im = x[c + 2][e];
-                x[c][e] = fmaf(re, cs, -(im * sn));
-                x[c + 2][e] = fmaf(re, sn, im * cs);
-            }
-    } else {
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const uint64_t w = turns[16 * c + 4 * kq + e];
-                float cs, sn;
-                const uint32_t phase = phase_of(pos, (uint32_t)w, (uint32_t)(w >> 32));
-                if (EXACT) turn_exact(phase, &cs, &sn);
-                else turn_fast(phase, &cs, &sn);
-                const float re = x[c][2 * e], im = x[c][2 * e + 1];
-                x[c][2 * e] = fmaf(re, cs, -(im * sn));
-                x[c][2 * e + 1] = fmaf(re, sn, im * cs);
-            }
-    }
+        for (int e = 0; e < (HALF ? 8 : 4); ++e) {
+            const uint64_t w = turns[HALF ? 32 * c + 8 * kq + e : 16 * c + 4 * kq + e];
+            float cs, sn;
+            turn_fast(phase_of(pos, (uint32_t)w, (uint32_t)(w >> 32)), &cs, &sn);
+            float &r = HALF ? x[c][e] : x[c][2 * e], &i = HALF ? x[(c + 2) & 3][e] : x[c][(2 * e + 1) & 7];
+            const float re = r, im = i;
+            r = fmaf(re, cs, -(im * sn));
+            i = fmaf(re, sn, im * cs);
+        }
 }
 
 // NT column tiles of sixteen rows against 32 keys at a time.  S^T[key][row] = K Q^T and O^T[dim][row] = V^T P^T run on v_mfma_f32_16x16x32_bf16; a lane (m = lane & 15,
@@ -53,7 +36,7 @@ __device__ __forceinline__ void rotate_row(float (*x)[8], int32_t pos, int kq, i
 // LO: columns 8 to 15 of a tile hold what the rounding to bf16 takes off the rows 0 to 7 (of q turned by its position, and of the weights): the matrix
 // instructions have that room where rows are at most eight to a tile, and both products are as good as in 16 bits of fraction.  Keys turned on the way (TURN)
 // are multiplied as two bf16 numbers for the same reason.  Without LO, q and the weights are rounded to bf16 once.
-template <int NT, bool LO, bool PAGED, bool TURN>
+template <int NT, bool LO, bool PAGED, bool TURN, bool HALF>
 __global__ __launch_bounds__(kRowsThreads, 2) void attend_rows_kernel(AttendArgs a)
 {
     constexpr int kCols = LO ? 8 : 16, kRows = kCols * NT;
@@ -91,7 +74,10 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attend_rows_kernel(AttendArgs
         float x[4][8];
 #pragma unroll
         for (int j = 0; j < 4; ++j) widen8(*reinterpret_cast<const uint4 *>(p + 64 * j + 16 * kq), x[j]);
-        if (a.rotate_q) rotate_row<true>(x, a.pos[t], kq, a.half, turns);
+        if (a.rotate_q) {
+            if (TURN ? HALF : (bool)a.half) rotate_row<true>(x, a.pos[t], kq, turns);
+            else rotate_row<false>(x, a.pos[t], kq, turns);
+        }
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -129,7 +115,7 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attend_rows_kernel(AttendArgs
     };
     auto find = [&](int k0, int block) {
         Rows r;
-        const int left = min(max(k_hi - k0, 0), 16);
+        const int left = __builtin_amdgcn_readfirstlane(min(max(k_hi - k0, 0), 16));
         if (PAGED) {
             const int in = k0 & ((1 << c.block_shift) - 1);
             r.n = block < 0 || (a.src.n_blocks > 0 && block >= a.src.n_blocks) ? 0 : left;
@@ -174,6 +160,7 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attend_rows_kernel(AttendArgs
     Rows here[2] = {find(k0, block_at(k0)), find(k0 + 16, block_at(k0 + 16))};
     int ahead[2] = {block_at(k0 + kStep), block_at(k0 + kStep + 16)};
     load_k(here);
+    __builtin_amdgcn_sched_barrier(0);   // (in this order, as in the loop: waiting for K's loads must not wait for V's)
     load_v(here);
     for (; k0 < k_hi; k0 += kStep) {
         const Rows next[2] = {find(k0 + kStep, ahead[0]), find(k0 + kStep + 16, ahead[1])};
@@ -188,7 +175,7 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attend_rows_kernel(AttendArgs
                 float x[4][8];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) widen8(k[i][j], x[j]);
-                rotate_row<false>(x, k_pos[i], kq, a.half, turns);
+                rotate_row<HALF>(x, k_pos[i], kq, turns);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     bf16x8 hi, lo;
@@ -362,11 +349,11 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attend_rows_kernel(AttendArgs
 template <int NT, bool LO>
 void launch_rows_of(const AttendArgs &a, uint32_t blocks, hipStream_t st)
 {
-    const bool paged = a.src.cache.block_shift >= 0, turn = !a.src.cache.k_rotated;
-    if (paged && turn) attend_rows_kernel<NT, LO, true, true><<<blocks, kRowsThreads, 0, st>>>(a);
-    else if (paged) attend_rows_kernel<NT, LO, true, false><<<blocks, kRowsThreads, 0, st>>>(a);
-    else if (turn) attend_rows_kernel<NT, LO, false, true><<<blocks, kRowsThreads, 0, st>>>(a);
-    else attend_rows_kernel<NT, LO, false, false><<<blocks, kRowsThreads, 0, st>>>(a);
+    const bool paged = a.src.cache.block_shift >= 0;
+    const auto launch = [&](auto kernel) { kernel<<<blocks, kRowsThreads, 0, st>>>(a); };
+    if (a.src.cache.k_rotated) launch(paged ? attend_rows_kernel<NT, LO, true, false, false> : attend_rows_kernel<NT, LO, false, false, false>);
+    else if (a.half) launch(paged ? attend_rows_kernel<NT, LO, true, true, true> : attend_rows_kernel<NT, LO, false, true, true>);
+    else launch(paged ? attend_rows_kernel<NT, LO, true, true, false> : attend_rows_kernel<NT, LO, false, true, false>);
 }
 
 }  // namespace
