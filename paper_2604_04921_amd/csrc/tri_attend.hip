@@ -10,10 +10,7 @@ namespace {
 
 constexpr int kRowTile = 16;        // rows (token, query head of the group) of a workgroup of the general kernel
 constexpr int kAttendThreads = 256;
-#ifndef WANTED
-#define WANTED 3072
-#endif
-constexpr int64_t kWantedGroups = WANTED;
+constexpr int64_t kPartKeys = 2800;
 
 template <typename T>
 __device__ __forceinline__ void load4(const char *p, float *x);
@@ -89,6 +86,10 @@ __global__ __launch_bounds__(kAttendThreads) void attend_general_kernel(AttendAr
     __syncthreads();
     const KeyRange range = keys_of_split(a, s, h, split);
     const int k_lo = range.lo, k_hi = range.hi;
+    if (k_lo >= k_hi && a.part_o) {
+        no_keys(a, split, tr.t0, r0, min(rows - r0, kRowTile), h, Hq);
+        return;
+    }
 
     // this lane's row: column m of S^T and O^T
     const int r = min(r0 + m, rows - 1), t = tr.t0 + r / G, hq = h * G + r % G;
@@ -237,19 +238,33 @@ __global__ __launch_bounds__(kAttendThreads) void attend_general_kernel(AttendAr
     finish_row<T>(a, split, tr.t0 + (r0 + row) / G, h * G + (r0 + row) % G, Hq, d0, best, total, x);
 }
 
-// Joins the parts of a row: sixteen threads a row, 8 dimensions each.
-template <typename T>
+// Joins the parts of a row: sixteen threads have 8 dimensions each, and SPREAD such groups of a workgroup's sixteen share a row's parts.  Sixteen where parts are many (their
+// sums are then added in LDS): one group alone walks 256 parts of a long cache one memory latency after the other.
+template <typename T, int SPREAD>
 __global__ __launch_bounds__(kAttendThreads) void join_kernel(const float *part_o, const float2 *part_ml, char *out, int64_t out_stride_token,
                                                               int64_t out_stride_head, int32_t n_q_heads, int64_t n_rows, int32_t parts, float scale_log2)
 {
-    const int64_t row = (int64_t)blockIdx.x * (kAttendThreads / 16) + (threadIdx.x >> 4);
-    const int d0 = 8 * (threadIdx.x & 15);
-    if (row >= n_rows) return;
+    __shared__ float most[SPREAD > 1 ? kAttendThreads / 64 : 1], totals[SPREAD > 1 ? SPREAD : 1];
+    __shared__ __align__(16) float sums[SPREAD > 1 ? SPREAD : 1][kHeadDim];
+    const int tid = threadIdx.x, group = tid >> 4, d0 = 8 * (tid & 15), first = SPREAD > 1 ? group : 0;
+    const int64_t row = SPREAD > 1 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * (kAttendThreads / 16) + group;
+    if (row >= n_rows) return;   // (SPREAD: never)
     float best = kNoScore;
-    for (int p = 0; p < parts; ++p) best = fmaxf(best, part_ml[p * n_rows + row].x);
+    if (SPREAD > 1) {
+        for (int p = tid; p < parts; p += kAttendThreads) best = fmaxf(best, part_ml[p * n_rows + row].x);
+#pragma unroll
+        for (int x = 1; x < 64; x *= 2) best = fmaxf(best, __shfl_xor(best, x));
+        if ((tid & 63) == 0) most[tid >> 6] = best;
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < kAttendThreads / 64; ++j) best = fmaxf(best, most[j]);
+    } else {
+        for (int p = 0; p < parts; ++p) best = fmaxf(best, part_ml[p * n_rows + row].x);
+    }
     float total = 0.f, x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     const float ref = best == kNoScore ? 0.f : best;
-    for (int p = 0; p < parts; ++p) {
+#pragma unroll 4
+    for (int p = first; p < parts; p += SPREAD) {
         const float2 ml = part_ml[p * n_rows + row];
         if (ml.y != 0.f) {   // (a part without a key has nothing to bring)
             const float f = __builtin_amdgcn_exp2f((ml.x - ref) * scale_log2);
@@ -258,6 +273,21 @@ __global__ __launch_bounds__(kAttendThreads) void join_kernel(const float *part_
             const f32x4 lo = po[0], hi = po[1];
 #pragma unroll
             for (int e = 0; e < 4; ++e) x[e] += f * lo[e], x[4 + e] += f * hi[e];
+        }
+    }
+    if (SPREAD > 1) {
+        store8(&sums[group][d0], x);
+        if (d0 == 0) totals[group] = total;
+        __syncthreads();
+        if (group > 0) return;
+        total = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = 0.f;
+#pragma unroll
+        for (int j = 0; j < SPREAD; ++j) {
+            total += totals[j];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] += sums[j][d0 + e];
         }
     }
     const float inv = 1.f / total;
@@ -275,14 +305,19 @@ static bool rows_kernel(const tri_cache &c, int64_t rows)
     return c.dtype == TRI_BF16 && (c.block_size == 0 || c.block_size >= 16) && c.stride_slot < (1 << 24) && rows <= 32;
 }
 
-int32_t attend_splits(const tri_model &m, const tri_cache &c, int32_t max_tokens, int32_t n_tokens)
+// Parts.  A workgroup of the rows kernel runs two to a CU, so 512 of them fill the GPU, and more even out ragged batches; each costs about what 200 keys do, and the joining of its
+// results (us by parts per head, 8 KV heads, G = 4: 16 x 65536 keys 1023 / 630 / 642 / 637 / 661 / 850 at 1, 2, 8, 16, 48, 128 parts; 16 sequences between 1000 and 65536 keys 938 / 526 /
+// 438 / 399 / 418 / 523; 16 x 4096 69 / 49 / 61 / 71 at 1, 2, 8, 16; 64 x 2176 90 / 98 / 143 at 1, 2, 8; one of 131072 at G = 8 201 / 114 / 96 / 107 at 16, 32, 64, 128).  So: 512 workgroups, or parts of 2800 keys where that
+// makes more; none below the keys that `least` gives, which the device goes by where the lengths turn out shorter than max_seq_len.
+void attend_split(const tri_model &m, const tri_cache &c, int32_t max_tokens, int32_t *n_split, int32_t *least_keys)
 {
-    (void)n_tokens;
     const int64_t rows = (int64_t)max_tokens * (m.n_q_heads / m.n_kv_heads);
     const int64_t tiles = rows_kernel(c, rows) ? 1 : (rows + kRowTile - 1) / kRowTile;
     const int64_t units = std::max<int64_t>((int64_t)c.n_seqs * m.n_kv_heads * tiles, 1);
-    const int64_t most = std::max<int64_t>(((int64_t)c.max_seq_len + 255) / 256, 1);
-    return (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(most, 256), (kWantedGroups + units - 1) / units));
+    const int64_t least = std::min<int64_t>(kPartKeys, std::max<int64_t>(128, kPartKeys * units / 256));
+    const int64_t want = std::max<int64_t>(512 / units, c.max_seq_len / kPartKeys);
+    *least_keys = (int32_t)least;
+    *n_split = (int32_t)std::max<int64_t>(1, std::min<int64_t>({want, (c.max_seq_len + least - 1) / least, 256}));
 }
 
 tri_status launch_attend(AttendArgs a, const tri_cache &c, hipStream_t st)
@@ -299,11 +334,13 @@ tri_status launch_attend(AttendArgs a, const tri_cache &c, hipStream_t st)
 tri_status launch_join(const AttendArgs &a, int32_t parts, int32_t n_q_heads, int32_t dtype, hipStream_t st)
 {
     const int64_t rows = (int64_t)a.n_tokens * n_q_heads;
-    const uint32_t blocks = (uint32_t)((rows + kAttendThreads / 16 - 1) / (kAttendThreads / 16));
-    if (dtype == TRI_BF16)
-        join_kernel<__bf16><<<blocks, kAttendThreads, 0, st>>>(a.part_o, a.part_ml, a.out, a.out_stride_token, a.out_stride_head, n_q_heads, rows, parts, a.scale_log2);
-    else
-        join_kernel<float><<<blocks, kAttendThreads, 0, st>>>(a.part_o, a.part_ml, a.out, a.out_stride_token, a.out_stride_head, n_q_heads, rows, parts, a.scale_log2);
+    const bool spread = parts > 8;
+    const uint32_t blocks = (uint32_t)(spread ? rows : (rows + kAttendThreads / 16 - 1) / (kAttendThreads / 16));
+    const auto launch = [&](auto kernel) {
+        kernel<<<blocks, kAttendThreads, 0, st>>>(a.part_o, a.part_ml, a.out, a.out_stride_token, a.out_stride_head, n_q_heads, rows, parts, a.scale_log2);
+    };
+    if (dtype == TRI_BF16) launch(spread ? join_kernel<__bf16, 16> : join_kernel<__bf16, 1>);
+    else launch(spread ? join_kernel<float, 16> : join_kernel<float, 1>);
     return hip_status("join_kernel");
 }
 

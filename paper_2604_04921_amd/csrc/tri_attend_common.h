@@ -32,16 +32,26 @@ __device__ __forceinline__ void widen8(const uint4 &u, float *x)
     for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(w[i] << 16), x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
 }
 
-// The keys of a part: split's share of the sequence's keys, in whole groups of 128 (pages of sixteen and more are not cut by a tile of 32 or 16).
+// The keys of a part: split's share of the sequence's keys, at least src.least_keys where there are so many, in whole groups of 128 (pages of sixteen and more are not cut by a
+// tile of 32 or 16).
 struct KeyRange {
     int lo, hi;
 };
 __device__ __forceinline__ KeyRange keys_of_split(const AttendArgs &a, int s, int h, int split)
 {
     const int n = keys_of(a, s, h);
-    const int64_t per = (((int64_t)n + a.src.n_split - 1) / a.src.n_split + 127) & ~(int64_t)127;
+    const int64_t share = max(((int64_t)n + a.src.n_split - 1) / a.src.n_split, (int64_t)a.src.least_keys), per = (share + 127) & ~(int64_t)127;
     const int lo = (int)min(split * per, (int64_t)n);
     return KeyRange{lo, (int)min(lo + per, (int64_t)n)};
+}
+
+// A part without a key says so; its sums are not read.
+__device__ __forceinline__ void no_keys(const AttendArgs &a, int split, int t0, int r0, int rows, int h, int Hq)
+{
+    for (int i = threadIdx.x; i < rows; i += blockDim.x) {
+        const int r = r0 + i;
+        a.part_ml[((int64_t)(a.src.part0 + split) * a.n_tokens + t0 + r / a.group_size) * Hq + h * a.group_size + r % a.group_size] = make_float2(kNoScore, 0.f);
+    }
 }
 
 // lane ^ 8 of each sixteen

@@ -58,6 +58,10 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attend_rows_kernel(AttendArgs
     if (tid < kBands) turns[tid] = a.turns.w[tid];
     __syncthreads();
     const KeyRange range = keys_of_split(a, s, h, split);
+    if (range.lo >= range.hi && a.part_o) {
+        no_keys(a, split, tr.t0, r0, min(rows - r0, kRows), h, Hq);
+        return;
+    }
     const int k_hi = __builtin_amdgcn_readfirstlane(range.hi);   // (what buffer descriptors are made of stays in scalar registers)
 
     // this lane's rows: columns m of the column tiles

@@ -79,6 +79,7 @@ struct AttendSource {
     int32_t all;               // one prefix for all the step's sequences (group is NULL then)
     int32_t max_tokens;        // tokens that attend to one sequence of this cache, at most
     int32_t n_split, part0;    // its keys are cut into n_split ranges; the results are entries part0 and on of the partial results
+    int32_t least_keys;        // of a range that is not the last
 };
 struct AttendArgs {
     AttendSource src;
@@ -112,8 +113,8 @@ __device__ __forceinline__ int keys_of(const AttendArgs &a, int s, int h)
     return clamp_len(n, c.max_seq_len);
 }
 
-// How the keys of a source are cut: the parts it gets (a function of bounds alone, for the workspace's size).
-int32_t attend_splits(const tri_model &m, const tri_cache &c, int32_t max_tokens, int32_t n_tokens);
+// How the keys of a cache are cut: ranges per head, and their least keys (a function of bounds alone, for the workspace's size).
+void attend_split(const tri_model &m, const tri_cache &c, int32_t max_tokens, int32_t *n_split, int32_t *least_keys);
 tri_status launch_attend(AttendArgs a, const tri_cache &c, hipStream_t st);   // (c: a.src's)
 tri_status launch_join(const AttendArgs &a, int32_t parts, int32_t n_q_heads, int32_t dtype, hipStream_t st);
 

@@ -67,7 +67,7 @@ tri_status check_rows(const void *p, int64_t stride_token, int64_t stride_head, 
 int32_t most_tokens(const tri_tokens &t) { return t.start ? std::max(t.max_tokens, 1) : 1; }
 
 struct AttendPlan {
-    int32_t own_split, prefix_split, parts;   // parts 0: no partial results
+    int32_t own_split, own_least, prefix_split, prefix_least, parts;   // parts 0: no partial results
     size_t o_bytes, ml_bytes, total;
 };
 
@@ -76,8 +76,8 @@ size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 AttendPlan attend_plan(const tri_model &m, const tri_cache *prefix, const tri_cache &c, const tri_tokens &t)
 {
     AttendPlan p{};
-    p.own_split = attend_splits(m, c, most_tokens(t), t.n_tokens);
-    if (prefix) p.prefix_split = attend_splits(m, *prefix, std::max(t.n_tokens, 1), t.n_tokens);
+    attend_split(m, c, most_tokens(t), &p.own_split, &p.own_least);
+    if (prefix) attend_split(m, *prefix, std::max(t.n_tokens, 1), &p.prefix_split, &p.prefix_least);
     p.parts = p.own_split + p.prefix_split;
     if (p.parts == 1) p.parts = 0;
     const size_t rows = (size_t)t.n_tokens * m.n_q_heads;
@@ -164,10 +164,11 @@ tri_status attend(const tri_model *model, const tri_cache *prefix, const int32_t
     a.rotate_q = !tokens->rotated;
     a.half = model->pairs == TRI_PAIR_HALF;
     if (prefix) {
-        a.src = AttendSource{make_view(*model, *prefix), group, nullptr, prefix->n_blocks, group ? 0 : 1, tokens->n_tokens, plan.prefix_split, plan.own_split};
+        a.src = AttendSource{make_view(*model, *prefix), group, nullptr, prefix->n_blocks, group ? 0 : 1, tokens->n_tokens, plan.prefix_split, plan.own_split,
+                             plan.prefix_least};
         if ((rc = launch_attend(a, *prefix, st)) != TRI_OK) return rc;
     }
-    a.src = AttendSource{make_view(*model, *cache), nullptr, tokens->head_len, cache->n_blocks, 0, most_tokens(*tokens), plan.own_split, 0};
+    a.src = AttendSource{make_view(*model, *cache), nullptr, tokens->head_len, cache->n_blocks, 0, most_tokens(*tokens), plan.own_split, 0, plan.own_least};
     if ((rc = launch_attend(a, *cache, st)) != TRI_OK) return rc;
     return plan.parts ? launch_join(a, plan.parts, model->n_q_heads, cache->dtype, st) : TRI_OK;
 }
