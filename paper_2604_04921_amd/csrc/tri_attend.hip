@@ -299,10 +299,12 @@ __global__ __launch_bounds__(kAttendThreads) void join_kernel(const float *part_
 
 }  // namespace
 
-// Which kernel takes a call: the bf16 ones need pages of sixteen slots, and 32 rows' addresses within 32 bits.
-static bool rows_kernel(const tri_cache &c, int64_t rows)
+// Which kernel takes a call: the bf16 ones need pages of sixteen slots, and sixteen rows' addresses within 32 bits.
+enum class Kernel { general, rows, tile };
+static Kernel kernel_of(const tri_cache &c, int64_t rows)
 {
-    return c.dtype == TRI_BF16 && (c.block_size == 0 || c.block_size >= 16) && c.stride_slot < (1 << 24) && rows <= 32;
+    if (c.dtype != TRI_BF16 || (c.block_size > 0 && c.block_size < 16) || c.stride_slot >= (1 << 24)) return Kernel::general;
+    return rows <= 32 ? Kernel::rows : Kernel::tile;
 }
 
 // Parts.  A workgroup of the rows kernel runs two to a CU, so 512 of them fill the GPU, and more even out ragged batches; each costs about what 200 keys do, and the joining of its
@@ -312,7 +314,8 @@ static bool rows_kernel(const tri_cache &c, int64_t rows)
 void attend_split(const tri_model &m, const tri_cache &c, int32_t max_tokens, int32_t *n_split, int32_t *least_keys)
 {
     const int64_t rows = (int64_t)max_tokens * (m.n_q_heads / m.n_kv_heads);
-    const int64_t tiles = rows_kernel(c, rows) ? 1 : (rows + kRowTile - 1) / kRowTile;
+    const Kernel kernel = kernel_of(c, rows);
+    const int64_t per_tile = kernel == Kernel::general ? kRowTile : kernel == Kernel::rows ? 32 : kTileRows, tiles = (rows + per_tile - 1) / per_tile;
     const int64_t units = std::max<int64_t>((int64_t)c.n_seqs * m.n_kv_heads * tiles, 1);
     const int64_t least = std::min<int64_t>(kPartKeys, std::max<int64_t>(128, kPartKeys * units / 256));
     const int64_t want = std::max<int64_t>(512 / units, c.max_seq_len / kPartKeys);
@@ -323,7 +326,9 @@ void attend_split(const tri_model &m, const tri_cache &c, int32_t max_tokens, in
 tri_status launch_attend(AttendArgs a, const tri_cache &c, hipStream_t st)
 {
     const int64_t rows = (int64_t)a.src.max_tokens * a.group_size;
-    if (rows_kernel(c, rows)) return launch_attend_rows(a, (int32_t)rows, st);
+    const Kernel kernel = kernel_of(c, rows);
+    if (kernel == Kernel::rows) return launch_attend_rows(a, (int32_t)rows, st);
+    if (kernel == Kernel::tile) return launch_attend_tile(a, (int32_t)rows, st);
     a.row_tiles = (int32_t)((rows + kRowTile - 1) / kRowTile);
     const int64_t blocks = (int64_t)a.row_tiles * a.src.n_split * a.src.cache.n_kv_heads * a.src.cache.n_seqs;
     if (c.dtype == TRI_BF16) attend_general_kernel<__bf16><<<(uint32_t)blocks, kAttendThreads, 0, st>>>(a);

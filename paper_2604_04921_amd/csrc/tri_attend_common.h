@@ -123,6 +123,8 @@ __device__ __forceinline__ void finish_row(const AttendArgs &a, int split, int t
     store8(reinterpret_cast<T *>(a.out) + (int64_t)t * a.out_stride_token + (int64_t)hq * a.out_stride_head + d0, x);
 }
 
+constexpr int kTileRows = 128;   // rows of a workgroup of the tile kernel
+tri_status launch_attend_tile(AttendArgs a, int32_t rows, hipStream_t st);
 tri_status launch_attend_rows(AttendArgs a, int32_t rows, hipStream_t st);
 
 }  // namespace tri

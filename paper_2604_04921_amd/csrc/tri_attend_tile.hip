@@ -1,0 +1,385 @@
+// Attention with many rows per KV head (chunks of prompts, batches behind a shared prefix): bf16, contiguous caches or pages of at least sixteen slots.
+#include "tri_attend_common.h"
+
+namespace tri {
+
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+typedef __attribute__((address_space(3))) void lds_void;
+
+constexpr int kTileThreads = 256;
+constexpr int kTileKeys = 64;
+constexpr float kStaleBits = 8.f;   // powers of two by which a score may pass the maximum that weights are relative to
+
+// Rotates a lane's 64 elements of a row: x[c][e] is dimension 16 c + 8 h + e.
+template <bool HALF>
+__device__ __forceinline__ void rotate_q(float (*x)[8], int32_t pos, int h, const uint64_t *turns)
+{
+#pragma unroll
+    for (int c = 0; c < (HALF ? 4 : 8); ++c)
+#pragma unroll
+        for (int e = 0; e < (HALF ? 8 : 4); ++e) {
+            const uint64_t w = turns[HALF ? 16 * c + 8 * h + e : 8 * c + 4 * h + e];
+            float cs, sn;
+            turn_fast(phase_of(pos, (uint32_t)w, (uint32_t)(w >> 32)), &cs, &sn);
+            float &r = HALF ? x[c][e] : x[c][2 * e], &i = HALF ? x[(c + 4) & 7][e] : x[c][(2 * e + 1) & 7];
+            const float re = r, im = i;
+            r = fmaf(re, cs, -(im * sn));
+            i = fmaf(re, sn, im * cs);
+        }
+}
+
+// The same value, as the compiler cannot tell.
+__device__ __forceinline__ void fresh(uint32_t &x) { asm volatile("" : "+v"(x)); }
+
+struct TileBuffer {
+    __bf16 k[kTileKeys * kHeadDim], v[kTileKeys * kHeadDim];
+    int32_t pos[kTileKeys], n[4];   // keys of the four sixteens
+};
+
+template <int RT, bool PAGED, bool TURN, bool HALF>
+__global__ __launch_bounds__(kTileThreads, RT == 1 ? 2 : 1) void attend_tile_kernel(AttendArgs a)
+{
+    constexpr int kWaveRows = 32 * RT, kRows = 4 * kWaveRows;
+    __shared__ __align__(16) uint64_t turns[kBands];
+    // (two objects and two copies of the loop's body: the compiler then knows that reading one does not have to wait for the loads into the other)
+    __shared__ __align__(16) TileBuffer buf0, buf1;
+    const CacheView &c = a.src.cache;
+    const int H = c.n_kv_heads, G = a.group_size, Hq = H * G;
+    // Row tiles of the same keys run next to each other on one XCD (workgroups go to the eight in turn), where the keys stay in its L2.
+    const uint32_t x = blockIdx.x & 7, y = blockIdx.x >> 3;
+    const int rt0 = y % a.row_tiles;
+    uint32_t w = (y / a.row_tiles) * 8 + x;
+    const int split = w % a.src.n_split;
+    w /= a.src.n_split;
+    const int head = w % H, s = w / H;
+    if (s >= c.n_seqs) return;
+    const TokenRange tr = tokens_of(a, s);
+    const int rows = tr.n * G, r0 = rt0 * kRows;
+    if (r0 >= rows) return;
+    const KeyRange range = keys_of_split(a, s, head, split);
+    if (range.lo >= range.hi && a.part_o) {
+        no_keys(a, split, tr.t0, r0, min(rows - r0, kRows), head, Hq);
+        return;
+    }
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, h = lane >> 5;
+    const int k_lo = __builtin_amdgcn_readfirstlane(range.lo), k_hi = __builtin_amdgcn_readfirstlane(range.hi);
+    if (tid < kBands) turns[tid] = a.turns.w[tid];
+    __syncthreads();
+
+    bf16x8 q[RT][8];
+    int32_t t_pos[RT], first_pos = 0x7fffffff, last_pos = -0x7fffffff - 1;
+    bool real[RT];
+#pragma unroll
+    for (int n = 0; n < RT; ++n) {
+        const int at = r0 + wave * kWaveRows + 32 * n + col, r = min(at, rows - 1), t = tr.t0 + r / G, hq = head * G + r % G;
+        real[n] = at < rows;
+        t_pos[n] = a.causal ? a.pos[t] : 0x7fffffff;
+        first_pos = min(first_pos, t_pos[n]);
+        last_pos = max(last_pos, real[n] ? t_pos[n] : last_pos);
+        const char *p = a.q + ((int64_t)t * a.q_stride_token + (int64_t)hq * a.q_stride_head) * 2 + 16 * h;
+        if (a.rotate_q) {
+            float v[8][8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) widen8(*reinterpret_cast<const uint4 *>(p + 32 * j), v[j]);
+            if (TURN ? HALF : (bool)a.half) rotate_q<true>(v, a.pos[t], h, turns);
+            else rotate_q<false>(v, a.pos[t], h, turns);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) q[n][j][e] = (__bf16)v[j][e];
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) q[n][j] = *reinterpret_cast<const bf16x8 *>(p + 32 * j);
+        }
+    }
+#pragma unroll
+    for (int i = 1; i < 32; i *= 2) first_pos = min(first_pos, __shfl_xor(first_pos, i)), last_pos = max(last_pos, __shfl_xor(last_pos, i));
+    first_pos = __builtin_amdgcn_readfirstlane(first_pos);
+    last_pos = __builtin_amdgcn_readfirstlane(last_pos);
+    const bool idle = r0 + wave * kWaveRows >= rows;
+
+    // Loading: wave w brings keys 16 w to 16 w + 15 of a tile.
+    const int64_t base = (int64_t)a.layer * c.stride_layer + (int64_t)head * c.stride_head;
+    const int64_t pbase = (int64_t)a.layer * c.pos_stride_layer + (int64_t)head * c.pos_stride_head;
+    const uint32_t sb = (uint32_t)c.stride_slot * 2u;
+    // Lane offsets, as the part that the others follow from by exclusive or: the compiler would keep all of them in registers that it does not have (fresh() hides that
+    // they stay the same from tile to tile).  Pieces of 16 bytes lie in LDS at their number exclusive-or the row (K) or twice the row (V), so that eight lanes of a 16-byte
+    // read of neighbouring rows, and sixteen of a transposing 8-byte read of four rows, meet different banks.
+    const uint32_t row4 = lane >> 4;
+    const uint32_t piece_k = TURN ? (lane & 3) * 16 : ((lane & 15) ^ row4) * 16, piece_v = ((lane & 15) ^ (2 * row4)) * 16, from_row = (TURN ? lane >> 2 : row4) * sb;
+    auto block_at = [&](int k0) {
+        return PAGED ? __builtin_amdgcn_readfirstlane(c.block_table[(int64_t)s * c.max_blocks + (min(k0, k_hi - 1) >> c.block_shift)]) : 0;
+    };
+    uint4 k_new[4];
+    int32_t pos_new = 0, turn_pos = 0, n_new = 0;
+    auto load = [&](TileBuffer &to, int k0, int block) __attribute__((always_inline)) {   // k0: this wave's first key
+        int n = __builtin_amdgcn_readfirstlane(min(max(k_hi - k0, 0), 16));
+        int64_t kv, at;
+        if (PAGED) {
+            const int in = k0 & ((1 << c.block_shift) - 1);
+            if (block < 0 || (a.src.n_blocks > 0 && block >= a.src.n_blocks)) n = 0;
+            const int b = n ? block : 0;
+            kv = base + (int64_t)b * c.stride_sb + (int64_t)in * c.stride_slot;
+            at = pbase + (int64_t)b * c.pos_stride_sb + in;
+        } else {
+            kv = base + (int64_t)s * c.stride_sb + (int64_t)k0 * c.stride_slot;
+            at = pbase + (int64_t)s * c.pos_stride_sb + k0;
+        }
+        n_new = n;
+        const uint32_t bytes = n > 0 ? (n - 1) * sb + kHeadDim * 2 : 0;   // (lanes beyond it bring zeros)
+        const auto kr = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>((const char *)c.k) + kv * 2, 0, bytes, 0x00027000);
+        const auto vr = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>((const char *)c.v) + kv * 2, 0, bytes, 0x00027000);
+        uint32_t row = from_row, pk = piece_k, pv = piece_v;
+        fresh(row), fresh(pk), fresh(pv);
+        const uint32_t row_v = TURN ? row4 * sb : row;
+        const auto pr = __builtin_amdgcn_make_buffer_rsrc(const_cast<int32_t *>(c.pos) + at, 0, a.causal || TURN ? n * 4 : 0, 0x00027000);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (TURN) k_new[i] = as_uint4(__builtin_amdgcn_raw_buffer_load_b128(kr, row + pk + 64 * i, 0, 0));
+            else __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, (lds_void *)(to.k + (16 * wave + 4 * i) * kHeadDim), 16, row + 4 * i * sb + (pk ^ (64 * i)), 0, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, (lds_void *)(to.v + (16 * wave + 4 * i) * kHeadDim), 16, row_v + 4 * i * sb + (pv ^ (128 * (i & 1))), 0, 0, 0);
+        pos_new = __builtin_amdgcn_raw_buffer_load_b32(pr, (lane & 15) * 4, 0, 0);
+        if (TURN) turn_pos = __builtin_amdgcn_raw_buffer_load_b32(pr, (lane >> 2) * 4, 0, 0);
+    };
+    auto put = [&](TileBuffer &to) __attribute__((always_inline)) {   // what passes through registers
+        if (TURN) {
+            float v[4][8];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) widen8(k_new[i], v[i]);
+#pragma unroll
+            for (int i = 0; i < (HALF ? 2 : 4); ++i)
+#pragma unroll
+                for (int e = 0; e < (HALF ? 8 : 4); ++e) {
+                    const int piece = (lane & 3) + 4 * i;
+                    const uint64_t t = turns[HALF ? 8 * piece + e : 4 * piece + e];
+                    float cs, sn;
+                    turn_fast(phase_of(turn_pos, (uint32_t)t, (uint32_t)(t >> 32)), &cs, &sn);
+                    float &r = HALF ? v[i][e] : v[i][2 * e], &im = HALF ? v[(i + 2) & 3][e] : v[i][(2 * e + 1) & 7];
+                    const float re = r, im0 = im;
+                    r = fmaf(re, cs, -(im0 * sn));
+                    im = fmaf(re, sn, im0 * cs);
+                }
+            const int row = lane >> 2;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                bf16x8 u;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) u[e] = (__bf16)v[i][e];
+                *reinterpret_cast<bf16x8 *>(to.k + (16 * wave + row) * kHeadDim + 8 * (((lane & 3) + 4 * i) ^ row)) = u;
+            }
+        }
+        if (lane < 16) to.pos[16 * wave + lane] = pos_new;
+        if (lane == 0) to.n[wave] = n_new;
+    };
+
+    f32x16 o[RT][4];
+    float top[RT], sum[RT];
+#pragma unroll
+    for (int n = 0; n < RT; ++n) {
+        top[n] = kNoScore;
+        sum[n] = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[n][j][i] = 0.f;
+    }
+    // the lane's operands in a tile: dimension group j of its K row at at_k ^ 32 j; of the V rows of a step, dimensions 32 j + col at at_v ^ 64 j
+    const uint32_t row_v0 = 4 * h + ((lane & 15) >> 2);
+    const uint32_t at_k = col * 256 + (h ^ (col & 15)) * 16;
+    const uint32_t at_v = row_v0 * 256 + (((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ (2 * row_v0)) * 16) + (lane & 1) * 8;
+
+    // 32 keys: half U of a tile
+    auto compute = [&](const TileBuffer &from, const int U) __attribute__((always_inline)) {
+        const char *kt = (const char *)from.k + U * 32 * 256, *vt = (const char *)from.v + U * 32 * 256;
+        uint32_t ak = at_k, av = at_v;
+        fresh(ak), fresh(av);
+        f32x16 sc[RT];
+#pragma unroll
+        for (int n = 0; n < RT; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sc[n][i] = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const bf16x8 k = *reinterpret_cast<const bf16x8 *>(kt + (ak ^ (32 * j)));
+#pragma unroll
+            for (int n = 0; n < RT; ++n) sc[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[n][j], sc[n], 0, 0, 0);
+        }
+        uint32_t keep[RT];   // bit i: key 8 (i / 4) + 4 h + i % 4 is attended to
+        bool hole = false;
+#pragma unroll
+        for (int n = 0; n < RT; ++n) keep[n] = 0xffffu;
+        const int n_lane = from.n[2 * U + (col >> 4)];
+        if (__ballot((from.pos[32 * U + col] > first_pos) | (n_lane < 16))) {   // (not causal: no position is above first_pos)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int n_there = from.n[2 * U + g / 2] - (8 * (g & 1) + 4 * h);
+                const int4 p4 = *reinterpret_cast<const int4 *>(&from.pos[32 * U + 8 * g + 4 * h]);
+                const int32_t p[4] = {p4.x, p4.y, p4.z, p4.w};
+#pragma unroll
+                for (int d = 0; d < 4; ++d) {
+                    const int i = 4 * g + d;
+#pragma unroll
+                    for (int n = 0; n < RT; ++n) {
+                        const bool on = (d < n_there) & (p[d] <= t_pos[n]);
+                        keep[n] &= on ? ~0u : ~(1u << i);
+                        sc[n][i] = on ? sc[n][i] : kNoScore;
+                        hole |= (d < n_there) & !on & real[n];
+                    }
+                }
+            }
+        }
+        bf16x8 weight[RT][2];
+#pragma unroll
+        for (int n = 0; n < RT; ++n) {
+            float best = kNoScore;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) best = fmaxf(best, sc[n][i]);
+            const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(best), __float_as_uint(best), false, false);
+            best = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
+            // weights are relative to a maximum that scores may pass by a factor of 2^8 before the sums are brought to the new one
+            if (__ballot(best > top[n] && !((best - top[n]) * a.scale_log2 <= kStaleBits))) {
+                const float next = fmaxf(top[n], best);
+                const float shrink = next == kNoScore ? 1.f : __builtin_amdgcn_exp2f((top[n] - next) * a.scale_log2);
+                top[n] = next;
+                sum[n] *= shrink;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o[n][j] *= shrink;
+            }
+            const float off = (top[n] == kNoScore ? 0.f : top[n]) * a.scale_log2;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float p = __builtin_amdgcn_exp2f(fmaf(sc[n][i], a.scale_log2, -off));
+                sum[n] += p;
+                weight[n][i / 8][i % 8] = (__bf16)p;
+            }
+        }
+        auto values = [&](int j, int u) {   // dimensions 32 j + col, the keys of weight[.][u]
+            const char *p = vt + (av ^ (64 * j)) + u * 16 * 256;
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)p), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p + 8 * 256));
+            return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        };
+        bool odd = false;
+        if (__ballot(hole)) {   // (see attend_general_kernel: values that are not finite and not everyone's)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int u = 0; u < 2; ++u) odd |= not_finite(__builtin_bit_cast(uint4, values(j, u)));
+        }
+        if (__ballot(odd)) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int n = 0; n < RT; ++n) {
+#pragma unroll
+                    for (int side = 0; side < 2; ++side) {
+                        f32x16 some;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) some[i] = 0.f;
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) {
+                            bf16x8 on;
+#pragma unroll
+                            for (int d = 0; d < 8; ++d) on[d] = (keep[n] >> (8 * u + d)) & 1 ? (__bf16)1.f : (__bf16)0.f;
+                            some = __builtin_amdgcn_mfma_f32_32x32x16_bf16(where_not_below(values(j, u), side ? 0xff80 : 0x7f80), on, some, 0, 0, 0);
+                        }
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) o[n][j][i] += some[i] > 0.f ? (side ? -__builtin_inff() : __builtin_inff()) : 0.f;
+                        __builtin_amdgcn_sched_barrier(0);   // (one after the other: few registers, and time does not matter here)
+                    }
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
+                        o[n][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, finite_only(__builtin_bit_cast(uint4, values(j, u)))), weight[n][u], o[n][j], 0, 0, 0);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            return;
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const bf16x8 v = values(j, u);
+#pragma unroll
+                for (int n = 0; n < RT; ++n) o[n][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, weight[n][u], o[n][j], 0, 0, 0);
+            }
+    };
+
+    int k0 = k_lo, ahead = block_at(k_lo + 16 * wave);
+    if (k0 < k_hi) {
+        load(buf0, k0 + 16 * wave, ahead);
+        ahead = block_at(k0 + kTileKeys + 16 * wave);
+        put(buf0);
+    }
+    auto step = [&](TileBuffer &here, TileBuffer &next) __attribute__((always_inline)) {
+        __syncthreads();   // this tile has come, and the last one is read
+        const bool more = k0 + kTileKeys < k_hi;
+        if (more) {
+            load(next, k0 + kTileKeys + 16 * wave, ahead);
+            ahead = block_at(k0 + 2 * kTileKeys + 16 * wave);
+        }
+        // (keys behind the last position of the wave's rows have nothing for it)
+        if (!idle) {
+#pragma unroll 1
+            for (int U = 0; U < 2; ++U)
+                if (__ballot((here.pos[32 * U + col] <= last_pos) & ((col & 15) < here.n[2 * U + (col >> 4)]))) compute(here, U);
+        }
+        if (more) put(next);
+        k0 += kTileKeys;
+        return more;
+    };
+    if (k0 < k_hi)
+        while (step(buf0, buf1) && step(buf1, buf0)) {
+        }
+#pragma unroll
+    for (int n = 0; n < RT; ++n) {
+        if (!real[n]) continue;
+        const int r = r0 + wave * kWaveRows + 32 * n + col, t = tr.t0 + r / G, hq = head * G + r % G;
+        const float total = sum[n] + __shfl_xor(sum[n], 32);
+        if (a.part_o) {
+            const int64_t at = ((int64_t)(a.src.part0 + split) * a.n_tokens + t) * Hq + hq;
+            if (h == 0) a.part_ml[at] = make_float2(top[n], total);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4)
+                    *reinterpret_cast<f32x4 *>(a.part_o + at * kHeadDim + 32 * j + 2 * i + 4 * h) = f32x4{o[n][j][i], o[n][j][i + 1], o[n][j][i + 2], o[n][j][i + 3]};
+        } else {
+            const float inv = total != 0.f ? 1.f / total : 0.f;
+            __bf16 *p = reinterpret_cast<__bf16 *>(a.out) + (int64_t)t * a.out_stride_token + (int64_t)hq * a.out_stride_head;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) {
+                    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+                    bf16x4 b;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) b[e] = (__bf16)(total != 0.f ? o[n][j][i + e] * inv : 0.f);
+                    *reinterpret_cast<bf16x4 *>(p + 32 * j + 2 * i + 4 * h) = b;
+                }
+        }
+    }
+}
+
+}  // namespace
+
+tri_status launch_attend_tile(AttendArgs a, int32_t rows, hipStream_t st)
+{
+    constexpr int RT = kTileRows / 128;
+    a.row_tiles = (rows + kTileRows - 1) / kTileRows;
+    const int64_t groups = (int64_t)a.src.n_split * a.src.cache.n_kv_heads * a.src.cache.n_seqs;
+    const uint32_t blocks = (uint32_t)((groups + 7) / 8 * 8 * a.row_tiles);
+    const bool paged = a.src.cache.block_shift >= 0;
+    const auto launch = [&](auto kernel) { kernel<<<blocks, kTileThreads, 0, st>>>(a); };
+    if (a.src.cache.k_rotated) launch(paged ? attend_tile_kernel<RT, true, false, false> : attend_tile_kernel<RT, false, false, false>);
+    else if (a.half) launch(paged ? attend_tile_kernel<RT, true, true, true> : attend_tile_kernel<RT, false, true, true>);
+    else launch(paged ? attend_tile_kernel<RT, true, true, false> : attend_tile_kernel<RT, false, true, false>);
+    return hip_status("attend_tile_kernel");
+}
+
+}  // namespace tri
