@@ -311,14 +311,17 @@ static Kernel kernel_of(const tri_cache &c, int64_t rows)
 // results (us by parts per head, 8 KV heads, G = 4: 16 x 65536 keys 1023 / 630 / 642 / 637 / 661 / 850 at 1, 2, 8, 16, 48, 128 parts; 16 sequences between 1000 and 65536 keys 938 / 526 /
 // 438 / 399 / 418 / 523; 16 x 4096 69 / 49 / 61 / 71 at 1, 2, 8, 16; 64 x 2176 90 / 98 / 143 at 1, 2, 8; one of 131072 at G = 8 201 / 114 / 96 / 107 at 16, 32, 64, 128).  So: 512 workgroups, or parts of 2800 keys where that
 // makes more; none below the keys that `least` gives, which the device goes by where the lengths turn out shorter than max_seq_len.
-void attend_split(const tri_model &m, const tri_cache &c, int32_t max_tokens, int32_t *n_split, int32_t *least_keys)
+void attend_split(const tri_model &m, const tri_cache &c, int32_t max_tokens, int32_t n_tokens, int32_t *n_split, int32_t *least_keys)
 {
     const int64_t rows = (int64_t)max_tokens * (m.n_q_heads / m.n_kv_heads);
     const Kernel kernel = kernel_of(c, rows);
-    const int64_t per_tile = kernel == Kernel::general ? kRowTile : kernel == Kernel::rows ? 32 : kTileRows, tiles = (rows + per_tile - 1) / per_tile;
-    const int64_t units = std::max<int64_t>((int64_t)c.n_seqs * m.n_kv_heads * tiles, 1);
-    const int64_t least = std::min<int64_t>(kPartKeys, std::max<int64_t>(128, kPartKeys * units / 256));
-    const int64_t want = std::max<int64_t>(512 / units, c.max_seq_len / kPartKeys);
+    const int64_t per_tile = kernel == Kernel::general ? kRowTile : kernel == Kernel::rows ? 32 : kTileRows;
+    // row tiles that there are: at least one per sequence, and all tokens' rows
+    const int64_t tiles = std::max<int64_t>(c.n_seqs, ((int64_t)n_tokens * (m.n_q_heads / m.n_kv_heads) + per_tile - 1) / per_tile);
+    const int64_t units = m.n_kv_heads * (kernel == Kernel::rows ? c.n_seqs : tiles);
+    const int64_t part = kernel == Kernel::tile ? 8192 : kPartKeys;
+    const int64_t least = kernel == Kernel::tile ? 256 : std::min<int64_t>(part, std::max<int64_t>(128, part * units / 256));
+    const int64_t want = std::max<int64_t>((512 + units / 2) / units, c.max_seq_len / part);
     *least_keys = (int32_t)least;
     *n_split = (int32_t)std::max<int64_t>(1, std::min<int64_t>({want, (c.max_seq_len + least - 1) / least, 256}));
 }

@@ -37,7 +37,8 @@ __device__ __forceinline__ void fresh(uint32_t &x) { asm volatile("" : "+v"(x));
 
 struct TileBuffer {
     __bf16 k[kTileKeys * kHeadDim], v[kTileKeys * kHeadDim];
-    int32_t pos[kTileKeys], n[4];   // keys of the four sixteens
+    int32_t pos[kTileKeys];
+    int32_t lim[12];   // of the four sixteens: highest and lowest position, and how many keys there are
 };
 
 template <int RT, bool PAGED, bool TURN, bool HALF>
@@ -175,8 +176,12 @@ __global__ __launch_bounds__(kTileThreads, RT == 1 ? 2 : 1) void attend_tile_ker
                 *reinterpret_cast<bf16x8 *>(to.k + (16 * wave + row) * kHeadDim + 8 * (((lane & 3) + 4 * i) ^ row)) = u;
             }
         }
+        const bool there = (lane & 15) < n_new;   // (the four sixteens of lanes hold the same)
+        int32_t hi = there ? pos_new : -0x7fffffff - 1, lo = there ? pos_new : 0x7fffffff;
+#pragma unroll
+        for (int i = 1; i < 16; i *= 2) hi = max(hi, __shfl_xor(hi, i)), lo = min(lo, __shfl_xor(lo, i));
         if (lane < 16) to.pos[16 * wave + lane] = pos_new;
-        if (lane == 0) to.n[wave] = n_new;
+        if (lane == 0) to.lim[wave] = hi, to.lim[4 + wave] = lo, to.lim[8 + wave] = n_new;
     };
 
     f32x16 o[RT][4];
@@ -195,31 +200,42 @@ __global__ __launch_bounds__(kTileThreads, RT == 1 ? 2 : 1) void attend_tile_ker
     const uint32_t at_k = col * 256 + (h ^ (col & 15)) * 16;
     const uint32_t at_v = row_v0 * 256 + (((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ (2 * row_v0)) * 16) + (lane & 1) * 8;
 
-    // 32 keys: half U of a tile
-    auto compute = [&](const TileBuffer &from, const int U) __attribute__((always_inline)) {
-        const char *kt = (const char *)from.k + U * 32 * 256, *vt = (const char *)from.v + U * 32 * 256;
-        uint32_t ak = at_k, av = at_v;
+    // 32 keys: half U of a tile.  mask: some of them are not everyone's
+    auto compute = [&](const TileBuffer &from, const int U, const bool mask) __attribute__((always_inline)) {
+        uint32_t ak = at_k + U * 32 * 256, av = at_v + U * 32 * 256;
         fresh(ak), fresh(av);
         f32x16 sc[RT];
 #pragma unroll
         for (int n = 0; n < RT; ++n)
 #pragma unroll
             for (int i = 0; i < 16; ++i) sc[n][i] = 0.f;
+        bf16x8 k[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const bf16x8 k = *reinterpret_cast<const bf16x8 *>(kt + (ak ^ (32 * j)));
+        for (int j = 0; j < 8; ++j) k[j] = *reinterpret_cast<const bf16x8 *>((const char *)from.k + (ak ^ (32 * j)));
+        __builtin_amdgcn_sched_barrier(0);   // all reads under way before the first product waits for one
 #pragma unroll
-            for (int n = 0; n < RT; ++n) sc[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[n][j], sc[n], 0, 0, 0);
-        }
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int n = 0; n < RT; ++n) sc[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[j], q[n][j], sc[n], 0, 0, 0);
+        bf16x8 v[2][4];   // v[u][j]: dimensions 32 j + col, the keys of weight[.][u]; asked for ahead of the softmax
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t at = av ^ (64 * j);
+                const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)((const char *)from.v + at + 16 * 256 * u));
+                const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)((const char *)from.v + at + (16 * 256 * u + 8 * 256)));
+                v[u][j] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+            }
+        __builtin_amdgcn_sched_barrier(0);
         uint32_t keep[RT];   // bit i: key 8 (i / 4) + 4 h + i % 4 is attended to
         bool hole = false;
 #pragma unroll
         for (int n = 0; n < RT; ++n) keep[n] = 0xffffu;
-        const int n_lane = from.n[2 * U + (col >> 4)];
-        if (__ballot((from.pos[32 * U + col] > first_pos) | (n_lane < 16))) {   // (not causal: no position is above first_pos)
+        if (mask) {
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                const int n_there = from.n[2 * U + g / 2] - (8 * (g & 1) + 4 * h);
+                const int n_there = from.lim[8 + 2 * U + g / 2] - (8 * (g & 1) + 4 * h);
                 const int4 p4 = *reinterpret_cast<const int4 *>(&from.pos[32 * U + 8 * g + 4 * h]);
                 const int32_t p[4] = {p4.x, p4.y, p4.z, p4.w};
 #pragma unroll
@@ -227,7 +243,7 @@ __global__ __launch_bounds__(kTileThreads, RT == 1 ? 2 : 1) void attend_tile_ker
                     const int i = 4 * g + d;
 #pragma unroll
                     for (int n = 0; n < RT; ++n) {
-                        const bool on = (d < n_there) & (p[d] <= t_pos[n]);
+                        const bool on = (d < n_there) & (p[d] <= t_pos[n]);   // (not causal: t_pos is the highest there is)
                         keep[n] &= on ? ~0u : ~(1u << i);
                         sc[n][i] = on ? sc[n][i] : kNoScore;
                         hole |= (d < n_there) & !on & real[n];
@@ -260,54 +276,44 @@ __global__ __launch_bounds__(kTileThreads, RT == 1 ? 2 : 1) void attend_tile_ker
                 weight[n][i / 8][i % 8] = (__bf16)p;
             }
         }
-        auto values = [&](int j, int u) {   // dimensions 32 j + col, the keys of weight[.][u]
-            const char *p = vt + (av ^ (64 * j)) + u * 16 * 256;
-            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)p), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p + 8 * 256));
-            return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-        };
-        bool odd = false;
         if (__ballot(hole)) {   // (see attend_general_kernel: values that are not finite and not everyone's)
+            bool odd = false;
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+            for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int u = 0; u < 2; ++u) odd |= not_finite(__builtin_bit_cast(uint4, values(j, u)));
-        }
-        if (__ballot(odd)) {
+                for (int j = 0; j < 4; ++j) odd |= not_finite(__builtin_bit_cast(uint4, v[u][j]));
+            if (__ballot(odd)) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+                for (int j = 0; j < 4; ++j) {
 #pragma unroll
-                for (int n = 0; n < RT; ++n) {
+                    for (int n = 0; n < RT; ++n)
 #pragma unroll
-                    for (int side = 0; side < 2; ++side) {
-                        f32x16 some;
+                        for (int side = 0; side < 2; ++side) {
+                            f32x16 some;
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) some[i] = 0.f;
+                            for (int i = 0; i < 16; ++i) some[i] = 0.f;
 #pragma unroll
-                        for (int u = 0; u < 2; ++u) {
-                            bf16x8 on;
+                            for (int u = 0; u < 2; ++u) {
+                                bf16x8 on;
 #pragma unroll
-                            for (int d = 0; d < 8; ++d) on[d] = (keep[n] >> (8 * u + d)) & 1 ? (__bf16)1.f : (__bf16)0.f;
-                            some = __builtin_amdgcn_mfma_f32_32x32x16_bf16(where_not_below(values(j, u), side ? 0xff80 : 0x7f80), on, some, 0, 0, 0);
+                                for (int d = 0; d < 8; ++d) on[d] = (keep[n] >> (8 * u + d)) & 1 ? (__bf16)1.f : (__bf16)0.f;
+                                some = __builtin_amdgcn_mfma_f32_32x32x16_bf16(where_not_below(v[u][j], side ? 0xff80 : 0x7f80), on, some, 0, 0, 0);
+                            }
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) o[n][j][i] += some[i] > 0.f ? (side ? -__builtin_inff() : __builtin_inff()) : 0.f;
+                            __builtin_amdgcn_sched_barrier(0);   // (one after the other: few registers, and time does not matter here)
                         }
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) o[n][j][i] += some[i] > 0.f ? (side ? -__builtin_inff() : __builtin_inff()) : 0.f;
-                        __builtin_amdgcn_sched_barrier(0);   // (one after the other: few registers, and time does not matter here)
-                    }
-#pragma unroll
-                    for (int u = 0; u < 2; ++u)
-                        o[n][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, finite_only(__builtin_bit_cast(uint4, values(j, u)))), weight[n][u], o[n][j], 0, 0, 0);
-                    __builtin_amdgcn_sched_barrier(0);
+                    for (int u = 0; u < 2; ++u) v[u][j] = __builtin_bit_cast(bf16x8, finite_only(__builtin_bit_cast(uint4, v[u][j])));
                 }
-            return;
+            }
         }
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const bf16x8 v = values(j, u);
+            for (int j = 0; j < 4; ++j)
 #pragma unroll
-                for (int n = 0; n < RT; ++n) o[n][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, weight[n][u], o[n][j], 0, 0, 0);
-            }
+                for (int n = 0; n < RT; ++n) o[n][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[u][j], weight[n][u], o[n][j], 0, 0, 0);
     };
 
     int k0 = k_lo, ahead = block_at(k_lo + 16 * wave);
@@ -323,11 +329,16 @@ __global__ __launch_bounds__(kTileThreads, RT == 1 ? 2 : 1) void attend_tile_ker
             load(next, k0 + kTileKeys + 16 * wave, ahead);
             ahead = block_at(k0 + 2 * kTileKeys + 16 * wave);
         }
-        // (keys behind the last position of the wave's rows have nothing for it)
         if (!idle) {
+            const int32_t lim = here.lim[min(lane, 11)];
 #pragma unroll 1
-            for (int U = 0; U < 2; ++U)
-                if (__ballot((here.pos[32 * U + col] <= last_pos) & ((col & 15) < here.n[2 * U + (col >> 4)]))) compute(here, U);
+            for (int U = 0; U < 2; ++U) {
+                const int32_t hi = max(__builtin_amdgcn_readlane(lim, 2 * U), __builtin_amdgcn_readlane(lim, 2 * U + 1));
+                const int32_t lo = min(__builtin_amdgcn_readlane(lim, 4 + 2 * U), __builtin_amdgcn_readlane(lim, 5 + 2 * U));
+                const int n = __builtin_amdgcn_readlane(lim, 8 + 2 * U) + __builtin_amdgcn_readlane(lim, 9 + 2 * U);
+                if (n == 0 || lo > last_pos) continue;   // (not there, or behind the last position of the wave's rows)
+                compute(here, U, n < 32 || hi > first_pos);
+            }
         }
         if (more) put(next);
         k0 += kTileKeys;

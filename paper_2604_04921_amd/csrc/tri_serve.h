@@ -114,7 +114,7 @@ __device__ __forceinline__ int keys_of(const AttendArgs &a, int s, int h)
 }
 
 // How the keys of a cache are cut: ranges per head, and their least keys (a function of bounds alone, for the workspace's size).
-void attend_split(const tri_model &m, const tri_cache &c, int32_t max_tokens, int32_t *n_split, int32_t *least_keys);
+void attend_split(const tri_model &m, const tri_cache &c, int32_t max_tokens, int32_t n_tokens, int32_t *n_split, int32_t *least_keys);
 tri_status launch_attend(AttendArgs a, const tri_cache &c, hipStream_t st);   // (c: a.src's)
 tri_status launch_join(const AttendArgs &a, int32_t parts, int32_t n_q_heads, int32_t dtype, hipStream_t st);
 

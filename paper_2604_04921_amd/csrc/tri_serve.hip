@@ -76,8 +76,8 @@ size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 AttendPlan attend_plan(const tri_model &m, const tri_cache *prefix, const tri_cache &c, const tri_tokens &t)
 {
     AttendPlan p{};
-    attend_split(m, c, most_tokens(t), &p.own_split, &p.own_least);
-    if (prefix) attend_split(m, *prefix, std::max(t.n_tokens, 1), &p.prefix_split, &p.prefix_least);
+    attend_split(m, c, most_tokens(t), t.n_tokens, &p.own_split, &p.own_least);
+    if (prefix) attend_split(m, *prefix, std::max(t.n_tokens, 1), t.n_tokens, &p.prefix_split, &p.prefix_least);
     p.parts = p.own_split + p.prefix_split;
     if (p.parts == 1) p.parts = 0;
     const size_t rows = (size_t)t.n_tokens * m.n_q_heads;
