@@ -10,8 +10,9 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 typedef __attribute__((address_space(3))) void lds_void;
 
-constexpr int kTileThreads = 256;
-constexpr int kTileKeys = 64;
+constexpr int kWaves = 4, kRows = 32 * kWaves;   // rows of a workgroup
+constexpr int kTileKeys = 64, kKeys = kTileKeys / kWaves;   // keys of a tile, and those of them that a wave brings
+static_assert(kRows == kTileRows, "");
 constexpr float kStaleBits = 8.f;   // powers of two by which a score may pass the maximum that weights are relative to
 
 // Rotates a lane's 64 elements of a row: x[c][e] is dimension 16 c + 8 h + e.
@@ -38,13 +39,13 @@ __device__ __forceinline__ void fresh(uint32_t &x) { asm volatile("" : "+v"(x));
 struct TileBuffer {
     __bf16 k[kTileKeys * kHeadDim], v[kTileKeys * kHeadDim];
     int32_t pos[kTileKeys];
-    int32_t lim[12];   // of the four sixteens: highest and lowest position, and how many keys there are
+    int32_t lim[3 * kWaves];   // of every wave's keys: highest and lowest position, and how many there are
 };
 
-template <int RT, bool PAGED, bool TURN, bool HALF>
-__global__ __launch_bounds__(kTileThreads, RT == 1 ? 2 : 1) void attend_tile_kernel(AttendArgs a)
+template <bool PAGED, bool TURN, bool HALF>
+__global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs a)
 {
-    constexpr int kWaveRows = 32 * RT, kRows = 4 * kWaveRows;
+    constexpr int kLanes = 64 / kKeys, kPieces = 16 / kLanes;   // TURN: lanes to a row of K, pieces to a lane
     __shared__ __align__(16) uint64_t turns[kBands];
     // (two objects and two copies of the loop's body: the compiler then knows that reading one does not have to wait for the loads into the other)
     __shared__ __align__(16) TileBuffer buf0, buf1;
@@ -71,16 +72,13 @@ __global__ __launch_bounds__(kTileThreads, RT == 1 ? 2 : 1) void attend_tile_ker
     if (tid < kBands) turns[tid] = a.turns.w[tid];
     __syncthreads();
 
-    bf16x8 q[RT][8];
-    int32_t t_pos[RT], first_pos = 0x7fffffff, last_pos = -0x7fffffff - 1;
-    bool real[RT];
-#pragma unroll
-    for (int n = 0; n < RT; ++n) {
-        const int at = r0 + wave * kWaveRows + 32 * n + col, r = min(at, rows - 1), t = tr.t0 + r / G, hq = head * G + r % G;
-        real[n] = at < rows;
-        t_pos[n] = a.causal ? a.pos[t] : 0x7fffffff;
-        first_pos = min(first_pos, t_pos[n]);
-        last_pos = max(last_pos, real[n] ? t_pos[n] : last_pos);
+    // this lane's row: column `col` of S^T and O^T
+    const int at = r0 + 32 * wave + col, r = min(at, rows - 1), t = tr.t0 + r / G, hq = head * G + r % G;
+    const bool real = at < rows;
+    const int32_t t_pos = a.causal ? a.pos[t] : 0x7fffffff;
+    int32_t first_pos = t_pos, last_pos = real ? t_pos : -0x7fffffff - 1;
+    bf16x8 q[8];
+    {
         const char *p = a.q + ((int64_t)t * a.q_stride_token + (int64_t)hq * a.q_stride_head) * 2 + 16 * h;
         if (a.rotate_q) {
             float v[8][8];
@@ -91,19 +89,18 @@ __global__ __launch_bounds__(kTileThreads, RT == 1 ? 2 : 1) void attend_tile_ker
 #pragma unroll
             for (int j = 0; j < 8; ++j)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) q[n][j][e] = (__bf16)v[j][e];
+                for (int e = 0; e < 8; ++e) q[j][e] = (__bf16)v[j][e];
         } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) q[n][j] = *reinterpret_cast<const bf16x8 *>(p + 32 * j);
+            for (int j = 0; j < 8; ++j) q[j] = *reinterpret_cast<const bf16x8 *>(p + 32 * j);
         }
     }
 #pragma unroll
     for (int i = 1; i < 32; i *= 2) first_pos = min(first_pos, __shfl_xor(first_pos, i)), last_pos = max(last_pos, __shfl_xor(last_pos, i));
     first_pos = __builtin_amdgcn_readfirstlane(first_pos);
     last_pos = __builtin_amdgcn_readfirstlane(last_pos);
-    const bool idle = r0 + wave * kWaveRows >= rows;
+    const bool idle = r0 + 32 * wave >= rows;
 
-    // Loading: wave w brings keys 16 w to 16 w + 15 of a tile.
     const int64_t base = (int64_t)a.layer * c.stride_layer + (int64_t)head * c.stride_head;
     const int64_t pbase = (int64_t)a.layer * c.pos_stride_layer + (int64_t)head * c.pos_stride_head;
     const uint32_t sb = (uint32_t)c.stride_slot * 2u;
@@ -111,14 +108,13 @@ __global__ __launch_bounds__(kTileThreads, RT == 1 ? 2 : 1) void attend_tile_ker
     // they stay the same from tile to tile).  Pieces of 16 bytes lie in LDS at their number exclusive-or the row (K) or twice the row (V), so that eight lanes of a 16-byte
     // read of neighbouring rows, and sixteen of a transposing 8-byte read of four rows, meet different banks.
     const uint32_t row4 = lane >> 4;
-    const uint32_t piece_k = TURN ? (lane & 3) * 16 : ((lane & 15) ^ row4) * 16, piece_v = ((lane & 15) ^ (2 * row4)) * 16, from_row = (TURN ? lane >> 2 : row4) * sb;
+    const uint32_t piece_k = ((lane & 15) ^ row4) * 16, piece_v = ((lane & 15) ^ (2 * row4)) * 16, from_row = row4 * sb;
     auto block_at = [&](int k0) {
         return PAGED ? __builtin_amdgcn_readfirstlane(c.block_table[(int64_t)s * c.max_blocks + (min(k0, k_hi - 1) >> c.block_shift)]) : 0;
     };
-    uint4 k_new[4];
-    int32_t pos_new = 0, turn_pos = 0, n_new = 0;
+    int32_t pos_new = 0, n_new = 0;
     auto load = [&](TileBuffer &to, int k0, int block) __attribute__((always_inline)) {   // k0: this wave's first key
-        int n = __builtin_amdgcn_readfirstlane(min(max(k_hi - k0, 0), 16));
+        int n = __builtin_amdgcn_readfirstlane(min(max(k_hi - k0, 0), kKeys));
         int64_t kv, at;
         if (PAGED) {
             const int in = k0 & ((1 << c.block_shift) - 1);
@@ -136,157 +132,152 @@ __global__ __launch_bounds__(kTileThreads, RT == 1 ? 2 : 1) void attend_tile_ker
         const auto vr = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>((const char *)c.v) + kv * 2, 0, bytes, 0x00027000);
         uint32_t row = from_row, pk = piece_k, pv = piece_v;
         fresh(row), fresh(pk), fresh(pv);
-        const uint32_t row_v = TURN ? row4 * sb : row;
         const auto pr = __builtin_amdgcn_make_buffer_rsrc(const_cast<int32_t *>(c.pos) + at, 0, a.causal || TURN ? n * 4 : 0, 0x00027000);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (TURN) k_new[i] = as_uint4(__builtin_amdgcn_raw_buffer_load_b128(kr, row + pk + 64 * i, 0, 0));
-            else __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, (lds_void *)(to.k + (16 * wave + 4 * i) * kHeadDim), 16, row + 4 * i * sb + (pk ^ (64 * i)), 0, 0, 0);
-        }
+        for (int i = 0; i < kKeys / 4; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, (lds_void *)(to.k + (kKeys * wave + 4 * i) * kHeadDim), 16, row + 4 * i * sb + (pk ^ (64 * i)), 0, 0, 0);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, (lds_void *)(to.v + (16 * wave + 4 * i) * kHeadDim), 16, row_v + 4 * i * sb + (pv ^ (128 * (i & 1))), 0, 0, 0);
-        pos_new = __builtin_amdgcn_raw_buffer_load_b32(pr, (lane & 15) * 4, 0, 0);
-        if (TURN) turn_pos = __builtin_amdgcn_raw_buffer_load_b32(pr, (lane >> 2) * 4, 0, 0);
+        for (int i = 0; i < kKeys / 4; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, (lds_void *)(to.v + (kKeys * wave + 4 * i) * kHeadDim), 16, row + 4 * i * sb + (pv ^ (128 * (i & 1))), 0, 0, 0);
+        pos_new = __builtin_amdgcn_raw_buffer_load_b32(pr, (lane % kKeys) * 4, 0, 0);
     };
-    auto put = [&](TileBuffer &to) __attribute__((always_inline)) {   // what passes through registers
+    // What the loads have brought, when it has come: the wave's own keys are turned where they lie, their positions written down.
+    auto put = [&](TileBuffer &to) __attribute__((always_inline)) {
         if (TURN) {
-            float v[4][8];
+            const int row = lane / kLanes, turn_pos = __shfl(pos_new, row);
+            bf16x8 *k = reinterpret_cast<bf16x8 *>(to.k + (kKeys * wave + row) * kHeadDim);
+            float v[kPieces][8];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) widen8(k_new[i], v[i]);
+            for (int i = 0; i < kPieces; ++i) widen8(__builtin_bit_cast(uint4, k[(lane % kLanes + kLanes * i) ^ row]), v[i]);
 #pragma unroll
-            for (int i = 0; i < (HALF ? 2 : 4); ++i)
+            for (int i = 0; i < (HALF ? kPieces / 2 : kPieces); ++i)
 #pragma unroll
                 for (int e = 0; e < (HALF ? 8 : 4); ++e) {
-                    const int piece = (lane & 3) + 4 * i;
+                    const int piece = lane % kLanes + kLanes * i;
                     const uint64_t t = turns[HALF ? 8 * piece + e : 4 * piece + e];
                     float cs, sn;
                     turn_fast(phase_of(turn_pos, (uint32_t)t, (uint32_t)(t >> 32)), &cs, &sn);
-                    float &r = HALF ? v[i][e] : v[i][2 * e], &im = HALF ? v[(i + 2) & 3][e] : v[i][(2 * e + 1) & 7];
+                    float &r = HALF ? v[i][e] : v[i][2 * e], &im = HALF ? v[(i + kPieces / 2) % kPieces][e] : v[i][(2 * e + 1) & 7];
                     const float re = r, im0 = im;
                     r = fmaf(re, cs, -(im0 * sn));
                     im = fmaf(re, sn, im0 * cs);
                 }
-            const int row = lane >> 2;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < kPieces; ++i) {
                 bf16x8 u;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) u[e] = (__bf16)v[i][e];
-                *reinterpret_cast<bf16x8 *>(to.k + (16 * wave + row) * kHeadDim + 8 * (((lane & 3) + 4 * i) ^ row)) = u;
+                k[(lane % kLanes + kLanes * i) ^ row] = u;
             }
         }
-        const bool there = (lane & 15) < n_new;   // (the four sixteens of lanes hold the same)
+        const bool there = lane % kKeys < n_new;   // (lanes kKeys apart hold the same)
         int32_t hi = there ? pos_new : -0x7fffffff - 1, lo = there ? pos_new : 0x7fffffff;
 #pragma unroll
-        for (int i = 1; i < 16; i *= 2) hi = max(hi, __shfl_xor(hi, i)), lo = min(lo, __shfl_xor(lo, i));
-        if (lane < 16) to.pos[16 * wave + lane] = pos_new;
-        if (lane == 0) to.lim[wave] = hi, to.lim[4 + wave] = lo, to.lim[8 + wave] = n_new;
+        for (int i = 1; i < kKeys; i *= 2) hi = max(hi, __shfl_xor(hi, i)), lo = min(lo, __shfl_xor(lo, i));
+        if (lane < kKeys) to.pos[kKeys * wave + lane] = pos_new;
+        if (lane == 0) to.lim[wave] = hi, to.lim[kWaves + wave] = lo, to.lim[2 * kWaves + wave] = n_new;
     };
 
-    f32x16 o[RT][4];
-    float top[RT], sum[RT];
+    f32x16 o[4];
+    float top = kNoScore, sum = 0.f;
 #pragma unroll
-    for (int n = 0; n < RT; ++n) {
-        top[n] = kNoScore;
-        sum[n] = 0.f;
+    for (int j = 0; j < 4; ++j)
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[n][j][i] = 0.f;
-    }
+        for (int i = 0; i < 16; ++i) o[j][i] = 0.f;
     // the lane's operands in a tile: dimension group j of its K row at at_k ^ 32 j; of the V rows of a step, dimensions 32 j + col at at_v ^ 64 j
     const uint32_t row_v0 = 4 * h + ((lane & 15) >> 2);
     const uint32_t at_k = col * 256 + (h ^ (col & 15)) * 16;
     const uint32_t at_v = row_v0 * 256 + (((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ (2 * row_v0)) * 16) + (lane & 1) * 8;
 
-    // 32 keys: half U of a tile.  mask: some of them are not everyone's
-    auto compute = [&](const TileBuffer &from, const int U, const bool mask) __attribute__((always_inline)) {
-        uint32_t ak = at_k + U * 32 * 256, av = at_v + U * 32 * 256;
+    // mask: some of the tile's keys are not everyone's
+    auto compute = [&](const TileBuffer &from, const bool mask) __attribute__((always_inline)) {
+        uint32_t ak = at_k, av = at_v;
         fresh(ak), fresh(av);
-        f32x16 sc[RT];
-#pragma unroll
-        for (int n = 0; n < RT; ++n)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) sc[n][i] = 0.f;
-        bf16x8 k[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) k[j] = *reinterpret_cast<const bf16x8 *>((const char *)from.k + (ak ^ (32 * j)));
-        __builtin_amdgcn_sched_barrier(0);   // all reads under way before the first product waits for one
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-#pragma unroll
-            for (int n = 0; n < RT; ++n) sc[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[j], q[n][j], sc[n], 0, 0, 0);
-        bf16x8 v[2][4];   // v[u][j]: dimensions 32 j + col, the keys of weight[.][u]; asked for ahead of the softmax
+        f32x16 sc[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const uint32_t at = av ^ (64 * j);
-                const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)((const char *)from.v + at + 16 * 256 * u));
-                const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)((const char *)from.v + at + (16 * 256 * u + 8 * 256)));
-                v[u][j] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-            }
-        __builtin_amdgcn_sched_barrier(0);
-        uint32_t keep[RT];   // bit i: key 8 (i / 4) + 4 h + i % 4 is attended to
-        bool hole = false;
-#pragma unroll
-        for (int n = 0; n < RT; ++n) keep[n] = 0xffffu;
-        if (mask) {
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int n_there = from.lim[8 + 2 * U + g / 2] - (8 * (g & 1) + 4 * h);
-                const int4 p4 = *reinterpret_cast<const int4 *>(&from.pos[32 * U + 8 * g + 4 * h]);
-                const int32_t p[4] = {p4.x, p4.y, p4.z, p4.w};
-#pragma unroll
-                for (int d = 0; d < 4; ++d) {
-                    const int i = 4 * g + d;
-#pragma unroll
-                    for (int n = 0; n < RT; ++n) {
-                        const bool on = (d < n_there) & (p[d] <= t_pos[n]);   // (not causal: t_pos is the highest there is)
-                        keep[n] &= on ? ~0u : ~(1u << i);
-                        sc[n][i] = on ? sc[n][i] : kNoScore;
-                        hole |= (d < n_there) & !on & real[n];
-                    }
-                }
-            }
-        }
-        bf16x8 weight[RT][2];
-#pragma unroll
-        for (int n = 0; n < RT; ++n) {
-            float best = kNoScore;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) best = fmaxf(best, sc[n][i]);
-            const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(best), __float_as_uint(best), false, false);
-            best = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
-            // weights are relative to a maximum that scores may pass by a factor of 2^8 before the sums are brought to the new one
-            if (__ballot(best > top[n] && !((best - top[n]) * a.scale_log2 <= kStaleBits))) {
-                const float next = fmaxf(top[n], best);
-                const float shrink = next == kNoScore ? 1.f : __builtin_amdgcn_exp2f((top[n] - next) * a.scale_log2);
-                top[n] = next;
-                sum[n] *= shrink;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) o[n][j] *= shrink;
-            }
-            const float off = (top[n] == kNoScore ? 0.f : top[n]) * a.scale_log2;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float p = __builtin_amdgcn_exp2f(fmaf(sc[n][i], a.scale_log2, -off));
-                sum[n] += p;
-                weight[n][i / 8][i % 8] = (__bf16)p;
-            }
-        }
-        if (__ballot(hole)) {   // (see attend_general_kernel: values that are not finite and not everyone's)
-            bool odd = false;
+            for (int i = 0; i < 16; ++i) sc[u][i] = 0.f;
+        bf16x8 k[2][8], v[2][4];   // v[u][j]: dimensions 32 j + col, the keys of weight[u]
+        auto values = [&](int U) __attribute__((always_inline)) {
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) odd |= not_finite(__builtin_bit_cast(uint4, v[u][j]));
-            if (__ballot(odd)) {
-#pragma unroll
                 for (int j = 0; j < 4; ++j) {
+                    const uint32_t at = av ^ (64 * j);
+                    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)((const char *)from.v + at + (32 * 256 * U + 16 * 256 * u)));
+                    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)((const char *)from.v + at + (32 * 256 * U + 16 * 256 * u + 8 * 256)));
+                    v[u][j] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+                }
+        };
 #pragma unroll
-                    for (int n = 0; n < RT; ++n)
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) k[u][j] = *reinterpret_cast<const bf16x8 *>((const char *)from.k + (ak ^ (32 * j)) + 32 * 256 * u);
+        __builtin_amdgcn_sched_barrier(0);   // all reads under way before the first product waits for one
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[0][j], q[j], sc[0], 0, 0, 0);
+        values(0);   // asked for ahead of the softmax
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sc[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[1][j], q[j], sc[1], 0, 0, 0);
+        uint32_t keep = ~0u;   // bit 16 u + i: key 32 u + 8 (i / 4) + 4 h + i % 4 is attended to
+        bool hole = false;
+        if (mask) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const int first = 32 * u + 8 * g + 4 * h, n_there = from.lim[2 * kWaves + first / kKeys] - first % kKeys;
+                    const int4 p4 = *reinterpret_cast<const int4 *>(&from.pos[first]);
+                    const int32_t p[4] = {p4.x, p4.y, p4.z, p4.w};
+#pragma unroll
+                    for (int d = 0; d < 4; ++d) {
+                        const int i = 4 * g + d;
+                        const bool on = (d < n_there) & (p[d] <= t_pos);   // (not causal: t_pos is the highest there is)
+                        keep &= on ? ~0u : ~(1u << (16 * u + i));
+                        sc[u][i] = on ? sc[u][i] : kNoScore;
+                        hole |= (d < n_there) & !on & real;
+                    }
+                }
+        }
+        float best = kNoScore;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) best = fmaxf(best, sc[u][i]);
+        const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(best), __float_as_uint(best), false, false);
+        best = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
+        // weights are relative to a maximum that scores may pass by a factor of 2^8 before the sums are brought to the new one
+        if (__ballot(best > top && !((best - top) * a.scale_log2 <= kStaleBits))) {
+            const float next = fmaxf(top, best);
+            const float shrink = next == kNoScore ? 1.f : __builtin_amdgcn_exp2f((top - next) * a.scale_log2);
+            top = next;
+            sum *= shrink;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[j] *= shrink;
+        }
+        const float off = (top == kNoScore ? 0.f : top) * a.scale_log2;
+        const bool holes = __ballot(hole);
+#pragma unroll
+        for (int U = 0; U < 2; ++U) {
+            bf16x8 weight[2];
+            if (U == 1) values(1);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float p = __builtin_amdgcn_exp2f(fmaf(sc[U][i], a.scale_log2, -off));
+                sum += p;
+                weight[i / 8][i % 8] = (__bf16)p;
+            }
+            if (holes) {   // (see attend_general_kernel: values that are not finite and not everyone's)
+                bool odd = false;
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) odd |= not_finite(__builtin_bit_cast(uint4, v[u][j]));
+                if (__ballot(odd)) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
 #pragma unroll
                         for (int side = 0; side < 2; ++side) {
                             f32x16 some;
@@ -296,49 +287,48 @@ __global__ __launch_bounds__(kTileThreads, RT == 1 ? 2 : 1) void attend_tile_ker
                             for (int u = 0; u < 2; ++u) {
                                 bf16x8 on;
 #pragma unroll
-                                for (int d = 0; d < 8; ++d) on[d] = (keep[n] >> (8 * u + d)) & 1 ? (__bf16)1.f : (__bf16)0.f;
+                                for (int d = 0; d < 8; ++d) on[d] = (keep >> (16 * U + 8 * u + d)) & 1 ? (__bf16)1.f : (__bf16)0.f;
                                 some = __builtin_amdgcn_mfma_f32_32x32x16_bf16(where_not_below(v[u][j], side ? 0xff80 : 0x7f80), on, some, 0, 0, 0);
                             }
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) o[n][j][i] += some[i] > 0.f ? (side ? -__builtin_inff() : __builtin_inff()) : 0.f;
+                            for (int i = 0; i < 16; ++i) o[j][i] += some[i] > 0.f ? (side ? -__builtin_inff() : __builtin_inff()) : 0.f;
                             __builtin_amdgcn_sched_barrier(0);   // (one after the other: few registers, and time does not matter here)
                         }
 #pragma unroll
-                    for (int u = 0; u < 2; ++u) v[u][j] = __builtin_bit_cast(bf16x8, finite_only(__builtin_bit_cast(uint4, v[u][j])));
+                        for (int u = 0; u < 2; ++u) v[u][j] = __builtin_bit_cast(bf16x8, finite_only(__builtin_bit_cast(uint4, v[u][j])));
+                    }
                 }
             }
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[u][j], weight[u], o[j], 0, 0, 0);
         }
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int n = 0; n < RT; ++n) o[n][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[u][j], weight[n][u], o[n][j], 0, 0, 0);
     };
 
-    int k0 = k_lo, ahead = block_at(k_lo + 16 * wave);
+    int k0 = k_lo, ahead = block_at(k_lo + kKeys * wave);
     if (k0 < k_hi) {
-        load(buf0, k0 + 16 * wave, ahead);
-        ahead = block_at(k0 + kTileKeys + 16 * wave);
+        load(buf0, k0 + kKeys * wave, ahead);
+        ahead = block_at(k0 + kTileKeys + kKeys * wave);
         put(buf0);
     }
     auto step = [&](TileBuffer &here, TileBuffer &next) __attribute__((always_inline)) {
-        __syncthreads();   // this tile has come, and the last one is read
+        // This tile has come, and the last one is read.  The wait is said here: a barrier alone waits for a wave's own LDS accesses, not for its loads into LDS.
+        __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
+        __syncthreads();
         const bool more = k0 + kTileKeys < k_hi;
         if (more) {
-            load(next, k0 + kTileKeys + 16 * wave, ahead);
-            ahead = block_at(k0 + 2 * kTileKeys + 16 * wave);
+            load(next, k0 + kTileKeys + kKeys * wave, ahead);
+            ahead = block_at(k0 + 2 * kTileKeys + kKeys * wave);
         }
         if (!idle) {
-            const int32_t lim = here.lim[min(lane, 11)];
-#pragma unroll 1
-            for (int U = 0; U < 2; ++U) {
-                const int32_t hi = max(__builtin_amdgcn_readlane(lim, 2 * U), __builtin_amdgcn_readlane(lim, 2 * U + 1));
-                const int32_t lo = min(__builtin_amdgcn_readlane(lim, 4 + 2 * U), __builtin_amdgcn_readlane(lim, 5 + 2 * U));
-                const int n = __builtin_amdgcn_readlane(lim, 8 + 2 * U) + __builtin_amdgcn_readlane(lim, 9 + 2 * U);
-                if (n == 0 || lo > last_pos) continue;   // (not there, or behind the last position of the wave's rows)
-                compute(here, U, n < 32 || hi > first_pos);
-            }
+            const int32_t lim = here.lim[min(lane, 3 * kWaves - 1)];
+            int32_t hi = -0x7fffffff - 1, lo = 0x7fffffff, n = 0;
+#pragma unroll
+            for (int i = 0; i < kWaves; ++i)
+                hi = max(hi, __builtin_amdgcn_readlane(lim, i)), lo = min(lo, __builtin_amdgcn_readlane(lim, kWaves + i)), n += __builtin_amdgcn_readlane(lim, 2 * kWaves + i);
+            // (nothing to do where no key is there, or all are behind the last position of the wave's rows)
+            if (n > 0 && lo <= last_pos) compute(here, n < kTileKeys || hi > first_pos);
         }
         if (more) put(next);
         k0 += kTileKeys;
@@ -347,49 +337,44 @@ __global__ __launch_bounds__(kTileThreads, RT == 1 ? 2 : 1) void attend_tile_ker
     if (k0 < k_hi)
         while (step(buf0, buf1) && step(buf1, buf0)) {
         }
+    const float total = sum + __shfl_xor(sum, 32);
+    if (!real) return;
+    if (a.part_o) {
+        const int64_t row = ((int64_t)(a.src.part0 + split) * a.n_tokens + t) * Hq + hq;
+        if (h == 0) a.part_ml[row] = make_float2(top, total);
 #pragma unroll
-    for (int n = 0; n < RT; ++n) {
-        if (!real[n]) continue;
-        const int r = r0 + wave * kWaveRows + 32 * n + col, t = tr.t0 + r / G, hq = head * G + r % G;
-        const float total = sum[n] + __shfl_xor(sum[n], 32);
-        if (a.part_o) {
-            const int64_t at = ((int64_t)(a.src.part0 + split) * a.n_tokens + t) * Hq + hq;
-            if (h == 0) a.part_ml[at] = make_float2(top[n], total);
+        for (int j = 0; j < 4; ++j)
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int i = 0; i < 16; i += 4)
-                    *reinterpret_cast<f32x4 *>(a.part_o + at * kHeadDim + 32 * j + 2 * i + 4 * h) = f32x4{o[n][j][i], o[n][j][i + 1], o[n][j][i + 2], o[n][j][i + 3]};
-        } else {
-            const float inv = total != 0.f ? 1.f / total : 0.f;
-            __bf16 *p = reinterpret_cast<__bf16 *>(a.out) + (int64_t)t * a.out_stride_token + (int64_t)hq * a.out_stride_head;
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int i = 0; i < 16; i += 4) {
-                    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-                    bf16x4 b;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) b[e] = (__bf16)(total != 0.f ? o[n][j][i + e] * inv : 0.f);
-                    *reinterpret_cast<bf16x4 *>(p + 32 * j + 2 * i + 4 * h) = b;
-                }
-        }
+            for (int i = 0; i < 16; i += 4)
+                *reinterpret_cast<f32x4 *>(a.part_o + row * kHeadDim + 32 * j + 2 * i + 4 * h) = f32x4{o[j][i], o[j][i + 1], o[j][i + 2], o[j][i + 3]};
+        return;
     }
+    const float inv = 1.f / total;
+    __bf16 *p = reinterpret_cast<__bf16 *>(a.out) + (int64_t)t * a.out_stride_token + (int64_t)hq * a.out_stride_head;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+            typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+            bf16x4 b;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) b[e] = (__bf16)(total != 0.f ? o[j][i + e] * inv : 0.f);
+            *reinterpret_cast<bf16x4 *>(p + 32 * j + 2 * i + 4 * h) = b;
+        }
 }
 
 }  // namespace
 
 tri_status launch_attend_tile(AttendArgs a, int32_t rows, hipStream_t st)
 {
-    constexpr int RT = kTileRows / 128;
-    a.row_tiles = (rows + kTileRows - 1) / kTileRows;
+    a.row_tiles = (rows + kRows - 1) / kRows;
     const int64_t groups = (int64_t)a.src.n_split * a.src.cache.n_kv_heads * a.src.cache.n_seqs;
     const uint32_t blocks = (uint32_t)((groups + 7) / 8 * 8 * a.row_tiles);
     const bool paged = a.src.cache.block_shift >= 0;
-    const auto launch = [&](auto kernel) { kernel<<<blocks, kTileThreads, 0, st>>>(a); };
-    if (a.src.cache.k_rotated) launch(paged ? attend_tile_kernel<RT, true, false, false> : attend_tile_kernel<RT, false, false, false>);
-    else if (a.half) launch(paged ? attend_tile_kernel<RT, true, true, true> : attend_tile_kernel<RT, false, true, true>);
-    else launch(paged ? attend_tile_kernel<RT, true, true, false> : attend_tile_kernel<RT, false, true, false>);
+    const auto launch = [&](auto kernel) { kernel<<<blocks, 64 * kWaves, 0, st>>>(a); };
+    if (a.src.cache.k_rotated) launch(paged ? attend_tile_kernel<true, false, false> : attend_tile_kernel<false, false, false>);
+    else if (a.half) launch(paged ? attend_tile_kernel<true, true, true> : attend_tile_kernel<false, true, true>);
+    else launch(paged ? attend_tile_kernel<true, true, false> : attend_tile_kernel<false, true, false>);
     return hip_status("attend_tile_kernel");
 }
 
