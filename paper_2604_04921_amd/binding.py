@@ -201,19 +201,17 @@ class Tokens:
         n = pos.numel()
         self.c = TriTokens(n, n if max_tokens is None else int(max_tokens), None if start is None else start.data_ptr(), pos.data_ptr(),
                            None if head_len is None else head_len.data_ptr(), int(bool(rotated)))
-
-    @property
-    def ref(self):
-        return ctypes.byref(self.c)
+        self.ref = ctypes.byref(self.c)
 
 
 def _rows(t, heads, tokens, cache, name):
-    """Rows [T][heads][d] of the cache's type, d dense; any strides of the other two."""
-    if t.dim() != 3 or tuple(t.shape) != (tokens.c.n_tokens, heads, 128) or t.stride(2) != 1:
+    """Strides of rows [T][heads][d] of the cache's type, d dense; any strides of the other two."""
+    strides = t.stride()
+    if t.shape != (tokens.c.n_tokens, heads, 128) or strides[2] != 1:
         raise ValueError("%s: [%d][%d][128] with dense rows, got %s" % (name, tokens.c.n_tokens, heads, tuple(t.shape)))
     if t.dtype != cache.tensors[0].dtype:
         raise TypeError("%s: %s, the cache holds %s" % (name, t.dtype, cache.tensors[0].dtype))
-    return t.stride(0), t.stride(1)
+    return strides
 
 
 def tri_append(model, cache, layer, tokens, k_new, v_new, new_seq_len=None, stream=None):
@@ -229,7 +227,7 @@ def _attention(model, cache, tokens, q, out, scale, causal):
     heads = model.c.n_q_heads
     qs, os_ = _rows(q, heads, tokens, cache, "q"), _rows(out, heads, tokens, cache, "out")
     return TriAttention(q.data_ptr(), out.data_ptr(), qs[0], qs[1], os_[0], os_[1], model.c.head_dim ** -0.5 if scale is None else scale,
-                        int(bool(causal)))
+                        1 if causal else 0)
 
 
 def tri_attend(model, cache, layer, tokens, q, out, scale=None, causal=True, workspace=None, stream=None):

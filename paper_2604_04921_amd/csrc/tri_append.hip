@@ -81,6 +81,12 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a)
     const int t_first = (int)(((int64_t)blockIdx.x * kAppendThreads + (threadIdx.x & ~63)) / kPieces / H);
     if (t_first >= a.n_tokens) return;   // (the whole wave)
     const int t = (int)(row / H), h = (int)(row - (int64_t)t * H);
+    // the rows are asked for before their place is known
+    const int64_t from = ((int64_t)min(t, a.n_tokens - 1) * a.stride_token + (int64_t)h * a.stride_head + part * kElems) * (int64_t)sizeof(T);
+    constexpr int64_t half_row = 64 * sizeof(T);
+    uint4 k0 = *reinterpret_cast<const uint4 *>(a.k_new + from), k1 = *reinterpret_cast<const uint4 *>(a.k_new + from + half_row);
+    const uint4 v0 = *reinterpret_cast<const uint4 *>(a.v_new + from), v1 = *reinterpret_cast<const uint4 *>(a.v_new + from + half_row);
+    const int32_t pos = a.pos[min(t, a.n_tokens - 1)];
     int s = t, first = t;
     if (a.start) {
         s = 0;
@@ -104,13 +110,8 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a)
         if (block < 0) return;
         n &= (1 << c.block_shift) - 1;
     }
-    const int64_t from = ((int64_t)t * a.stride_token + (int64_t)h * a.stride_head + part * kElems) * (int64_t)sizeof(T);
     const int64_t to = ((int64_t)a.layer * c.stride_layer + (int64_t)h * c.stride_head + block * c.stride_sb + slot_offset(c, n) + part * kElems) *
                        (int64_t)sizeof(T);
-    constexpr int64_t half_row = 64 * sizeof(T);
-    uint4 k0 = *reinterpret_cast<const uint4 *>(a.k_new + from), k1 = *reinterpret_cast<const uint4 *>(a.k_new + from + half_row);
-    const uint4 v0 = *reinterpret_cast<const uint4 *>(a.v_new + from), v1 = *reinterpret_cast<const uint4 *>(a.v_new + from + half_row);
-    const int32_t pos = a.pos[t];
     if (a.rotate) {
         float x[kElems], y[kElems];
         Piece<T>::get(k0, x);

@@ -55,8 +55,6 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attend_rows_kernel(AttendArgs
     const int rows = tr.n * G, r0 = rt * kRows;
     if (r0 >= rows) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15, kq = lane >> 4;
-    if (tid < kBands) turns[tid] = a.turns.w[tid];
-    __syncthreads();
     const KeyRange range = keys_of_split(a, s, h, split);
     if (range.lo >= range.hi && a.part_o) {
         no_keys(a, split, tr.t0, r0, min(rows - r0, kRows), h, Hq);
@@ -64,45 +62,6 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attend_rows_kernel(AttendArgs
     }
     const int k_hi = __builtin_amdgcn_readfirstlane(range.hi);   // (what buffer descriptors are made of stays in scalar registers)
 
-    // this lane's rows: columns m of the column tiles
-    bf16x8 q[NT][4];
-    int32_t t_pos[NT], first_pos = 0x7fffffff;
-    bool real[NT];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const int at = r0 + n * kCols + (LO ? m & 7 : m), r = min(at, rows - 1), t = tr.t0 + r / G, hq = h * G + r % G;
-        real[n] = at < rows;
-        t_pos[n] = a.causal ? a.pos[t] : 0x7fffffff;
-        first_pos = min(first_pos, t_pos[n]);
-        const char *p = a.q + ((int64_t)t * a.q_stride_token + (int64_t)hq * a.q_stride_head) * 2;
-        float x[4][8];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) widen8(*reinterpret_cast<const uint4 *>(p + 64 * j + 16 * kq), x[j]);
-        if (a.rotate_q) {
-            if (TURN ? HALF : (bool)a.half) rotate_row<true>(x, a.pos[t], kq, turns);
-            else rotate_row<false>(x, a.pos[t], kq, turns);
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const __bf16 hi = (__bf16)x[j][e];
-                q[n][j][e] = LO && m >= 8 ? (__bf16)(x[j][e] - (float)hi) : hi;
-            }
-    }
-#pragma unroll
-    for (int x = 1; x < 16; x *= 2) first_pos = min(first_pos, __shfl_xor(first_pos, x));
-    first_pos = __builtin_amdgcn_readfirstlane(first_pos);
-
-    f32x4 o[NT][8];
-    float top[NT], sum[NT];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        top[n] = kNoScore;
-        sum[n] = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) o[n][e] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
     const int64_t base = (int64_t)a.layer * c.stride_layer + (int64_t)h * c.stride_head;
     const int64_t pbase = (int64_t)a.layer * c.pos_stride_layer + (int64_t)h * c.pos_stride_head;
     const uint32_t sb = (uint32_t)c.stride_slot * 2u;
@@ -163,9 +122,52 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attend_rows_kernel(AttendArgs
     int k0 = __builtin_amdgcn_readfirstlane(range.lo) + kRowsTile * wave;
     Rows here[2] = {find(k0, block_at(k0)), find(k0 + 16, block_at(k0 + 16))};
     int ahead[2] = {block_at(k0 + kStep), block_at(k0 + kStep + 16)};
+    // The first tile is asked for before anything is known of the queries: in short rows most of the time is latency.
     load_k(here);
     __builtin_amdgcn_sched_barrier(0);   // (in this order, as in the loop: waiting for K's loads must not wait for V's)
     load_v(here);
+    if (tid < kBands) turns[tid] = a.turns.w[tid];
+    __syncthreads();
+
+    // this lane's rows: columns m of the column tiles
+    bf16x8 q[NT][4];
+    int32_t t_pos[NT], first_pos = 0x7fffffff;
+    bool real[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const int at = r0 + n * kCols + (LO ? m & 7 : m), r = min(at, rows - 1), t = tr.t0 + r / G, hq = h * G + r % G;
+        real[n] = at < rows;
+        t_pos[n] = a.causal ? a.pos[t] : 0x7fffffff;
+        first_pos = min(first_pos, t_pos[n]);
+        const char *p = a.q + ((int64_t)t * a.q_stride_token + (int64_t)hq * a.q_stride_head) * 2;
+        float x[4][8];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) widen8(*reinterpret_cast<const uint4 *>(p + 64 * j + 16 * kq), x[j]);
+        if (a.rotate_q) {
+            if (TURN ? HALF : (bool)a.half) rotate_row<true>(x, a.pos[t], kq, turns);
+            else rotate_row<false>(x, a.pos[t], kq, turns);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const __bf16 hi = (__bf16)x[j][e];
+                q[n][j][e] = LO && m >= 8 ? (__bf16)(x[j][e] - (float)hi) : hi;
+            }
+    }
+#pragma unroll
+    for (int x = 1; x < 16; x *= 2) first_pos = min(first_pos, __shfl_xor(first_pos, x));
+    first_pos = __builtin_amdgcn_readfirstlane(first_pos);
+
+    f32x4 o[NT][8];
+    float top[NT], sum[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        top[n] = kNoScore;
+        sum[n] = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[n][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
     for (; k0 < k_hi; k0 += kStep) {
         const Rows next[2] = {find(k0 + kStep, ahead[0]), find(k0 + kStep + 16, ahead[1])};
         ahead[0] = block_at(k0 + 2 * kStep);

@@ -69,38 +69,6 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
     }
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, h = lane >> 5;
     const int k_lo = __builtin_amdgcn_readfirstlane(range.lo), k_hi = __builtin_amdgcn_readfirstlane(range.hi);
-    if (tid < kBands) turns[tid] = a.turns.w[tid];
-    __syncthreads();
-
-    // this lane's row: column `col` of S^T and O^T
-    const int at = r0 + 32 * wave + col, r = min(at, rows - 1), t = tr.t0 + r / G, hq = head * G + r % G;
-    const bool real = at < rows;
-    const int32_t t_pos = a.causal ? a.pos[t] : 0x7fffffff;
-    int32_t first_pos = t_pos, last_pos = real ? t_pos : -0x7fffffff - 1;
-    bf16x8 q[8];
-    {
-        const char *p = a.q + ((int64_t)t * a.q_stride_token + (int64_t)hq * a.q_stride_head) * 2 + 16 * h;
-        if (a.rotate_q) {
-            float v[8][8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) widen8(*reinterpret_cast<const uint4 *>(p + 32 * j), v[j]);
-            if (TURN ? HALF : (bool)a.half) rotate_q<true>(v, a.pos[t], h, turns);
-            else rotate_q<false>(v, a.pos[t], h, turns);
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) q[j][e] = (__bf16)v[j][e];
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) q[j] = *reinterpret_cast<const bf16x8 *>(p + 32 * j);
-        }
-    }
-#pragma unroll
-    for (int i = 1; i < 32; i *= 2) first_pos = min(first_pos, __shfl_xor(first_pos, i)), last_pos = max(last_pos, __shfl_xor(last_pos, i));
-    first_pos = __builtin_amdgcn_readfirstlane(first_pos);
-    last_pos = __builtin_amdgcn_readfirstlane(last_pos);
-    const bool idle = r0 + 32 * wave >= rows;
-
     const int64_t base = (int64_t)a.layer * c.stride_layer + (int64_t)head * c.stride_head;
     const int64_t pbase = (int64_t)a.layer * c.pos_stride_layer + (int64_t)head * c.pos_stride_head;
     const uint32_t sb = (uint32_t)c.stride_slot * 2u;
@@ -110,7 +78,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
     const uint32_t row4 = lane >> 4;
     const uint32_t piece_k = ((lane & 15) ^ row4) * 16, piece_v = ((lane & 15) ^ (2 * row4)) * 16, from_row = row4 * sb;
     auto block_at = [&](int k0) {
-        return PAGED ? __builtin_amdgcn_readfirstlane(c.block_table[(int64_t)s * c.max_blocks + (min(k0, k_hi - 1) >> c.block_shift)]) : 0;
+        return PAGED ? __builtin_amdgcn_readfirstlane(c.block_table[(int64_t)s * c.max_blocks + (min(k0, max(k_hi - 1, 0)) >> c.block_shift)]) : 0;
     };
     int32_t pos_new = 0, n_new = 0;
     auto load = [&](TileBuffer &to, int k0, int block) __attribute__((always_inline)) {   // k0: this wave's first key
@@ -177,6 +145,44 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
         if (lane < kKeys) to.pos[kKeys * wave + lane] = pos_new;
         if (lane == 0) to.lim[wave] = hi, to.lim[kWaves + wave] = lo, to.lim[2 * kWaves + wave] = n_new;
     };
+
+    // The first tile is asked for before anything is known of the queries.
+    int k0 = k_lo, ahead = block_at(k_lo + kKeys * wave);
+    if (k0 < k_hi) {
+        load(buf0, k0 + kKeys * wave, ahead);
+        ahead = block_at(k0 + kTileKeys + kKeys * wave);
+    }
+    if (tid < kBands) turns[tid] = a.turns.w[tid];
+    __syncthreads();
+
+    // this lane's row: column `col` of S^T and O^T
+    const int at = r0 + 32 * wave + col, r = min(at, rows - 1), t = tr.t0 + r / G, hq = head * G + r % G;
+    const bool real = at < rows;
+    const int32_t t_pos = a.causal ? a.pos[t] : 0x7fffffff;
+    int32_t first_pos = t_pos, last_pos = real ? t_pos : -0x7fffffff - 1;
+    bf16x8 q[8];
+    {
+        const char *p = a.q + ((int64_t)t * a.q_stride_token + (int64_t)hq * a.q_stride_head) * 2 + 16 * h;
+        if (a.rotate_q) {
+            float v[8][8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) widen8(*reinterpret_cast<const uint4 *>(p + 32 * j), v[j]);
+            if (TURN ? HALF : (bool)a.half) rotate_q<true>(v, a.pos[t], h, turns);
+            else rotate_q<false>(v, a.pos[t], h, turns);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) q[j][e] = (__bf16)v[j][e];
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) q[j] = *reinterpret_cast<const bf16x8 *>(p + 32 * j);
+        }
+    }
+#pragma unroll
+    for (int i = 1; i < 32; i *= 2) first_pos = min(first_pos, __shfl_xor(first_pos, i)), last_pos = max(last_pos, __shfl_xor(last_pos, i));
+    first_pos = __builtin_amdgcn_readfirstlane(first_pos);
+    last_pos = __builtin_amdgcn_readfirstlane(last_pos);
+    const bool idle = r0 + 32 * wave >= rows;
 
     f32x16 o[4];
     float top = kNoScore, sum = 0.f;
@@ -306,12 +312,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
         }
     };
 
-    int k0 = k_lo, ahead = block_at(k_lo + kKeys * wave);
-    if (k0 < k_hi) {
-        load(buf0, k0 + kKeys * wave, ahead);
-        ahead = block_at(k0 + kTileKeys + kKeys * wave);
-        put(buf0);
-    }
+    if (k0 < k_hi) put(buf0);
     auto step = [&](TileBuffer &here, TileBuffer &next) __attribute__((always_inline)) {
         // This tile has come, and the last one is read.  The wait is said here: a barrier alone waits for a wave's own LDS accesses, not for its loads into LDS.
         __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)

@@ -112,6 +112,8 @@ def test_rows_without_a_key(dtype, tokens):
     out = run(B, c)
     check(out, c.want(roundings=roundings(c)))
     assert not out[:tokens[0]].any()
+    c = P.Case(5, (0, 0), tokens, dtype=dtype, appended=False, block=16)   # (no sequence has a key; the first page of the table is not read for one)
+    assert not run(B, c).any()
     c = P.Case(4, (40, 200), tokens, dtype=dtype, appended=False, pos0=1000)
     c.pos[:] = np.where(np.arange(c.T) % 2, c.pos, 5)
     out = run(B, c)
