@@ -54,6 +54,17 @@ __device__ __forceinline__ void no_keys(const AttendArgs &a, int split, int t0, 
     }
 }
 
+// The same value, as the compiler cannot tell: what follows from it is worked out where it is used instead of being kept in registers from tile to tile.
+__device__ __forceinline__ void fresh(uint32_t &x) { asm volatile("" : "+v"(x)); }
+
+// The lane's number worked out on the spot, in no register before or after.
+__device__ __forceinline__ uint32_t lane_again()
+{
+    uint32_t none = 0;
+    fresh(none);
+    return __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, none));
+}
+
 // lane ^ 8 of each sixteen
 __device__ __forceinline__ float across_8(float x) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x128, 0xf, 0xf, false)); }
 // the maximum over the four lanes that share lane & 15

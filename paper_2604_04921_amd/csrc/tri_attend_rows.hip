@@ -65,10 +65,6 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attend_rows_kernel(AttendArgs
     const int64_t base = (int64_t)a.layer * c.stride_layer + (int64_t)h * c.stride_head;
     const int64_t pbase = (int64_t)a.layer * c.pos_stride_layer + (int64_t)h * c.pos_stride_head;
     const uint32_t sb = (uint32_t)c.stride_slot * 2u;
-    const uint32_t lane_k = m * sb + kq * 16;
-    uint32_t lane_v[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) lane_v[j] = (4 * kq + j) * sb + m * 16;
     const bool need_pos = a.causal || TURN;
 
     // Sixteen keys: where their rows begin and how many there are (0: none, or their block is not there).  Lanes beyond the last row lie beyond the buffer and load zeros.
@@ -76,8 +72,9 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attend_rows_kernel(AttendArgs
         int64_t kv, pos;
         int n;
     };
-    auto find = [&](int k0, int block) {
+    auto find = [&](int k0, int block_loaded) {
         Rows r;
+        const int block = __builtin_amdgcn_readfirstlane(block_loaded);   // (here and not where it is asked for: that is a step ago)
         const int left = __builtin_amdgcn_readfirstlane(min(max(k_hi - k0, 0), 16));
         if (PAGED) {
             const int in = k0 & ((1 << c.block_shift) - 1);
@@ -93,29 +90,31 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attend_rows_kernel(AttendArgs
         return r;
     };
     auto block_at = [&](int k0) {
-        return PAGED ? __builtin_amdgcn_readfirstlane(c.block_table[(int64_t)s * c.max_blocks + (min(k0, max(k_hi - 1, 0)) >> c.block_shift)]) : 0;
+        return PAGED ? c.block_table[(int64_t)s * c.max_blocks + (min(k0, max(k_hi - 1, 0)) >> c.block_shift)] : 0;
     };
     auto rsrc = [&](const void *p, int64_t at, int n) {
-        return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>((const char *)p) + at * 2, 0, n > 0 ? (n - 1) * sb + kHeadDim * 2 : 0, 0x00027000);
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>((const char *)p) + at * 2, 0, __builtin_amdgcn_readfirstlane(n > 0 ? (n - 1) * sb + kHeadDim * 2 : 0), 0x00027000);
     };
     uint4 k[2][4], v[2][4];
     int32_t k_pos[2];
     auto load_k = [&](const Rows (&r)[2]) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
+            const uint32_t l = lane_again(), at = (l & 15) * sb + (l >> 4) * 16, at_pos = (l & 15) * 4;
             const auto b = rsrc(c.k, r[i].kv, r[i].n);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) k[i][j] = as_uint4(__builtin_amdgcn_raw_buffer_load_b128(b, lane_k + 64 * j, 0, kNonTemporal));
-            const auto p = __builtin_amdgcn_make_buffer_rsrc(const_cast<int32_t *>(c.pos) + r[i].pos, 0, need_pos ? r[i].n * 4 : 0, 0x00027000);
-            k_pos[i] = __builtin_amdgcn_raw_buffer_load_b32(p, m * 4, 0, 0);
+            for (int j = 0; j < 4; ++j) k[i][j] = as_uint4(__builtin_amdgcn_raw_buffer_load_b128(b, at + 64 * j, 0, kNonTemporal));
+            const auto p = __builtin_amdgcn_make_buffer_rsrc(const_cast<int32_t *>(c.pos) + r[i].pos, 0, __builtin_amdgcn_readfirstlane(need_pos ? r[i].n * 4 : 0), 0x00027000);
+            k_pos[i] = __builtin_amdgcn_raw_buffer_load_b32(p, at_pos, 0, 0);
         }
     };
     auto load_v = [&](const Rows (&r)[2]) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
+            const uint32_t l = lane_again(), at = (l >> 4) * 4 * sb + (l & 15) * 16;
             const auto b = rsrc(c.v, r[i].kv, r[i].n);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[i][j] = as_uint4(__builtin_amdgcn_raw_buffer_load_b128(b, lane_v[j], 0, kNonTemporal));
+            for (int j = 0; j < 4; ++j) v[i][j] = as_uint4(__builtin_amdgcn_raw_buffer_load_b128(b, at + j * sb, 0, kNonTemporal));
         }
     };
     constexpr int kStep = 4 * kRowsTile;
@@ -218,12 +217,13 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attend_rows_kernel(AttendArgs
 #pragma unroll
         for (int n = 0; n < NT; ++n) keep[n] = 0xffu;
         if (late || here[0].n < 16 || here[1].n < 16) {
+            const uint32_t key = (lane_again() >> 4) * 4;
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
                 for (int d = 0; d < 4; ++d) {
-                    const bool there = 4 * kq + d < here[i].n;
-                    const int32_t p = __shfl(pos_here[i], 4 * kq + d);
+                    const bool there = (int)key + d < here[i].n;
+                    const int32_t p = __shfl(pos_here[i], (int)key + d);
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
                         const bool on = there && (!a.causal || p <= t_pos[n]);
@@ -277,20 +277,20 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attend_rows_kernel(AttendArgs
                 for (int j = 0; j < 4; ++j) odd |= not_finite(v[i][j]);
             if (__ballot(odd)) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const bf16x8 x = column(v, e), up_at = where_not_below(x, 0x7f80), down_at = where_not_below(x, 0xff80);
+                for (int e = 0; e < 8; ++e)
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
                         bf16x8 on;
 #pragma unroll
                         for (int d = 0; d < 8; ++d) on[d] = (keep[n] >> d) & 1 ? (__bf16)1.f : (__bf16)0.f;
-                        const f32x4 none = f32x4{0.f, 0.f, 0.f, 0.f};
-                        const f32x4 up = __builtin_amdgcn_mfma_f32_16x16x32_bf16(up_at, on, none, 0, 0, 0);
-                        const f32x4 down = __builtin_amdgcn_mfma_f32_16x16x32_bf16(down_at, on, none, 0, 0, 0);
 #pragma unroll
-                        for (int d = 0; d < 4; ++d) o[n][e][d] += (up[d] > 0.f ? __builtin_inff() : 0.f) + (down[d] > 0.f ? -__builtin_inff() : 0.f);
+                        for (int side = 0; side < 2; ++side) {
+                            const f32x4 some = __builtin_amdgcn_mfma_f32_16x16x32_bf16(where_not_below(column(v, e), side ? 0xff80 : 0x7f80), on, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+                            for (int d = 0; d < 4; ++d) o[n][e][d] += some[d] > 0.f ? (side ? -__builtin_inff() : __builtin_inff()) : 0.f;
+                            __builtin_amdgcn_sched_barrier(0);   // (one after the other: few registers, and time does not matter here)
+                        }
                     }
-                }
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
 #pragma unroll

@@ -33,9 +33,6 @@ __device__ __forceinline__ void rotate_q(float (*x)[8], int32_t pos, int h, cons
         }
 }
 
-// The same value, as the compiler cannot tell.
-__device__ __forceinline__ void fresh(uint32_t &x) { asm volatile("" : "+v"(x)); }
-
 struct TileBuffer {
     __bf16 k[kTileKeys * kHeadDim], v[kTileKeys * kHeadDim];
     int32_t pos[kTileKeys];
@@ -78,10 +75,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
     const uint32_t row4 = lane >> 4;
     const uint32_t piece_k = ((lane & 15) ^ row4) * 16, piece_v = ((lane & 15) ^ (2 * row4)) * 16, from_row = row4 * sb;
     auto block_at = [&](int k0) {
-        return PAGED ? __builtin_amdgcn_readfirstlane(c.block_table[(int64_t)s * c.max_blocks + (min(k0, max(k_hi - 1, 0)) >> c.block_shift)]) : 0;
+        return PAGED ? c.block_table[(int64_t)s * c.max_blocks + (min(k0, max(k_hi - 1, 0)) >> c.block_shift)] : 0;
     };
     int32_t pos_new = 0, n_new = 0;
-    auto load = [&](TileBuffer &to, int k0, int block) __attribute__((always_inline)) {   // k0: this wave's first key
+    auto load = [&](TileBuffer &to, int k0, int block_loaded) __attribute__((always_inline)) {   // k0: this wave's first key
+        const int block = __builtin_amdgcn_readfirstlane(block_loaded);   // (here and not where it is asked for: that is a tile ago)
         int n = __builtin_amdgcn_readfirstlane(min(max(k_hi - k0, 0), kKeys));
         int64_t kv, at;
         if (PAGED) {
@@ -95,12 +93,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
             at = pbase + (int64_t)s * c.pos_stride_sb + k0;
         }
         n_new = n;
-        const uint32_t bytes = n > 0 ? (n - 1) * sb + kHeadDim * 2 : 0;   // (lanes beyond it bring zeros)
+        const uint32_t bytes = __builtin_amdgcn_readfirstlane(n > 0 ? (n - 1) * sb + kHeadDim * 2 : 0);   // (lanes beyond it bring zeros)
         const auto kr = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>((const char *)c.k) + kv * 2, 0, bytes, 0x00027000);
         const auto vr = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>((const char *)c.v) + kv * 2, 0, bytes, 0x00027000);
         uint32_t row = from_row, pk = piece_k, pv = piece_v;
         fresh(row), fresh(pk), fresh(pv);
-        const auto pr = __builtin_amdgcn_make_buffer_rsrc(const_cast<int32_t *>(c.pos) + at, 0, a.causal || TURN ? n * 4 : 0, 0x00027000);
+        const auto pr = __builtin_amdgcn_make_buffer_rsrc(const_cast<int32_t *>(c.pos) + at, 0, __builtin_amdgcn_readfirstlane(a.causal || TURN ? n * 4 : 0), 0x00027000);
 #pragma unroll
         for (int i = 0; i < kKeys / 4; ++i)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, (lds_void *)(to.k + (kKeys * wave + 4 * i) * kHeadDim), 16, row + 4 * i * sb + (pk ^ (64 * i)), 0, 0, 0);
