@@ -299,11 +299,11 @@ __global__ __launch_bounds__(kAttendThreads) void join_kernel(const float *part_
 
 }  // namespace
 
-// Which kernel takes a call: the bf16 ones need pages of sixteen slots, and sixteen rows' addresses within 32 bits.
+// Which kernel takes a call: the bf16 ones need sixteen rows' addresses within 32 bits.
 enum class Kernel { general, rows, tile };
 static Kernel kernel_of(const tri_cache &c, int64_t rows)
 {
-    if (c.dtype != TRI_BF16 || (c.block_size > 0 && c.block_size < 16) || c.stride_slot >= (1 << 24)) return Kernel::general;
+    if (c.dtype != TRI_BF16 || c.stride_slot >= (1 << 24)) return Kernel::general;
     return rows <= 32 ? Kernel::rows : Kernel::tile;
 }
 

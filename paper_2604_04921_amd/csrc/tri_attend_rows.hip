@@ -36,7 +36,7 @@ __device__ __forceinline__ void rotate_row(float (*x)[8], int32_t pos, int kq, c
 // LO: columns 8 to 15 of a tile hold what the rounding to bf16 takes off the rows 0 to 7 (of q turned by its position, and of the weights): the matrix
 // instructions have that room where rows are at most eight to a tile, and both products are as good as in 16 bits of fraction.  Keys turned on the way (TURN)
 // are multiplied as two bf16 numbers for the same reason.  Without LO, q and the weights are rounded to bf16 once.
-template <int NT, bool LO, bool PAGED, bool TURN, bool HALF>
+template <int NT, bool LO, int PAGES, bool TURN, bool HALF>
 __global__ __launch_bounds__(kRowsThreads, 2) void attend_rows_kernel(AttendArgs a)
 {
     constexpr int kCols = LO ? 8 : 16, kRows = kCols * NT;
@@ -67,40 +67,66 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attend_rows_kernel(AttendArgs
     const uint32_t sb = (uint32_t)c.stride_slot * 2u;
     const bool need_pos = a.causal || TURN;
 
-    // Sixteen keys: where their rows begin and how many there are (0: none, or their block is not there).  Lanes beyond the last row lie beyond the buffer and load zeros.
+    // Sixteen keys: which of them are there (in a block that is), and where their rows begin.  Lanes beyond the last row lie beyond the buffer and load zeros.  Pages below sixteen
+    // slots have rows of their own addresses: keys that are not there load the pool's first row, and their values are cleared when they have come.
     struct Rows {
         int64_t kv, pos;
         int n;
+        uint32_t there;
     };
+    const int in_block = PAGES ? (1 << c.block_shift) - 1 : 0;
+    auto is_block = [&](int b) { return (b >= 0) & ((a.src.n_blocks == 0) | (b < a.src.n_blocks)); };
     auto find = [&](int k0, int block_loaded) {
         Rows r;
-        const int block = __builtin_amdgcn_readfirstlane(block_loaded);   // (here and not where it is asked for: that is a step ago)
         const int left = __builtin_amdgcn_readfirstlane(min(max(k_hi - k0, 0), 16));
-        if (PAGED) {
-            const int in = k0 & ((1 << c.block_shift) - 1);
-            r.n = block < 0 || (a.src.n_blocks > 0 && block >= a.src.n_blocks) ? 0 : left;
+        r.n = left;
+        r.kv = r.pos = 0;
+        if (PAGES == 2) {
+            const uint32_t l = lane_again();
+            r.there = (uint32_t)(__ballot(((int)(l & 15) < left) & is_block(block_loaded)) >> (k0 & 16)) & 0xffffu;
+            return r;
+        }
+        if (PAGES == 1) {
+            const int block = __builtin_amdgcn_readfirstlane(block_loaded);   // (here and not where it is asked for: that is a step ago)
+            const int in = k0 & in_block;
+            if (!is_block(block)) r.n = 0;
             const int b = r.n ? block : 0;
             r.kv = base + (int64_t)b * c.stride_sb + (int64_t)in * c.stride_slot;
             r.pos = pbase + (int64_t)b * c.pos_stride_sb + in;
         } else {
-            r.n = left;
             r.kv = base + (int64_t)s * c.stride_sb + (int64_t)k0 * c.stride_slot;
             r.pos = pbase + (int64_t)s * c.pos_stride_sb + k0;
         }
+        r.there = (1u << r.n) - 1;
         return r;
     };
+    // the block of key k0, or (PAGES 2) of the lane's key of the 32 from k0 on
     auto block_at = [&](int k0) {
-        return PAGED ? c.block_table[(int64_t)s * c.max_blocks + (min(k0, max(k_hi - 1, 0)) >> c.block_shift)] : 0;
+        if (PAGES == 2) k0 += lane_again() & 31;
+        return PAGES ? c.block_table[(int64_t)s * c.max_blocks + (min(k0, max(k_hi - 1, 0)) >> c.block_shift)] : 0;
     };
     auto rsrc = [&](const void *p, int64_t at, int n) {
         return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>((const char *)p) + at * 2, 0, __builtin_amdgcn_readfirstlane(n > 0 ? (n - 1) * sb + kHeadDim * 2 : 0), 0x00027000);
     };
     uint4 k[2][4], v[2][4];
     int32_t k_pos[2];
-    auto load_k = [&](const Rows (&r)[2]) {
+    // key `key` (0 to 31) of the tile from k0 on, its block being with lane `key`: the offset of its row
+    auto slot_of = [&](int k0, int key, int block) {
+        const int b = __shfl(block, key);
+        return is_block(b) & (k0 + key < k_hi) ? base + (int64_t)b * c.stride_sb + slot_offset(c, (k0 + key) & in_block) : base;
+    };
+    auto load_k = [&](const Rows (&r)[2], int k0, int block) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const uint32_t l = lane_again(), at = (l & 15) * sb + (l >> 4) * 16, at_pos = (l & 15) * 4;
+            if (PAGES == 2) {
+                const int key = 16 * i + (l & 15), b = __shfl(block, key);
+                const char *p = (const char *)c.k + slot_of(k0, key, block) * 2 + (l >> 4) * 16;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) k[i][j] = load_stream16(p + 64 * j);
+                k_pos[i] = need_pos ? c.pos[pbase + (is_block(b) & (k0 + key < k_hi) ? (int64_t)b * c.pos_stride_sb + ((k0 + key) & in_block) : 0)] : 0;
+                continue;
+            }
             const auto b = rsrc(c.k, r[i].kv, r[i].n);
 #pragma unroll
             for (int j = 0; j < 4; ++j) k[i][j] = as_uint4(__builtin_amdgcn_raw_buffer_load_b128(b, at + 64 * j, 0, kNonTemporal));
@@ -108,10 +134,15 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attend_rows_kernel(AttendArgs
             k_pos[i] = __builtin_amdgcn_raw_buffer_load_b32(p, at_pos, 0, 0);
         }
     };
-    auto load_v = [&](const Rows (&r)[2]) {
+    auto load_v = [&](const Rows (&r)[2], int k0, int block) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const uint32_t l = lane_again(), at = (l >> 4) * 4 * sb + (l & 15) * 16;
+            if (PAGES == 2) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[i][j] = load_stream16((const char *)c.v + slot_of(k0, 16 * i + 4 * (l >> 4) + j, block) * 2 + (l & 15) * 16);
+                continue;
+            }
             const auto b = rsrc(c.v, r[i].kv, r[i].n);
 #pragma unroll
             for (int j = 0; j < 4; ++j) v[i][j] = as_uint4(__builtin_amdgcn_raw_buffer_load_b128(b, at + j * sb, 0, kNonTemporal));
@@ -119,12 +150,13 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attend_rows_kernel(AttendArgs
     };
     constexpr int kStep = 4 * kRowsTile;
     int k0 = __builtin_amdgcn_readfirstlane(range.lo) + kRowsTile * wave;
-    Rows here[2] = {find(k0, block_at(k0)), find(k0 + 16, block_at(k0 + 16))};
-    int ahead[2] = {block_at(k0 + kStep), block_at(k0 + kStep + 16)};
+    int block_here = block_at(k0), block_here2 = PAGES == 1 ? block_at(k0 + 16) : block_here;
+    Rows here[2] = {find(k0, block_here), find(k0 + 16, block_here2)};
+    int ahead = block_at(k0 + kStep), ahead2 = PAGES == 1 ? block_at(k0 + kStep + 16) : ahead;
     // The first tile is asked for before anything is known of the queries: in short rows most of the time is latency.
-    load_k(here);
+    load_k(here, k0, block_here);
     __builtin_amdgcn_sched_barrier(0);   // (in this order, as in the loop: waiting for K's loads must not wait for V's)
-    load_v(here);
+    load_v(here, k0, block_here);
     if (tid < kBands) turns[tid] = a.turns.w[tid];
     __syncthreads();
 
@@ -168,9 +200,10 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attend_rows_kernel(AttendArgs
         for (int e = 0; e < 8; ++e) o[n][e] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
     for (; k0 < k_hi; k0 += kStep) {
-        const Rows next[2] = {find(k0 + kStep, ahead[0]), find(k0 + kStep + 16, ahead[1])};
-        ahead[0] = block_at(k0 + 2 * kStep);
-        ahead[1] = block_at(k0 + 2 * kStep + 16);
+        const Rows next[2] = {find(k0 + kStep, ahead), find(k0 + kStep + 16, PAGES == 1 ? ahead2 : ahead)};
+        const int block_next = ahead;
+        ahead = block_at(k0 + 2 * kStep);
+        if (PAGES == 1) ahead2 = block_at(k0 + 2 * kStep + 16);
         f32x4 sc[2][NT];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -201,7 +234,7 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attend_rows_kernel(AttendArgs
             }
         }
         const int32_t pos_here[2] = {k_pos[0], k_pos[1]};
-        load_k(next);
+        load_k(next, k0 + kStep, block_next);
         if (LO) {
 #pragma unroll
             for (int i = 0; i < 2; ++i)
@@ -216,13 +249,14 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attend_rows_kernel(AttendArgs
         bool hole = false;
 #pragma unroll
         for (int n = 0; n < NT; ++n) keep[n] = 0xffu;
-        if (late || here[0].n < 16 || here[1].n < 16) {
+        if (late || (here[0].there & here[1].there) != 0xffffu) {
             const uint32_t key = (lane_again() >> 4) * 4;
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
                 for (int d = 0; d < 4; ++d) {
-                    const bool there = (int)key + d < here[i].n;
+                    const bool there = (here[i].there >> (key + d)) & 1;
+                    if (PAGES == 2) v[i][d] = there ? v[i][d] : make_uint4(0, 0, 0, 0);
                     const int32_t p = __shfl(pos_here[i], (int)key + d);
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
@@ -303,7 +337,7 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attend_rows_kernel(AttendArgs
 #pragma unroll
             for (int n = 0; n < NT; ++n) o[n][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, weight[n], o[n][e], 0, 0, 0);
         }
-        load_v(next);
+        load_v(next, k0 + kStep, block_next);
         here[0] = next[0];
         here[1] = next[1];
     }
@@ -355,11 +389,11 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attend_rows_kernel(AttendArgs
 template <int NT, bool LO>
 void launch_rows_of(const AttendArgs &a, uint32_t blocks, hipStream_t st)
 {
-    const bool paged = a.src.cache.block_shift >= 0;
+    const int shift = a.src.cache.block_shift, pages = shift < 0 ? 0 : shift >= 4 ? 1 : 2;
     const auto launch = [&](auto kernel) { kernel<<<blocks, kRowsThreads, 0, st>>>(a); };
-    if (a.src.cache.k_rotated) launch(paged ? attend_rows_kernel<NT, LO, true, false, false> : attend_rows_kernel<NT, LO, false, false, false>);
-    else if (a.half) launch(paged ? attend_rows_kernel<NT, LO, true, true, true> : attend_rows_kernel<NT, LO, false, true, true>);
-    else launch(paged ? attend_rows_kernel<NT, LO, true, true, false> : attend_rows_kernel<NT, LO, false, true, false>);
+    if (a.src.cache.k_rotated) launch(pages == 0 ? attend_rows_kernel<NT, LO, 0, false, false> : pages == 1 ? attend_rows_kernel<NT, LO, 1, false, false> : attend_rows_kernel<NT, LO, 2, false, false>);
+    else if (a.half) launch(pages == 0 ? attend_rows_kernel<NT, LO, 0, true, true> : pages == 1 ? attend_rows_kernel<NT, LO, 1, true, true> : attend_rows_kernel<NT, LO, 2, true, true>);
+    else launch(pages == 0 ? attend_rows_kernel<NT, LO, 0, true, false> : pages == 1 ? attend_rows_kernel<NT, LO, 1, true, false> : attend_rows_kernel<NT, LO, 2, true, false>);
 }
 
 }  // namespace

@@ -12,7 +12,7 @@ typedef __attribute__((address_space(3))) void lds_void;
 
 constexpr int kWaves = 4, kRows = 32 * kWaves;   // rows of a workgroup
 constexpr int kTileKeys = 64, kKeys = kTileKeys / kWaves;   // keys of a tile, and those of them that a wave brings
-static_assert(kRows == kTileRows, "");
+static_assert(kRows == kTileRows && kKeys == 16, "");
 constexpr float kStaleBits = 8.f;   // powers of two by which a score may pass the maximum that weights are relative to
 
 // Rotates a lane's 64 elements of a row: x[c][e] is dimension 16 c + 8 h + e.
@@ -36,10 +36,10 @@ __device__ __forceinline__ void rotate_q(float (*x)[8], int32_t pos, int h, cons
 struct TileBuffer {
     __bf16 k[kTileKeys * kHeadDim], v[kTileKeys * kHeadDim];
     int32_t pos[kTileKeys];
-    int32_t lim[3 * kWaves];   // of every wave's keys: highest and lowest position, and how many there are
+    int32_t lim[3 * kWaves];   // of every wave's keys: highest and lowest position, and which are there (a bit each)
 };
 
-template <bool PAGED, bool TURN, bool HALF>
+template <int PAGES, bool TURN, bool HALF>
 __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs a)
 {
     constexpr int kLanes = 64 / kKeys, kPieces = 16 / kLanes;   // TURN: lanes to a row of K, pieces to a lane
@@ -74,17 +74,37 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
     // read of neighbouring rows, and sixteen of a transposing 8-byte read of four rows, meet different banks.
     const uint32_t row4 = lane >> 4;
     const uint32_t piece_k = ((lane & 15) ^ row4) * 16, piece_v = ((lane & 15) ^ (2 * row4)) * 16, from_row = row4 * sb;
+    const int in_block = PAGES ? (1 << c.block_shift) - 1 : 0;
+    auto is_block = [&](int b) { return (b >= 0) & ((a.src.n_blocks == 0) | (b < a.src.n_blocks)); };
+    // the block of key k0, or (PAGES 2: below sixteen slots) of the lane's key of the sixteen from k0 on
     auto block_at = [&](int k0) {
-        return PAGED ? c.block_table[(int64_t)s * c.max_blocks + (min(k0, max(k_hi - 1, 0)) >> c.block_shift)] : 0;
+        if (PAGES == 2) k0 += lane_again() & 15;
+        return PAGES ? c.block_table[(int64_t)s * c.max_blocks + (min(k0, max(k_hi - 1, 0)) >> c.block_shift)] : 0;
     };
-    int32_t pos_new = 0, n_new = 0;
+    int32_t pos_new = 0;
+    uint32_t there_new = 0;
     auto load = [&](TileBuffer &to, int k0, int block_loaded) __attribute__((always_inline)) {   // k0: this wave's first key
-        const int block = __builtin_amdgcn_readfirstlane(block_loaded);   // (here and not where it is asked for: that is a tile ago)
         int n = __builtin_amdgcn_readfirstlane(min(max(k_hi - k0, 0), kKeys));
+        if (PAGES == 2) {   // every row has an address of its own; keys that are not there bring the pool's first row, which put() clears
+            const uint32_t l = lane_again();
+            const bool mine = ((int)(l & 15) < n) & is_block(block_loaded);
+            there_new = (uint32_t)__ballot(mine) & 0xffffu;
+#pragma unroll
+            for (int i = 0; i < kKeys / 4; ++i) {
+                const int row = 4 * i + (l >> 4), b = __shfl(block_loaded, row);
+                const int64_t at = ((there_new >> row) & 1 ? base + (int64_t)b * c.stride_sb + slot_offset(c, (k0 + row) & in_block) : base) * 2;
+                typedef const __attribute__((address_space(1))) void global_void;
+                __builtin_amdgcn_global_load_lds((global_void *)((const char *)c.k + at + ((l & 15) ^ row) * 16), (lds_void *)(to.k + (kKeys * wave + 4 * i) * kHeadDim), 16, 0, 0);
+                __builtin_amdgcn_global_load_lds((global_void *)((const char *)c.v + at + ((l & 15) ^ (2 * (row & 7))) * 16), (lds_void *)(to.v + (kKeys * wave + 4 * i) * kHeadDim), 16, 0, 0);
+            }
+            pos_new = a.causal || TURN ? c.pos[pbase + (mine ? (int64_t)block_loaded * c.pos_stride_sb + ((k0 + (l & 15)) & in_block) : 0)] : 0;
+            return;
+        }
         int64_t kv, at;
-        if (PAGED) {
-            const int in = k0 & ((1 << c.block_shift) - 1);
-            if (block < 0 || (a.src.n_blocks > 0 && block >= a.src.n_blocks)) n = 0;
+        if (PAGES == 1) {
+            const int block = __builtin_amdgcn_readfirstlane(block_loaded);   // (here and not where it is asked for: that is a tile ago)
+            const int in = k0 & in_block;
+            if (!is_block(block)) n = 0;
             const int b = n ? block : 0;
             kv = base + (int64_t)b * c.stride_sb + (int64_t)in * c.stride_slot;
             at = pbase + (int64_t)b * c.pos_stride_sb + in;
@@ -92,7 +112,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
             kv = base + (int64_t)s * c.stride_sb + (int64_t)k0 * c.stride_slot;
             at = pbase + (int64_t)s * c.pos_stride_sb + k0;
         }
-        n_new = n;
+        there_new = (1u << n) - 1;
         const uint32_t bytes = __builtin_amdgcn_readfirstlane(n > 0 ? (n - 1) * sb + kHeadDim * 2 : 0);   // (lanes beyond it bring zeros)
         const auto kr = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>((const char *)c.k) + kv * 2, 0, bytes, 0x00027000);
         const auto vr = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>((const char *)c.v) + kv * 2, 0, bytes, 0x00027000);
@@ -109,6 +129,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
     };
     // What the loads have brought, when it has come: the wave's own keys are turned where they lie, their positions written down.
     auto put = [&](TileBuffer &to) __attribute__((always_inline)) {
+        if (PAGES == 2 && there_new != 0xffffu) {
+            __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0): the rows have come
+            const uint32_t l = lane_again();
+            if (!((there_new >> (l >> 2)) & 1)) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4 *>(to.v + (kKeys * wave + (l >> 2)) * kHeadDim + 8 * ((l & 3) + 4 * i)) = make_uint4(0, 0, 0, 0);
+            }
+        }
         if (TURN) {
             const int row = lane / kLanes, turn_pos = __shfl(pos_new, row);
             bf16x8 *k = reinterpret_cast<bf16x8 *>(to.k + (kKeys * wave + row) * kHeadDim);
@@ -136,12 +164,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
                 k[(lane % kLanes + kLanes * i) ^ row] = u;
             }
         }
-        const bool there = lane % kKeys < n_new;   // (lanes kKeys apart hold the same)
+        const bool there = (there_new >> (lane % kKeys)) & 1;   // (lanes kKeys apart hold the same)
         int32_t hi = there ? pos_new : -0x7fffffff - 1, lo = there ? pos_new : 0x7fffffff;
 #pragma unroll
         for (int i = 1; i < kKeys; i *= 2) hi = max(hi, __shfl_xor(hi, i)), lo = min(lo, __shfl_xor(lo, i));
         if (lane < kKeys) to.pos[kKeys * wave + lane] = pos_new;
-        if (lane == 0) to.lim[wave] = hi, to.lim[kWaves + wave] = lo, to.lim[2 * kWaves + wave] = n_new;
+        if (lane == 0) to.lim[wave] = hi, to.lim[kWaves + wave] = lo, to.lim[2 * kWaves + wave] = there_new;
     };
 
     // The first tile is asked for before anything is known of the queries.
@@ -232,16 +260,17 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
-                    const int first = 32 * u + 8 * g + 4 * h, n_there = from.lim[2 * kWaves + first / kKeys] - first % kKeys;
+                    const int first = 32 * u + 8 * g + 4 * h;
+                    const uint32_t there = (uint32_t)from.lim[2 * kWaves + first / kKeys] >> (first % kKeys);
                     const int4 p4 = *reinterpret_cast<const int4 *>(&from.pos[first]);
                     const int32_t p[4] = {p4.x, p4.y, p4.z, p4.w};
 #pragma unroll
                     for (int d = 0; d < 4; ++d) {
                         const int i = 4 * g + d;
-                        const bool on = (d < n_there) & (p[d] <= t_pos);   // (not causal: t_pos is the highest there is)
+                        const bool on = ((there >> d) & 1) & (p[d] <= t_pos);   // (not causal: t_pos is the highest there is)
                         keep &= on ? ~0u : ~(1u << (16 * u + i));
                         sc[u][i] = on ? sc[u][i] : kNoScore;
-                        hole |= (d < n_there) & !on & real;
+                        hole |= ((there >> d) & 1) & !on & real;
                     }
                 }
         }
@@ -322,12 +351,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
         }
         if (!idle) {
             const int32_t lim = here.lim[min(lane, 3 * kWaves - 1)];
-            int32_t hi = -0x7fffffff - 1, lo = 0x7fffffff, n = 0;
+            int32_t hi = -0x7fffffff - 1, lo = 0x7fffffff, any = 0, all = 0xffff;
 #pragma unroll
             for (int i = 0; i < kWaves; ++i)
-                hi = max(hi, __builtin_amdgcn_readlane(lim, i)), lo = min(lo, __builtin_amdgcn_readlane(lim, kWaves + i)), n += __builtin_amdgcn_readlane(lim, 2 * kWaves + i);
+                hi = max(hi, __builtin_amdgcn_readlane(lim, i)), lo = min(lo, __builtin_amdgcn_readlane(lim, kWaves + i)), any |= __builtin_amdgcn_readlane(lim, 2 * kWaves + i), all &= __builtin_amdgcn_readlane(lim, 2 * kWaves + i);
             // (nothing to do where no key is there, or all are behind the last position of the wave's rows)
-            if (n > 0 && lo <= last_pos) compute(here, n < kTileKeys || hi > first_pos);
+            if (any && lo <= last_pos) compute(here, all != 0xffff || hi > first_pos);
         }
         if (more) put(next);
         k0 += kTileKeys;
@@ -369,11 +398,11 @@ tri_status launch_attend_tile(AttendArgs a, int32_t rows, hipStream_t st)
     a.row_tiles = (rows + kRows - 1) / kRows;
     const int64_t groups = (int64_t)a.src.n_split * a.src.cache.n_kv_heads * a.src.cache.n_seqs;
     const uint32_t blocks = (uint32_t)((groups + 7) / 8 * 8 * a.row_tiles);
-    const bool paged = a.src.cache.block_shift >= 0;
+    const int shift = a.src.cache.block_shift, pages = shift < 0 ? 0 : shift >= 4 ? 1 : 2;
     const auto launch = [&](auto kernel) { kernel<<<blocks, 64 * kWaves, 0, st>>>(a); };
-    if (a.src.cache.k_rotated) launch(paged ? attend_tile_kernel<true, false, false> : attend_tile_kernel<false, false, false>);
-    else if (a.half) launch(paged ? attend_tile_kernel<true, true, true> : attend_tile_kernel<false, true, true>);
-    else launch(paged ? attend_tile_kernel<true, true, false> : attend_tile_kernel<false, true, false>);
+    if (a.src.cache.k_rotated) launch(pages == 0 ? attend_tile_kernel<0, false, false> : pages == 1 ? attend_tile_kernel<1, false, false> : attend_tile_kernel<2, false, false>);
+    else if (a.half) launch(pages == 0 ? attend_tile_kernel<0, true, true> : pages == 1 ? attend_tile_kernel<1, true, true> : attend_tile_kernel<2, true, true>);
+    else launch(pages == 0 ? attend_tile_kernel<0, true, false> : pages == 1 ? attend_tile_kernel<1, true, false> : attend_tile_kernel<2, true, false>);
     return hip_status("attend_tile_kernel");
 }
 
