@@ -29,33 +29,21 @@ __device__ __forceinline__ void load4<__bf16>(const char *p, float *x)
     x[2] = __uint_as_float(u.y << 16), x[3] = __uint_as_float(u.y & 0xffff0000u);
 }
 // Rotates a lane's 32 elements of a row: x[c][e] is dimension 16 c + 4 kq + e, so both parts of a band lie in one lane in either pair layout.
-__device__ __forceinline__ void rotate32(float (*x)[4], int32_t pos, int kq, int half, const uint64_t *turns)
+template <bool HALF>
+__device__ __forceinline__ void rotate32(float (*x)[4], int32_t pos, int kq, const uint64_t *turns)
 {
-    if (half) {
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
+    for (int c = 0; c < (HALF ? 4 : 8); ++c)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const uint64_t w = turns[16 * c + 4 * kq + e];
-                float cs, sn;
-                turn_exact(phase_of(pos, (uint32_t)w, (uint32_t)(w >> 32)), &cs, &sn);
-                const float re = x[c][e], im = x[c + 4][e];
-                x[c][e] = fmaf(re, cs, -(im * sn));
-                x[c + 4][e] = fmaf(re, sn, im * cs);
-            }
-    } else {
-#pragma unroll
-        for (int c = 0; c < 8; ++c)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const uint64_t w = turns[8 * c + 2 * kq + e];
-                float cs, sn;
-                turn_exact(phase_of(pos, (uint32_t)w, (uint32_t)(w >> 32)), &cs, &sn);
-                const float re = x[c][2 * e], im = x[c][2 * e + 1];
-                x[c][2 * e] = fmaf(re, cs, -(im * sn));
-                x[c][2 * e + 1] = fmaf(re, sn, im * cs);
-            }
-    }
+        for (int e = 0; e < (HALF ? 4 : 2); ++e) {
+            const uint64_t w = turns[HALF ? 16 * c + 4 * kq + e : 8 * c + 2 * kq + e];
+            float cs, sn;
+            turn_exact(phase_of(pos, (uint32_t)w, (uint32_t)(w >> 32)), &cs, &sn);
+            float &r = HALF ? x[c][e] : x[c][2 * e], &i = HALF ? x[(c + 4) & 7][e] : x[c][(2 * e + 1) & 3];
+            const float re = r, im = i;
+            r = fmaf(re, cs, -(im * sn));
+            i = fmaf(re, sn, im * cs);
+        }
 }
 
 // One wave takes 16 keys at a time against 16 rows.  S^T[key][row] = K Q^T and O^T[dim][row] = V^T P^T run on v_mfma_f32_16x16x4_f32, whose lane (m = lane & 15,
@@ -64,8 +52,8 @@ __device__ __forceinline__ void rotate32(float (*x)[4], int32_t pos, int kq, int
 // S^T leaves key 4 kq + i of row (lane & 15) in register i, which is where the second product wants it: no data crosses lanes but the
 // maximum and, at the end, the sum over kq.  The maximum is that of the products before the scale, which their differences are multiplied
 // by (a score of 30 powers of two rounded as such is off by 2^-20).  The workgroup's four waves take every fourth tile of the range and join in LDS.
-template <typename T>
-__global__ __launch_bounds__(kAttendThreads) void attend_general_kernel(AttendArgs a)
+template <typename T, bool TURN, bool HALF>
+__global__ __launch_bounds__(kAttendThreads, 2) void attend_general_kernel(AttendArgs a)
 {
     __shared__ uint64_t turns[kBands];
     __shared__ float wave_m[4][kRowTile], wave_l[4][kRowTile];
@@ -95,12 +83,18 @@ __global__ __launch_bounds__(kAttendThreads) void attend_general_kernel(AttendAr
     const int r = min(r0 + m, rows - 1), t = tr.t0 + r / G, hq = h * G + r % G;
     const bool real = r0 + m < rows;
     const int32_t t_pos = a.pos ? a.pos[t] : 0;
+    int32_t first_pos = t_pos;
+#pragma unroll
+    for (int i = 1; i < 16; i *= 2) first_pos = min(first_pos, __shfl_xor(first_pos, i));
     float q[8][4];
     {
         const char *p = a.q + ((int64_t)t * a.q_stride_token + (int64_t)hq * a.q_stride_head) * (int64_t)sizeof(T);
 #pragma unroll
         for (int j = 0; j < 8; ++j) load4<T>(p + (16 * j + 4 * kq) * sizeof(T), q[j]);
-        if (a.rotate_q) rotate32(q, t_pos, kq, a.half, turns);
+        if (a.rotate_q) {
+            if (TURN ? HALF : (bool)a.half) rotate32<true>(q, t_pos, kq, turns);
+            else rotate32<false>(q, t_pos, kq, turns);
+        }
     }
     f32x4 o[8];
 #pragma unroll
@@ -109,49 +103,61 @@ __global__ __launch_bounds__(kAttendThreads) void attend_general_kernel(AttendAr
     const int64_t base = (int64_t)a.layer * c.stride_layer + (int64_t)h * c.stride_head;
     const int64_t pbase = (int64_t)a.layer * c.pos_stride_layer + (int64_t)h * c.pos_stride_head;
     const int in_block = c.block_shift < 0 ? 0x7fffffff : (1 << c.block_shift) - 1;
-    for (int k0 = k_lo + 16 * wave; k0 < k_hi; k0 += 64) {
-        // lane: key k0 + m of the tile for K, its position and whether it is there
-        const int key = k0 + m;
-        int b = key < k_hi ? s : -1;
-        if (b >= 0 && c.block_shift >= 0) b = block_of(c, a.src.n_blocks, s, key);
-        const int at = key & in_block;
-        float k[8][4];
-        int32_t k_pos = 0;
+    // A lane's key of a tile is k0 + m.  Its block, or -1 where it is not there (keys of which the pool's first block is read instead).
+    auto block_at = [&](int k0) { return c.block_shift < 0 || k_hi == 0 ? s : block_of(c, a.src.n_blocks, s, min(k0 + m, k_hi - 1)); };
+    auto there_at = [&](int k0, int block) { return (k0 + m < k_hi) & (block >= 0); };
+    auto slot_at = [&](int key) { return min(key, max(k_hi - 1, 0)) & in_block; };
+    float k[8][4], v[4][2][4];
+    int32_t k_pos = 0;
+    auto load_k = [&](int k0, int block) {
+        const int at = slot_at(k0 + m);
+        const char *p = (const char *)c.k + row_of(c, base, max(block, 0), at) * (int64_t)sizeof(T);
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
+        for (int j = 0; j < 8; ++j) load4<T>(p + (16 * j + 4 * kq) * sizeof(T), k[j]);
+        k_pos = a.causal || TURN ? c.pos[pbase + (int64_t)max(block, 0) * c.pos_stride_sb + at] : 0;
+    };
+    auto load_v = [&](int k0, int block) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) k[j][e] = 0.f;
-        if (b >= 0) {
-            const char *p = (const char *)c.k + row_of(c, base, b, at) * (int64_t)sizeof(T);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) load4<T>(p + (16 * j + 4 * kq) * sizeof(T), k[j]);
-            if (a.causal || !c.k_rotated) k_pos = c.pos[pbase + (int64_t)b * c.pos_stride_sb + at];
-            if (!c.k_rotated) rotate32(k, k_pos, kq, a.half, turns);
+        for (int i = 0; i < 4; ++i) {
+            const int from = 4 * kq + i;
+            const char *p = (const char *)c.v + row_of(c, base, max(__shfl(block, from), 0), slot_at(k0 + from)) * (int64_t)sizeof(T);
+            load4<T>(p + 4 * m * sizeof(T), v[i][0]);
+            load4<T>(p + (64 + 4 * m) * sizeof(T), v[i][1]);
         }
+    };
+    int k0 = k_lo + 16 * wave, block = block_at(k0), ahead = block_at(k0 + 64);
+    if (k0 < k_hi) {
+        load_k(k0, block);
+        __builtin_amdgcn_sched_barrier(0);
+        load_v(k0, block);
+    }
+    for (; k0 < k_hi; k0 += 64) {
+        if (TURN) rotate32<HALF>(k, k_pos, kq, turns);
         f32x4 sc = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < 8; ++j)
 #pragma unroll
             for (int e = 0; e < 4; ++e) sc = __builtin_amdgcn_mfma_f32_16x16x4f32(k[j][e], q[j][e], sc, 0, 0, 0);
-        // the keys this lane has scores of (and whose V rows it loads): 4 kq + i
-        bool keep[4];
-        float v[4][2][4];
+        // the keys this lane has scores of (and whose V rows it has): 4 kq + i
+        const bool there = there_at(k0, block);
+        const int32_t pos_here = k_pos;
+        const uint32_t there_bits = (uint32_t)__ballot(there) & 0xffffu;
+        const int block_next = ahead;
+        load_k(k0 + 64, block_next);   // (beyond the last tile: its last key again)
+        ahead = block_at(k0 + 128);
+        bool keep[4] = {true, true, true, true};
         bool hole = false, odd = false;
+        if (there_bits != 0xffffu || (a.causal && __ballot(pos_here > first_pos))) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int from = 4 * kq + i;
-            const int vb = __shfl(b, from);
-            const int32_t vp = __shfl(k_pos, from);
-            keep[i] = vb >= 0 && (!a.causal || vp <= t_pos);
-            hole |= real && vb >= 0 && !keep[i];
+            for (int i = 0; i < 4; ++i) {
+                const bool on = (there_bits >> (4 * kq + i)) & 1;
+                const int32_t vp = __shfl(pos_here, 4 * kq + i);
+                keep[i] = on && (!a.causal || vp <= t_pos);
+                hole |= real && on && !keep[i];
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
+                for (int j = 0; j < 2; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[i][j][e] = 0.f;
-            if (vb >= 0) {
-                const char *p = (const char *)c.v + row_of(c, base, vb, (k0 + from) & in_block) * (int64_t)sizeof(T);
-                load4<T>(p + 4 * m * sizeof(T), v[i][0]);
-                load4<T>(p + (64 + 4 * m) * sizeof(T), v[i][1]);
+                    for (int e = 0; e < 4; ++e) v[i][j][e] = on ? v[i][j][e] : 0.f;
             }
         }
         float best = kNoScore;
@@ -162,12 +168,15 @@ __global__ __launch_bounds__(kAttendThreads) void attend_general_kernel(AttendAr
         }
         best = fmaxf(best, __shfl_xor(best, 16));
         best = fmaxf(best, __shfl_xor(best, 32));
-        const float next = fmaxf(top, best), ref = next == kNoScore ? 0.f : next;
-        const float shrink = __builtin_amdgcn_exp2f((top - ref) * a.scale_log2);   // (no score yet: 2^-inf = 0)
-        top = next;
-        sum *= shrink;
+        if (__ballot(best > top)) {   // (rare after the first tiles)
+            const float next = fmaxf(top, best);
+            const float shrink = next == kNoScore ? 1.f : __builtin_amdgcn_exp2f((top - next) * a.scale_log2);   // (no score yet: 2^-inf = 0)
+            top = next;
+            sum *= shrink;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) o[j] *= shrink;
+            for (int j = 0; j < 8; ++j) o[j] *= shrink;
+        }
+        const float ref = top == kNoScore ? 0.f : top;
         float p[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -198,6 +207,7 @@ __global__ __launch_bounds__(kAttendThreads) void attend_general_kernel(AttendAr
                         }
 #pragma unroll
                         for (int d = 0; d < 4; ++d) o[4 * j + e][d] += (up[d] > 0.f ? __builtin_inff() : 0.f) + (down[d] > 0.f ? -__builtin_inff() : 0.f);
+                        __builtin_amdgcn_sched_barrier(0);   // (one after the other: few registers, and time does not matter here)
                     }
             }
         }
@@ -207,6 +217,8 @@ __global__ __launch_bounds__(kAttendThreads) void attend_general_kernel(AttendAr
             for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[4 * j + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[i][j][e], p[i], o[4 * j + e], 0, 0, 0);
+        load_v(k0 + 64, block_next);
+        block = block_next;
     }
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
@@ -334,8 +346,11 @@ tri_status launch_attend(AttendArgs a, const tri_cache &c, hipStream_t st)
     if (kernel == Kernel::tile) return launch_attend_tile(a, (int32_t)rows, st);
     a.row_tiles = (int32_t)((rows + kRowTile - 1) / kRowTile);
     const int64_t blocks = (int64_t)a.row_tiles * a.src.n_split * a.src.cache.n_kv_heads * a.src.cache.n_seqs;
-    if (c.dtype == TRI_BF16) attend_general_kernel<__bf16><<<(uint32_t)blocks, kAttendThreads, 0, st>>>(a);
-    else attend_general_kernel<float><<<(uint32_t)blocks, kAttendThreads, 0, st>>>(a);
+    const auto launch = [&](auto kernel) { kernel<<<(uint32_t)blocks, kAttendThreads, 0, st>>>(a); };
+    const bool bf16 = c.dtype == TRI_BF16;
+    if (c.k_rotated) launch(bf16 ? attend_general_kernel<__bf16, false, false> : attend_general_kernel<float, false, false>);
+    else if (a.half) launch(bf16 ? attend_general_kernel<__bf16, true, true> : attend_general_kernel<float, true, true>);
+    else launch(bf16 ? attend_general_kernel<__bf16, true, false> : attend_general_kernel<float, true, false>);
     return hip_status("attend_general_kernel");
 }
 

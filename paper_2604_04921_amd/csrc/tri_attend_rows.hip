@@ -35,7 +35,7 @@ __device__ __forceinline__ void rotate_row(float (*x)[8], int32_t pos, int kq, c
 // or between lanes until the end but the maximum, so waves run on their own, 16 KB of loads under way each, and what bounds the kernel is the cache's bytes.
 // LO: columns 8 to 15 of a tile hold what the rounding to bf16 takes off the rows 0 to 7 (of q turned by its position, and of the weights): the matrix
 // instructions have that room where rows are at most eight to a tile, and both products are as good as in 16 bits of fraction.  Keys turned on the way (TURN)
-// are multiplied as two bf16 numbers for the same reason.  Without LO, q and the weights are rounded to bf16 once.
+// are multiplied as two bf16 numbers for the same reason.  Without LO what is taken off q lies in LDS and is multiplied on its own, and the weights are rounded to bf16 once.
 template <int NT, bool LO, int PAGES, bool TURN, bool HALF>
 __global__ __launch_bounds__(kRowsThreads, 2) void attend_rows_kernel(AttendArgs a)
 {
@@ -43,6 +43,7 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attend_rows_kernel(AttendArgs
     __shared__ __align__(16) uint64_t turns[kBands];
     __shared__ float wave_m[4][kRows], wave_l[4][kRows];
     __shared__ __align__(16) float wave_o[4][kRows][kHeadDim + 4];
+    __shared__ __align__(16) bf16x8 q_low[LO ? 1 : NT][4][64];   // what rounding takes off the rows, as operands
     const CacheView &c = a.src.cache;
     const int H = c.n_kv_heads, G = a.group_size, Hq = H * G;
     uint32_t w = blockIdx.x;
@@ -184,8 +185,19 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attend_rows_kernel(AttendArgs
             for (int e = 0; e < 8; ++e) {
                 const __bf16 hi = (__bf16)x[j][e];
                 q[n][j][e] = LO && m >= 8 ? (__bf16)(x[j][e] - (float)hi) : hi;
+                x[j][e] -= (float)hi;
             }
+        if (!LO && a.rotate_q && wave == 0) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                bf16x8 low;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) low[e] = (__bf16)x[j][e];
+                q_low[n][j][lane] = low;
+            }
+        }
     }
+    if (!LO) __syncthreads();
 #pragma unroll
     for (int x = 1; x < 16; x *= 2) first_pos = min(first_pos, __shfl_xor(first_pos, x));
     first_pos = __builtin_amdgcn_readfirstlane(first_pos);
@@ -223,6 +235,7 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attend_rows_kernel(AttendArgs
                     for (int n = 0; n < NT; ++n) {
                         sc[i][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi, q[n][j], sc[i][n], 0, 0, 0);
                         sc[i][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lo, q[n][j], sc[i][n], 0, 0, 0);
+                        if (!LO && a.rotate_q) sc[i][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi, q_low[n][j][lane], sc[i][n], 0, 0, 0);
                     }
                 }
             } else {
@@ -232,6 +245,16 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attend_rows_kernel(AttendArgs
                     for (int n = 0; n < NT; ++n)
                         sc[i][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[i][j]), q[n][j], sc[i][n], 0, 0, 0);
             }
+        }
+        if (!LO && !TURN && a.rotate_q) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const bf16x8 low = q_low[n][j][lane];
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) sc[i][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[i][j]), low, sc[i][n], 0, 0, 0);
+                }
         }
         const int32_t pos_here[2] = {k_pos[0], k_pos[1]};
         load_k(next, k0 + kStep, block_next);
