@@ -319,21 +319,26 @@ static Kernel kernel_of(const tri_cache &c, int64_t rows)
     return rows <= 32 ? Kernel::rows : Kernel::tile;
 }
 
-// Parts.  A workgroup of the rows kernel runs two to a CU, so 512 of them fill the GPU, and more even out ragged batches; each costs about what 200 keys do, and the joining of its
-// results (us by parts per head, 8 KV heads, G = 4: 16 x 65536 keys 1023 / 630 / 642 / 637 / 661 / 850 at 1, 2, 8, 16, 48, 128 parts; 16 sequences between 1000 and 65536 keys 938 / 526 /
-// 438 / 399 / 418 / 523; 16 x 4096 69 / 49 / 61 / 71 at 1, 2, 8, 16; 64 x 2176 90 / 98 / 143 at 1, 2, 8; one of 131072 at G = 8 201 / 114 / 96 / 107 at 16, 32, 64, 128).  So: 512 workgroups, or parts of 2800 keys where that
-// makes more; none below the keys that `least` gives, which the device goes by where the lengths turn out shorter than max_seq_len.
+// Parts.  Two workgroups of either bf16 kernel share a CU, so 512 of them fill the GPU; more even out ragged batches, and each costs what 100 to 200 keys do, and the joining of its
+// results.  Measured, us by parts per head, 8 KV heads, G = 4, bf16 single tokens: 16 x 65536 keys 1023 / 630 / 642 / 637 / 661 / 850 at 1, 2, 8, 16, 48, 128 parts; 16 sequences between
+// 1000 and 65536 keys 938 / 526 / 438 / 399 / 418 / 523 at the same; 16 x 4096 69 / 49 / 61 / 71 at 1, 2, 8, 16; 64 x 2176 90 / 98 / 143 at 1, 2, 8; one of 131072 at G = 8 201 / 114 / 96 /
+// 107 at 16, 32, 64, 128.  fp32: 4 x 30238 1025 / 287 / 178 / 184 at 1, 4, 16, 64; 16 between 300 and 2176 92 / 57 / 51 / 47 / 55 at 1, 2, 3, 4, 8.  The tile kernel: 64 sequences behind 32768 keys
+// 1253 / 351 / 133 / 111 at 1, 4, 16, 32; two chunks of 1024 tokens over 8192 keys, 480 row tiles, 321 / 364 / 387 at 1, 2, 4; one of 512 over 16384 400 / 201 / 169 / 182 at 1, 3, 4, 8.
+// So: 512 workgroups, or parts of 2800 keys (1400 in fp32, 8192 for row tiles) where that makes more; none below the keys that `least` gives, which the device goes by where the lengths
+// turn out shorter than max_seq_len.
 void attend_split(const tri_model &m, const tri_cache &c, int32_t max_tokens, int32_t n_tokens, int32_t *n_split, int32_t *least_keys)
 {
-    const int64_t rows = (int64_t)max_tokens * (m.n_q_heads / m.n_kv_heads);
+    const int64_t G = m.n_q_heads / m.n_kv_heads, rows = max_tokens * G;
     const Kernel kernel = kernel_of(c, rows);
     const int64_t per_tile = kernel == Kernel::general ? kRowTile : kernel == Kernel::rows ? 32 : kTileRows;
-    // row tiles that there are: at least one per sequence, and all tokens' rows
-    const int64_t tiles = std::max<int64_t>(c.n_seqs, ((int64_t)n_tokens * (m.n_q_heads / m.n_kv_heads) + per_tile - 1) / per_tile);
-    const int64_t units = m.n_kv_heads * (kernel == Kernel::rows ? c.n_seqs : tiles);
-    const int64_t part = kernel == Kernel::tile ? 8192 : kPartKeys;
+    // row tiles that there are: all tokens' rows, and half a tile more per sequence, whose last one is not full
+    const int64_t tiles = kernel == Kernel::rows ? c.n_seqs : std::max<int64_t>(c.n_seqs, (n_tokens * G + per_tile - 1) / per_tile + c.n_seqs / 2);
+    const int64_t units = m.n_kv_heads * tiles;
+    const int64_t part = kernel == Kernel::tile ? 8192 : c.dtype == TRI_F32 ? kPartKeys / 2 : kPartKeys;
     const int64_t least = kernel == Kernel::tile ? 256 : std::min<int64_t>(part, std::max<int64_t>(128, part * units / 256));
-    const int64_t want = std::max<int64_t>((512 + units / 2) / units, c.max_seq_len / part);
+    const int64_t fill = std::max<int64_t>(1, (512 + units / 2) / units);
+    int64_t want = std::max<int64_t>(fill, c.max_seq_len / part);
+    if (want * units < 2048) want = want / fill * fill;   // (few rounds: whole ones; 4 x 30238 keys in fp32 178 us with 16 parts, 210 with 21)
     *least_keys = (int32_t)least;
     *n_split = (int32_t)std::max<int64_t>(1, std::min<int64_t>({want, (c.max_seq_len + least - 1) / least, 256}));
 }

@@ -234,6 +234,21 @@ def test_offsets_beyond_32_bits(tokens, block):
     check(run(B, c), c.want(roundings=roundings(c)))
 
 
+@pytest.mark.parametrize("tokens", [1, 20, 70])
+@pytest.mark.parametrize("stored", [False, True], ids=["pre", "post"])
+def test_slots_far_apart(tokens, stored):
+    """Slots 2^24 elements apart and more: rows whose addresses 32 bits do not hold (the general kernel, in bf16)."""
+    from paper_2604_04921_amd import binding as B
+    c = P.Case(52, (30,), (tokens,), H=2, layers=1, layer=0, stored_rotated=stored, pairs=int(stored))
+    n, apart = c.own["cap"], 1 << 24
+    k, v = (torch.empty((n, apart), dtype=torch.bfloat16, device="cuda") for _ in range(2))   # (only the slots' rows of it are touched)
+    for to, f in ((k, "k_gpu"), (v, "v_gpu")):
+        to[:, :256] = c.own[f][0, 0].transpose(0, 1).reshape(n, 256)
+    strided = [t.as_strided((1, 1, 2, n, 128), (0, 0, 128, apart, 1)) for t in (k, v)]
+    c.own.update(k_gpu=strided[0], v_gpu=strided[1])
+    check(run(B, c), c.want(roundings=roundings(c)))
+
+
 def test_graph_replays():
     """A step's append and attention captured once and replayed, with eager work between the replays."""
     from paper_2604_04921_amd import binding as B
