@@ -250,56 +250,57 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_general_kernel(Atten
     finish_row<T>(a, split, tr.t0 + (r0 + row) / G, h * G + (r0 + row) % G, Hq, d0, best, total, x);
 }
 
-// Joins the parts of a row: sixteen threads have 8 dimensions each, and SPREAD such groups of a workgroup's sixteen share a row's parts.  Sixteen where parts are many (their
-// sums are then added in LDS): one group alone walks 256 parts of a long cache one memory latency after the other.
+// Joins the parts of a row: sixteen threads have 8 dimensions each, and SPREAD such groups of a workgroup's sixteen share a row's parts, each going through its own in one pass
+// with a running maximum; the groups are joined in LDS.  Sixteen where parts are many: one group alone walks 256 parts of a long cache one memory latency after the other.
 template <typename T, int SPREAD>
-__global__ __launch_bounds__(kAttendThreads) void join_kernel(const float *part_o, const float2 *part_ml, char *out, int64_t out_stride_token,
-                                                              int64_t out_stride_head, int32_t n_q_heads, int64_t n_rows, int32_t parts, float scale_log2)
+__global__ __launch_bounds__(kAttendThreads, 6) void join_kernel(const float *part_o, const float2 *part_ml, char *out, int64_t out_stride_token,
+                                                                 int64_t out_stride_head, int32_t n_q_heads, int64_t n_rows, int32_t parts, float scale_log2)
 {
-    __shared__ float most[SPREAD > 1 ? kAttendThreads / 64 : 1], totals[SPREAD > 1 ? SPREAD : 1];
+    __shared__ float tops[SPREAD], totals[SPREAD];
     __shared__ __align__(16) float sums[SPREAD > 1 ? SPREAD : 1][kHeadDim];
     const int tid = threadIdx.x, group = tid >> 4, d0 = 8 * (tid & 15), first = SPREAD > 1 ? group : 0;
     const int64_t row = SPREAD > 1 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * (kAttendThreads / 16) + group;
     if (row >= n_rows) return;   // (SPREAD: never)
-    float best = kNoScore;
-    if (SPREAD > 1) {
-        for (int p = tid; p < parts; p += kAttendThreads) best = fmaxf(best, part_ml[p * n_rows + row].x);
+    float top = kNoScore, total = 0.f, x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int p0 = first; p0 < parts; p0 += 2 * SPREAD) {
+        float2 ml[2];
+        f32x4 o[2][2];
 #pragma unroll
-        for (int x = 1; x < 64; x *= 2) best = fmaxf(best, __shfl_xor(best, x));
-        if ((tid & 63) == 0) most[tid >> 6] = best;
-        __syncthreads();
+        for (int i = 0; i < 2; ++i) {   // (a part without a key is read like any other, whatever its sums hold)
+            const int64_t at = min(p0 + i * SPREAD, parts - 1) * n_rows + row;
+            ml[i] = part_ml[at];
+            const f32x4 *po = reinterpret_cast<const f32x4 *>(part_o + at * kHeadDim + d0);
+            o[i][0] = po[0], o[i][1] = po[1];
+        }
 #pragma unroll
-        for (int j = 0; j < kAttendThreads / 64; ++j) best = fmaxf(best, most[j]);
-    } else {
-        for (int p = 0; p < parts; ++p) best = fmaxf(best, part_ml[p * n_rows + row].x);
-    }
-    float total = 0.f, x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    const float ref = best == kNoScore ? 0.f : best;
-#pragma unroll 4
-    for (int p = first; p < parts; p += SPREAD) {
-        const float2 ml = part_ml[p * n_rows + row];
-        if (ml.y != 0.f) {   // (a part without a key has nothing to bring)
-            const float f = __builtin_amdgcn_exp2f((ml.x - ref) * scale_log2);
-            total += f * ml.y;
-            const f32x4 *po = reinterpret_cast<const f32x4 *>(part_o + (p * n_rows + row) * kHeadDim + d0);
-            const f32x4 lo = po[0], hi = po[1];
+        for (int i = 0; i < 2; ++i) {
+            if (p0 + i * SPREAD >= parts || ml[i].y == 0.f) continue;   // (no key: nothing to bring)
+            const float next = fmaxf(top, ml[i].x), ref = next == kNoScore ? 0.f : next;
+            const float old = __builtin_amdgcn_exp2f((top - ref) * scale_log2), f = __builtin_amdgcn_exp2f((ml[i].x - ref) * scale_log2);
+            top = next;
+            total = total * old + f * ml[i].y;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] += f * lo[e], x[4 + e] += f * hi[e];
+            for (int e = 0; e < 8; ++e) x[e] = x[e] * old + f * o[i][e / 4][e % 4];
         }
     }
     if (SPREAD > 1) {
         store8(&sums[group][d0], x);
-        if (d0 == 0) totals[group] = total;
+        if (d0 == 0) tops[group] = top, totals[group] = total;
         __syncthreads();
         if (group > 0) return;
+        float best = kNoScore;
+#pragma unroll
+        for (int j = 0; j < SPREAD; ++j) best = fmaxf(best, tops[j]);
+        const float ref = best == kNoScore ? 0.f : best;
         total = 0.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = 0.f;
-#pragma unroll
+#pragma unroll 4
         for (int j = 0; j < SPREAD; ++j) {
-            total += totals[j];
+            const float f = __builtin_amdgcn_exp2f((tops[j] - ref) * scale_log2);
+            total += f * totals[j];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] += sums[j][d0 + e];
+            for (int e = 0; e < 8; ++e) x[e] += f * sums[j][d0 + e];
         }
     }
     const float inv = 1.f / total;

@@ -247,12 +247,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
 #pragma unroll
             for (int j = 0; j < 8; ++j) k[u][j] = *reinterpret_cast<const bf16x8 *>((const char *)from.k + (ak ^ (32 * j)) + 32 * 256 * u);
         __builtin_amdgcn_sched_barrier(0);   // all reads under way before the first product waits for one
+        __builtin_amdgcn_s_setprio(1);   // (the products of a wave go before the other's softmax: 263 -> 258 us for two chunks of 1024 tokens over 8192 keys)
 #pragma unroll
         for (int j = 0; j < 8; ++j) sc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[0][j], q[j], sc[0], 0, 0, 0);
         values(0);   // asked for ahead of the softmax
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int j = 0; j < 8; ++j) sc[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[1][j], q[j], sc[1], 0, 0, 0);
+        __builtin_amdgcn_s_setprio(0);
         uint32_t keep = ~0u;   // bit 16 u + i: key 32 u + 8 (i / 4) + 4 h + i % 4 is attended to
         bool hole = false;
         if (mask) {
