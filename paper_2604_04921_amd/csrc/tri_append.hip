@@ -61,7 +61,9 @@ struct Piece<__bf16> {
 // A thread takes two 16-byte pieces of one K row and of its V row, half a row apart: both parts of its bands lie in them in either
 // pair layout.  Pure streaming: a row is read and written once; the rotation (a sincos per band and row) is not what bounds it.
 // A wave covers 8 (bf16) or 4 (fp32) neighbouring rows; the sequence of its first token is found by all lanes at once (the number of
-// starts at or below it), the others' by going on from there.
+// starts at or below it), the others' by going on from there.  The rows are asked for before that: 19972 tokens of four prompts, 8 KV heads, 164 MB read and written, take
+// 28.5 us (5.7 TB/s; 37 with the loads behind the search); non-temporal loads take 34, the rows coming out of a product that has just written them.  A single
+// token's launch takes 3.2 us, 256 sequences' 5.1.
 template <typename T>
 __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a)
 {

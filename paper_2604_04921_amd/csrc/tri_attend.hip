@@ -52,6 +52,8 @@ __device__ __forceinline__ void rotate32(float (*x)[4], int32_t pos, int kq, con
 // S^T leaves key 4 kq + i of row (lane & 15) in register i, which is where the second product wants it: no data crosses lanes but the
 // maximum and, at the end, the sum over kq.  The maximum is that of the products before the scale, which their differences are multiplied
 // by (a score of 30 powers of two rounded as such is off by 2^-20).  The workgroup's four waves take every fourth tile of the range and join in LDS.
+// Takes fp32 caches, and bf16 ones whose slots lie 2^24 elements apart or more.  fp32, 8 KV heads, G = 4: four sequences of 30238 keys 178 us (5.6 TB/s), pre-RoPE 184; chunks of 256 tokens over 4352 keys, two
+// sequences, 315 us, 77 TFLOP/s of the 153 that a library product reaches.
 template <typename T, bool TURN, bool HALF>
 __global__ __launch_bounds__(kAttendThreads, 2) void attend_general_kernel(AttendArgs a)
 {
