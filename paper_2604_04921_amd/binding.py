@@ -129,7 +129,8 @@ def _p(t):
 
 def _stream(stream):
     if stream is None:
-        stream = torch.cuda.current_stream()
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # (the current stream's handle without an object around it: 1 us of a call)
+        return ctypes.c_void_p(raw(-1) if raw is not None else torch.cuda.current_stream().cuda_stream)
     return ctypes.c_void_p(stream.cuda_stream)
 
 

@@ -8,7 +8,6 @@ namespace tri {
 
 namespace {
 
-constexpr int kRowTile = 16;        // rows (token, query head of the group) of a workgroup of the general kernel
 constexpr int kAttendThreads = 256;
 constexpr int64_t kPartKeys = 2800;
 
@@ -46,62 +45,73 @@ __device__ __forceinline__ void rotate32(float (*x)[4], int32_t pos, int kq, con
         }
 }
 
-// One wave takes 16 keys at a time against 16 rows.  S^T[key][row] = K Q^T and O^T[dim][row] = V^T P^T run on v_mfma_f32_16x16x4_f32, whose lane (m = lane & 15,
+// One wave takes 16 keys at a time against NT times 16 rows.  S^T[key][row] = K Q^T and O^T[dim][row] = V^T P^T run on v_mfma_f32_16x16x4_f32, whose lane (m = lane & 15,
 // kq = lane >> 4) holds one element of either operand: contractions may take their terms in any order, so a lane feeds the four dimensions (QK) of a 16-byte piece of
 // its key's row in turn, and O's rows are numbered so that the V rows it loads whole are operands as they are (dimension 64 b + 4 m + e is row m of tile (b, e)).
 // S^T leaves key 4 kq + i of row (lane & 15) in register i, which is where the second product wants it: no data crosses lanes but the
 // maximum and, at the end, the sum over kq.  The maximum is that of the products before the scale, which their differences are multiplied
 // by (a score of 30 powers of two rounded as such is off by 2^-20).  The workgroup's four waves take every fourth tile of the range and join in LDS.
-// Takes fp32 caches, and bf16 ones whose slots lie 2^24 elements apart or more.  fp32, 8 KV heads, G = 4: four sequences of 30238 keys 178 us (5.6 TB/s), pre-RoPE 184; chunks of 256 tokens over 4352 keys, two
-// sequences, 315 us, 77 TFLOP/s of the 153 that a library product reaches.
-template <typename T, bool TURN, bool HALF>
-__global__ __launch_bounds__(kAttendThreads, 2) void attend_general_kernel(AttendArgs a)
+// Takes fp32 caches, and bf16 ones whose slots lie 2^24 elements apart or more.  fp32, 8 KV heads, G = 4: four sequences of 30238 keys 175 us (5.7 TB/s), pre-RoPE 184; chunks of 256 tokens over 4352 keys, two
+// sequences, 295 us, 83 TFLOP/s of the 153 that a library product reaches (317 with the row tiles of a head on all XCDs).
+template <typename T, int NT, bool TURN, bool HALF>
+__global__ __launch_bounds__(kAttendThreads, NT == 1 ? 2 : 1) void attend_general_kernel(AttendArgs a)
 {
+    constexpr int kRows = 16 * NT;
     __shared__ uint64_t turns[kBands];
-    __shared__ float wave_m[4][kRowTile], wave_l[4][kRowTile];
-    __shared__ __align__(16) float wave_o[4][kRowTile][kHeadDim + 4];
+    __shared__ float wave_m[4][kRows], wave_l[4][kRows];
+    __shared__ __align__(16) float wave_o[4][kRows][kHeadDim + 4];
     const CacheView &c = a.src.cache;
     const int H = c.n_kv_heads, G = a.group_size, Hq = H * G;
-    uint32_t w = blockIdx.x;
-    const int rt = w % a.row_tiles;
-    w /= a.row_tiles;
+    // row tiles of the same keys next to each other on one XCD, as in attend_tile_kernel
+    const uint32_t y = blockIdx.x >> 3;
+    const int rt = y % a.row_tiles;
+    uint32_t w = (y / a.row_tiles) * 8 + (blockIdx.x & 7);
     const int split = w % a.src.n_split;
     w /= a.src.n_split;
     const int h = w % H, s = w / H;
-    const TokenRange tr = tokens_of(a, s);
-    const int rows = tr.n * G, r0 = rt * kRowTile;
+    if (s >= c.n_seqs) return;
+    const TokenRange tr = tokens_of(a, a.src, s);
+    const int rows = tr.n * G, r0 = rt * kRows;
     if (r0 >= rows) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane & 15, kq = lane >> 4;
     if (tid < kBands) turns[tid] = a.turns.w[tid];
     __syncthreads();
-    const KeyRange range = keys_of_split(a, s, h, split);
+    const KeyRange range = keys_of_split(a, a.src, s, h, split);
     const int k_lo = range.lo, k_hi = range.hi;
     if (k_lo >= k_hi && a.part_o) {
-        no_keys(a, split, tr.t0, r0, min(rows - r0, kRowTile), h, Hq);
+        no_keys(a, a.src, split, tr.t0, r0, min(rows - r0, kRows), h, Hq);
         return;
     }
 
-    // this lane's row: column m of S^T and O^T
-    const int r = min(r0 + m, rows - 1), t = tr.t0 + r / G, hq = h * G + r % G;
-    const bool real = r0 + m < rows;
-    const int32_t t_pos = a.pos ? a.pos[t] : 0;
-    int32_t first_pos = t_pos;
+    // this lane's rows: columns m of the column tiles of S^T and O^T
+    float q[NT][8][4];
+    int32_t t_pos[NT], first_pos = 0x7fffffff;
+    bool real[NT];
 #pragma unroll
-    for (int i = 1; i < 16; i *= 2) first_pos = min(first_pos, __shfl_xor(first_pos, i));
-    float q[8][4];
-    {
+    for (int n = 0; n < NT; ++n) {
+        const int at = r0 + 16 * n + m, r = min(at, rows - 1), t = tr.t0 + r / G, hq = h * G + r % G;
+        real[n] = at < rows;
+        t_pos[n] = a.pos ? a.pos[t] : 0;
+        first_pos = min(first_pos, t_pos[n]);
         const char *p = a.q + ((int64_t)t * a.q_stride_token + (int64_t)hq * a.q_stride_head) * (int64_t)sizeof(T);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) load4<T>(p + (16 * j + 4 * kq) * sizeof(T), q[j]);
+        for (int j = 0; j < 8; ++j) load4<T>(p + (16 * j + 4 * kq) * sizeof(T), q[n][j]);
         if (a.rotate_q) {
-            if (TURN ? HALF : (bool)a.half) rotate32<true>(q, t_pos, kq, turns);
-            else rotate32<false>(q, t_pos, kq, turns);
+            if (TURN ? HALF : (bool)a.half) rotate32<true>(q[n], t_pos[n], kq, turns);
+            else rotate32<false>(q[n], t_pos[n], kq, turns);
         }
     }
-    f32x4 o[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float top = kNoScore, sum = 0.f;
+    for (int i = 1; i < 16; i *= 2) first_pos = min(first_pos, __shfl_xor(first_pos, i));
+    f32x4 o[NT][8];
+    float top[NT], sum[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        top[n] = kNoScore;
+        sum[n] = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) o[n][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
     const int64_t base = (int64_t)a.layer * c.stride_layer + (int64_t)h * c.stride_head;
     const int64_t pbase = (int64_t)a.layer * c.pos_stride_layer + (int64_t)h * c.pos_stride_head;
     const int in_block = c.block_shift < 0 ? 0x7fffffff : (1 << c.block_shift) - 1;
@@ -135,11 +145,15 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_general_kernel(Atten
     }
     for (; k0 < k_hi; k0 += 64) {
         if (TURN) rotate32<HALF>(k, k_pos, kq, turns);
-        f32x4 sc = f32x4{0.f, 0.f, 0.f, 0.f};
+        f32x4 sc[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) sc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < 8; ++j)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sc = __builtin_amdgcn_mfma_f32_16x16x4f32(k[j][e], q[j][e], sc, 0, 0, 0);
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) sc[n] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[j][e], q[n][j][e], sc[n], 0, 0, 0);
         // the keys this lane has scores of (and whose V rows it has): 4 kq + i
         const bool there = there_at(k0, block);
         const int32_t pos_here = k_pos;
@@ -147,43 +161,53 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_general_kernel(Atten
         const int block_next = ahead;
         load_k(k0 + 64, block_next);   // (beyond the last tile: its last key again)
         ahead = block_at(k0 + 128);
-        bool keep[4] = {true, true, true, true};
+        uint32_t keep[NT];   // bit i
         bool hole = false, odd = false;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) keep[n] = 0xfu;
         if (there_bits != 0xffffu || (a.causal && __ballot(pos_here > first_pos))) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const bool on = (there_bits >> (4 * kq + i)) & 1;
                 const int32_t vp = __shfl(pos_here, 4 * kq + i);
-                keep[i] = on && (!a.causal || vp <= t_pos);
-                hole |= real && on && !keep[i];
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const bool attends = on & (!a.causal | (vp <= t_pos[n]));
+                    if (!attends) keep[n] &= ~(1u << i), sc[n][i] = kNoScore;
+                    hole |= real[n] & on & !attends;
+                }
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) v[i][j][e] = on ? v[i][j][e] : 0.f;
             }
         }
-        float best = kNoScore;
+        float p[NT][4], best[NT];
+        bool higher = false;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            sc[i] = keep[i] ? sc[i] : kNoScore;
-            best = fmaxf(best, sc[i]);
+        for (int n = 0; n < NT; ++n) {
+            best[n] = max_over_kq(fmaxf(fmaxf(sc[n][0], sc[n][1]), fmaxf(sc[n][2], sc[n][3])));
+            higher |= best[n] > top[n];
         }
-        best = fmaxf(best, __shfl_xor(best, 16));
-        best = fmaxf(best, __shfl_xor(best, 32));
-        if (__ballot(best > top)) {   // (rare after the first tiles)
-            const float next = fmaxf(top, best);
-            const float shrink = next == kNoScore ? 1.f : __builtin_amdgcn_exp2f((top - next) * a.scale_log2);   // (no score yet: 2^-inf = 0)
-            top = next;
-            sum *= shrink;
+        if (__ballot(higher)) {   // (rare after the first tiles)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) o[j] *= shrink;
+            for (int n = 0; n < NT; ++n) {
+                const float next = fmaxf(top[n], best[n]);
+                const float shrink = next == kNoScore ? 1.f : __builtin_amdgcn_exp2f((top[n] - next) * a.scale_log2);   // (no score yet: 2^-inf = 0)
+                top[n] = next;
+                sum[n] *= shrink;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) o[n][j] *= shrink;
+            }
         }
-        const float ref = top == kNoScore ? 0.f : top;
-        float p[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            p[i] = keep[i] ? __builtin_amdgcn_exp2f((sc[i] - ref) * a.scale_log2) : 0.f;
-            sum += p[i];
+        for (int n = 0; n < NT; ++n) {
+            const float ref = top[n] == kNoScore ? 0.f : top[n];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                p[n][i] = __builtin_amdgcn_exp2f((sc[n][i] - ref) * a.scale_log2);   // (left out: 2^-inf = 0)
+                sum[n] += p[n][i];
+            }
         }
         // A value that is not finite must not reach rows that do not attend to its key (0 times it is no 0).  Where a row of the tile leaves a key out, such values
         // are taken out of the product and added as what they are, by products of "attends" with "is +inf or NaN" and "is -inf or NaN".
@@ -199,17 +223,22 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_general_kernel(Atten
                 for (int j = 0; j < 2; ++j)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        f32x4 up = f32x4{0.f, 0.f, 0.f, 0.f}, down = up;
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const float x = v[i][j][e], on = keep[i] ? 1.f : 0.f;
-                            up = __builtin_amdgcn_mfma_f32_16x16x4f32(x < __builtin_inff() ? 0.f : 1.f, on, up, 0, 0, 0);
-                            down = __builtin_amdgcn_mfma_f32_16x16x4f32(x > -__builtin_inff() ? 0.f : 1.f, on, down, 0, 0, 0);
-                            if (!(fabsf(x) < __builtin_inff())) v[i][j][e] = 0.f;
+                        for (int n = 0; n < NT; ++n) {
+                            f32x4 up = f32x4{0.f, 0.f, 0.f, 0.f}, down = up;
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const float x = v[i][j][e], on = (keep[n] >> i) & 1 ? 1.f : 0.f;
+                                up = __builtin_amdgcn_mfma_f32_16x16x4f32(x < __builtin_inff() ? 0.f : 1.f, on, up, 0, 0, 0);
+                                down = __builtin_amdgcn_mfma_f32_16x16x4f32(x > -__builtin_inff() ? 0.f : 1.f, on, down, 0, 0, 0);
+                            }
+#pragma unroll
+                            for (int d = 0; d < 4; ++d) o[n][4 * j + e][d] += (up[d] > 0.f ? __builtin_inff() : 0.f) + (down[d] > 0.f ? -__builtin_inff() : 0.f);
+                            __builtin_amdgcn_sched_barrier(0);   // (one after the other: few registers, and time does not matter here)
                         }
 #pragma unroll
-                        for (int d = 0; d < 4; ++d) o[4 * j + e][d] += (up[d] > 0.f ? __builtin_inff() : 0.f) + (down[d] > 0.f ? -__builtin_inff() : 0.f);
-                        __builtin_amdgcn_sched_barrier(0);   // (one after the other: few registers, and time does not matter here)
+                        for (int i = 0; i < 4; ++i)
+                            if (!(fabsf(v[i][j][e]) < __builtin_inff())) v[i][j][e] = 0.f;
                     }
             }
         }
@@ -218,38 +247,49 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_general_kernel(Atten
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[4 * j + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[i][j][e], p[i], o[4 * j + e], 0, 0, 0);
+                for (int e = 0; e < 4; ++e)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) o[n][4 * j + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[i][j][e], p[n][i], o[n][4 * j + e], 0, 0, 0);
         load_v(k0 + 64, block_next);
         block = block_next;
     }
-    sum += __shfl_xor(sum, 16);
-    sum += __shfl_xor(sum, 32);
-    if (kq == 0) wave_m[wave][m] = top, wave_l[wave][m] = sum;
-    __syncthreads();
-    float all = kNoScore;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) all = fmaxf(all, wave_m[j][m]);
-    const float mine = __builtin_amdgcn_exp2f((top - (all == kNoScore ? 0.f : all)) * a.scale_log2);
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int d = 0; d < 4; ++d)   // dimensions 64 j + 16 kq + 4 d + e
-            *reinterpret_cast<f32x4 *>(&wave_o[wave][m][64 * j + 16 * kq + 4 * d]) =
-                f32x4{o[4 * j][d], o[4 * j + 1][d], o[4 * j + 2][d], o[4 * j + 3][d]} * mine;
-    __syncthreads();
-    const int row = tid >> 4, d0 = 8 * (tid & 15);
-    if (r0 + row >= rows) return;
-    float best = kNoScore, total = 0.f, x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) best = fmaxf(best, wave_m[j][row]);
-    const float ref = best == kNoScore ? 0.f : best;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        total += wave_l[j][row] * __builtin_amdgcn_exp2f((wave_m[j][row] - ref) * a.scale_log2);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] += wave_o[j][row][d0 + e];
+    for (int n = 0; n < NT; ++n) {
+        sum[n] += __shfl_xor(sum[n], 16);
+        sum[n] += __shfl_xor(sum[n], 32);
+        if (kq == 0) wave_m[wave][16 * n + m] = top[n], wave_l[wave][16 * n + m] = sum[n];
     }
-    finish_row<T>(a, split, tr.t0 + (r0 + row) / G, h * G + (r0 + row) % G, Hq, d0, best, total, x);
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        float all = kNoScore;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) all = fmaxf(all, wave_m[j][16 * n + m]);
+        const float mine = __builtin_amdgcn_exp2f((top[n] - (all == kNoScore ? 0.f : all)) * a.scale_log2);
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int d = 0; d < 4; ++d)   // dimensions 64 j + 16 kq + 4 d + e
+                *reinterpret_cast<f32x4 *>(&wave_o[wave][16 * n + m][64 * j + 16 * kq + 4 * d]) =
+                    f32x4{o[n][4 * j][d], o[n][4 * j + 1][d], o[n][4 * j + 2][d], o[n][4 * j + 3][d]} * mine;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const int row = 16 * n + (tid >> 4), d0 = 8 * (tid & 15);
+        if (r0 + row >= rows) return;
+        float best = kNoScore, total = 0.f, x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) best = fmaxf(best, wave_m[j][row]);
+        const float ref = best == kNoScore ? 0.f : best;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            total += wave_l[j][row] * __builtin_amdgcn_exp2f((wave_m[j][row] - ref) * a.scale_log2);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] += wave_o[j][row][d0 + e];
+        }
+        finish_row<T>(a, a.src, split, tr.t0 + (r0 + row) / G, h * G + (r0 + row) % G, Hq, d0, best, total, x);
+    }
 }
 
 // Joins the parts of a row: sixteen threads have 8 dimensions each, and SPREAD such groups of a workgroup's sixteen share a row's parts, each going through its own in one pass
@@ -322,6 +362,10 @@ static Kernel kernel_of(const tri_cache &c, int64_t rows)
     return rows <= 32 ? Kernel::rows : Kernel::tile;
 }
 
+// Rows of a workgroup of the general kernel.  32 where that spares a second pass over the keys (fp32, eight sequences of 4096 keys, 28 rows: 89 / 83 us); with more rows two waves to a SIMD, which 16
+// rows leave room for, are worth more (two chunks of 256 tokens over 4352 keys 295 us with 16, 371 with 32).
+static int64_t general_rows(const tri_cache &c, int64_t rows) { return c.dtype == TRI_F32 && rows > 16 && rows <= 32 ? 32 : 16; }
+
 // Parts.  Two workgroups of either bf16 kernel share a CU, so 512 of them fill the GPU; more even out ragged batches, and each costs what 100 to 200 keys do, and the joining of its
 // results.  Measured, us by parts per head, 8 KV heads, G = 4, bf16 single tokens: 16 x 65536 keys 1023 / 630 / 642 / 637 / 661 / 850 at 1, 2, 8, 16, 48, 128 parts; 16 sequences between
 // 1000 and 65536 keys 938 / 526 / 438 / 399 / 418 / 523 at the same; 16 x 4096 69 / 49 / 61 / 71 at 1, 2, 8, 16; 64 x 2176 90 / 98 / 143 at 1, 2, 8; one of 131072 at G = 8 201 / 114 / 96 /
@@ -333,7 +377,7 @@ void attend_split(const tri_model &m, const tri_cache &c, int32_t max_tokens, in
 {
     const int64_t G = m.n_q_heads / m.n_kv_heads, rows = max_tokens * G;
     const Kernel kernel = kernel_of(c, rows);
-    const int64_t per_tile = kernel == Kernel::general ? kRowTile : kernel == Kernel::rows ? 32 : kTileRows;
+    const int64_t per_tile = kernel == Kernel::general ? general_rows(c, rows) : kernel == Kernel::rows ? 32 : kTileRows;
     // row tiles that there are: all tokens' rows, and half a tile more per sequence, whose last one is not full
     const int64_t tiles = kernel == Kernel::rows ? c.n_seqs : std::max<int64_t>(c.n_seqs, (n_tokens * G + per_tile - 1) / per_tile + c.n_seqs / 2);
     const int64_t units = m.n_kv_heads * tiles;
@@ -352,14 +396,35 @@ tri_status launch_attend(AttendArgs a, const tri_cache &c, hipStream_t st)
     const Kernel kernel = kernel_of(c, rows);
     if (kernel == Kernel::rows) return launch_attend_rows(a, (int32_t)rows, st);
     if (kernel == Kernel::tile) return launch_attend_tile(a, (int32_t)rows, st);
-    a.row_tiles = (int32_t)((rows + kRowTile - 1) / kRowTile);
-    const int64_t blocks = (int64_t)a.row_tiles * a.src.n_split * a.src.cache.n_kv_heads * a.src.cache.n_seqs;
-    const auto launch = [&](auto kernel) { kernel<<<(uint32_t)blocks, kAttendThreads, 0, st>>>(a); };
-    const bool bf16 = c.dtype == TRI_BF16;
-    if (c.k_rotated) launch(bf16 ? attend_general_kernel<__bf16, false, false> : attend_general_kernel<float, false, false>);
-    else if (a.half) launch(bf16 ? attend_general_kernel<__bf16, true, true> : attend_general_kernel<float, true, true>);
-    else launch(bf16 ? attend_general_kernel<__bf16, true, false> : attend_general_kernel<float, true, false>);
+    const int64_t per_tile = general_rows(c, rows);
+    a.row_tiles = (int32_t)((rows + per_tile - 1) / per_tile);
+    const int64_t groups = (int64_t)a.src.n_split * a.src.cache.n_kv_heads * a.src.cache.n_seqs;
+    const uint32_t blocks = (uint32_t)((groups + 7) / 8 * 8 * a.row_tiles);
+    const auto launch = [&](auto kernel) { kernel<<<blocks, kAttendThreads, 0, st>>>(a); };
+    if (c.dtype == TRI_BF16) launch(c.k_rotated ? attend_general_kernel<__bf16, 1, false, false> : a.half ? attend_general_kernel<__bf16, 1, true, true> : attend_general_kernel<__bf16, 1, true, false>);
+    else if (per_tile == 16) launch(c.k_rotated ? attend_general_kernel<float, 1, false, false> : a.half ? attend_general_kernel<float, 1, true, true> : attend_general_kernel<float, 1, true, false>);
+    else launch(c.k_rotated ? attend_general_kernel<float, 2, false, false> : a.half ? attend_general_kernel<float, 2, true, true> : attend_general_kernel<float, 2, true, false>);
     return hip_status("attend_general_kernel");
+}
+
+// Small batches behind a prefix spend their time in one chain of memory latencies per launch: both caches go in one launch of attend_rows_kernel where both are its, of the same layout, and either take the same
+// variant of it or are so few workgroups that all run at once (eight sequences of up to 130 keys behind 2048: 28 us with a launch each and the joining, 20 with one).
+tri_status launch_attend_both(AttendArgs a, const tri_cache &c, const tri_cache &other, hipStream_t st)
+{
+    const auto rows_of = [&](const AttendSource &s) { return (int64_t)s.max_tokens * a.group_size; };
+    const auto variant = [](int64_t rows) { return rows <= 8 ? 0 : rows <= 16 ? 1 : 2; };
+    const auto pages = [](const AttendSource &s) { return s.cache.block_shift < 0 ? 0 : s.cache.block_shift >= 4 ? 1 : 2; };
+    const auto groups = [](const AttendSource &s) { return (int64_t)s.n_split * s.cache.n_kv_heads * s.cache.n_seqs; };
+    const int64_t rows = rows_of(a.src), more = rows_of(a.other);
+    if (kernel_of(c, rows) == Kernel::rows && kernel_of(other, more) == Kernel::rows && pages(a.src) == pages(a.other) && a.src.cache.k_rotated == a.other.cache.k_rotated &&
+        (variant(rows) == variant(more) || groups(a.src) + groups(a.other) <= 512))
+        return launch_attend_rows(a, (int32_t)std::max(rows, more), st);
+    const AttendSource second = a.other;
+    a.other = AttendSource{};
+    const tri_status rc = launch_attend(a, c, st);
+    if (rc != TRI_OK) return rc;
+    a.src = second;
+    return launch_attend(a, other, st);
 }
 
 tri_status launch_join(const AttendArgs &a, int32_t parts, int32_t n_q_heads, int32_t dtype, hipStream_t st)

@@ -37,20 +37,20 @@ __device__ __forceinline__ void widen8(const uint4 &u, float *x)
 struct KeyRange {
     int lo, hi;
 };
-__device__ __forceinline__ KeyRange keys_of_split(const AttendArgs &a, int s, int h, int split)
+__device__ __forceinline__ KeyRange keys_of_split(const AttendArgs &a, const AttendSource &src, int s, int h, int split)
 {
-    const int n = keys_of(a, s, h);
-    const int64_t share = max(((int64_t)n + a.src.n_split - 1) / a.src.n_split, (int64_t)a.src.least_keys), per = (share + 127) & ~(int64_t)127;
+    const int n = keys_of(a, src, s, h);
+    const int64_t share = max(((int64_t)n + src.n_split - 1) / src.n_split, (int64_t)src.least_keys), per = (share + 127) & ~(int64_t)127;
     const int lo = (int)min(split * per, (int64_t)n);
     return KeyRange{lo, (int)min(lo + per, (int64_t)n)};
 }
 
 // A part without a key says so; its sums are not read.
-__device__ __forceinline__ void no_keys(const AttendArgs &a, int split, int t0, int r0, int rows, int h, int Hq)
+__device__ __forceinline__ void no_keys(const AttendArgs &a, const AttendSource &src, int split, int t0, int r0, int rows, int h, int Hq)
 {
     for (int i = threadIdx.x; i < rows; i += blockDim.x) {
         const int r = r0 + i;
-        a.part_ml[((int64_t)(a.src.part0 + split) * a.n_tokens + t0 + r / a.group_size) * Hq + h * a.group_size + r % a.group_size] = make_float2(kNoScore, 0.f);
+        a.part_ml[((int64_t)(src.part0 + split) * a.n_tokens + t0 + r / a.group_size) * Hq + h * a.group_size + r % a.group_size] = make_float2(kNoScore, 0.f);
     }
 }
 
@@ -120,10 +120,10 @@ __device__ __forceinline__ bf16x8 where_not_below(const bf16x8 &x, uint32_t whic
 
 // Eight dimensions of a row whose keys are all seen to: to the output, or as a part.
 template <typename T>
-__device__ __forceinline__ void finish_row(const AttendArgs &a, int split, int t, int hq, int Hq, int d0, float best, float total, float *x)
+__device__ __forceinline__ void finish_row(const AttendArgs &a, const AttendSource &src, int split, int t, int hq, int Hq, int d0, float best, float total, float *x)
 {
     if (a.part_o) {
-        const int64_t at = ((int64_t)(a.src.part0 + split) * a.n_tokens + t) * Hq + hq;
+        const int64_t at = ((int64_t)(src.part0 + split) * a.n_tokens + t) * Hq + hq;
         if (d0 == 0) a.part_ml[at] = make_float2(best, total);
         store8(a.part_o + at * kHeadDim + d0, x);
         return;
@@ -136,6 +136,6 @@ __device__ __forceinline__ void finish_row(const AttendArgs &a, int split, int t
 
 constexpr int kTileRows = 128;   // rows of a workgroup of the tile kernel
 tri_status launch_attend_tile(AttendArgs a, int32_t rows, hipStream_t st);
-tri_status launch_attend_rows(AttendArgs a, int32_t rows, hipStream_t st);
+tri_status launch_attend_rows(AttendArgs a, int32_t rows, hipStream_t st);   // a.src, and a.other where it has sequences
 
 }  // namespace tri

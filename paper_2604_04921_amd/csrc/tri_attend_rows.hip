@@ -36,8 +36,8 @@ __device__ __forceinline__ void rotate_row(float (*x)[8], int32_t pos, int kq, c
 // LO: columns 8 to 15 of a tile hold what the rounding to bf16 takes off the rows 0 to 7 (of q turned by its position, and of the weights): the matrix
 // instructions have that room where rows are at most eight to a tile, and both products are as good as in 16 bits of fraction.  Keys turned on the way (TURN)
 // are multiplied as two bf16 numbers for the same reason.  Without LO what is taken off q lies in LDS and is multiplied on its own, and the weights are rounded to bf16 once.
-// Measured (8 KV heads): 32 ragged sequences up to 32768 keys in pages of 16, G = 4, 378 us, 2.29 GB at 6.1 TB/s (read once: 1.14 GB by the counter of fetches, which counts half of non-temporal
-// reads; a pure read stream reaches 7.0); the matrix pipe is busy for 4 % of that.  One of 131072 pre-RoPE keys at G = 8 96 us, 5.6 TB/s: 48 % of the time the vector pipe is busy turning keys.  One sequence
+// Measured (8 KV heads): 32 ragged sequences up to 32768 keys in pages of 16, G = 4, 378 us, 2.29 GB at 6.1 TB/s (read once: 1.14 GB by the counter of fetches, which shows half of what is
+// known to be read; a pure read stream reaches 7.0); the matrix pipe is busy for 4 % of that.  One of 131072 pre-RoPE keys at G = 8 96 us, 5.6 TB/s: 48 % of the time the vector pipe is busy turning keys.  One sequence
 // of 2176 keys: 10 us, nearly all of it one chain of memory latencies.  Two workgroups to a CU: with three (168 registers, what does not fit spilled) the ragged batch takes 490.  Operands of pages
 // below sixteen slots have addresses of their own, 64 bits each: 452 us for that batch in pages of one slot.
 template <int NT, bool LO, int PAGES, bool TURN, bool HALF>
@@ -48,21 +48,21 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attend_rows_kernel(AttendArgs
     __shared__ float wave_m[4][kRows], wave_l[4][kRows];
     __shared__ __align__(16) float wave_o[4][kRows][kHeadDim + 4];
     __shared__ __align__(16) bf16x8 q_low[LO ? 1 : NT][4][64];   // what rounding takes off the rows, as operands
-    const CacheView &c = a.src.cache;
+    const bool second = blockIdx.x >= a.first_groups;
+    const AttendSource &src = second ? a.other : a.src;
+    const CacheView &c = src.cache;
     const int H = c.n_kv_heads, G = a.group_size, Hq = H * G;
-    uint32_t w = blockIdx.x;
-    const int rt = w % a.row_tiles;
-    w /= a.row_tiles;
-    const int split = w % a.src.n_split;
-    w /= a.src.n_split;
+    uint32_t w = blockIdx.x - (second ? a.first_groups : 0);
+    const int split = w % src.n_split;
+    w /= src.n_split;
     const int h = w % H, s = w / H;
-    const TokenRange tr = tokens_of(a, s);
-    const int rows = tr.n * G, r0 = rt * kRows;
-    if (r0 >= rows) return;
+    const TokenRange tr = tokens_of(a, src, s);
+    const int rows = min(tr.n * G, kRows);
+    if (rows == 0) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15, kq = lane >> 4;
-    const KeyRange range = keys_of_split(a, s, h, split);
+    const KeyRange range = keys_of_split(a, src, s, h, split);
     if (range.lo >= range.hi && a.part_o) {
-        no_keys(a, split, tr.t0, r0, min(rows - r0, kRows), h, Hq);
+        no_keys(a, src, split, tr.t0, 0, rows, h, Hq);
         return;
     }
     const int k_hi = __builtin_amdgcn_readfirstlane(range.hi);   // (what buffer descriptors are made of stays in scalar registers)
@@ -80,7 +80,7 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attend_rows_kernel(AttendArgs
         uint32_t there;
     };
     const int in_block = PAGES ? (1 << c.block_shift) - 1 : 0;
-    auto is_block = [&](int b) { return (b >= 0) & ((a.src.n_blocks == 0) | (b < a.src.n_blocks)); };
+    auto is_block = [&](int b) { return (b >= 0) & ((src.n_blocks == 0) | (b < src.n_blocks)); };
     auto find = [&](int k0, int block_loaded) {
         Rows r;
         const int left = __builtin_amdgcn_readfirstlane(min(max(k_hi - k0, 0), 16));
@@ -171,7 +171,7 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attend_rows_kernel(AttendArgs
     bool real[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        const int at = r0 + n * kCols + (LO ? m & 7 : m), r = min(at, rows - 1), t = tr.t0 + r / G, hq = h * G + r % G;
+        const int at = n * kCols + (LO ? m & 7 : m), r = min(at, rows - 1), t = tr.t0 + r / G, hq = h * G + r % G;
         real[n] = at < rows;
         t_pos[n] = a.causal ? a.pos[t] : 0x7fffffff;
         first_pos = min(first_pos, t_pos[n]);
@@ -398,7 +398,7 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attend_rows_kernel(AttendArgs
 #pragma unroll
     for (int i = 0; i < kRows / 16 + (kRows < 16); ++i) {
         const int row = 16 * i + (tid >> 4), d0 = 8 * (tid & 15);
-        if (row >= kRows || r0 + row >= rows) break;
+        if (row >= rows) break;
         float best = kNoScore, total = 0.f, x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < 4; ++j) best = fmaxf(best, wave_m[j][row]);
@@ -409,7 +409,7 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attend_rows_kernel(AttendArgs
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] += wave_o[j][row][d0 + e];
         }
-        finish_row<__bf16>(a, split, tr.t0 + (r0 + row) / G, h * G + (r0 + row) % G, Hq, d0, best, total, x);
+        finish_row<__bf16>(a, src, split, tr.t0 + row / G, h * G + row % G, Hq, d0, best, total, x);
     }
 }
 
@@ -427,8 +427,8 @@ void launch_rows_of(const AttendArgs &a, uint32_t blocks, hipStream_t st)
 
 tri_status launch_attend_rows(AttendArgs a, int32_t rows, hipStream_t st)
 {
-    a.row_tiles = 1;
-    const uint32_t blocks = (uint32_t)((int64_t)a.src.n_split * a.src.cache.n_kv_heads * a.src.cache.n_seqs);
+    a.first_groups = (uint32_t)((int64_t)a.src.n_split * a.src.cache.n_kv_heads * a.src.cache.n_seqs);
+    const uint32_t blocks = a.first_groups + (uint32_t)((int64_t)a.other.n_split * a.other.cache.n_kv_heads * a.other.cache.n_seqs);
     if (rows <= 8) launch_rows_of<1, true>(a, blocks, st);
     else if (rows <= 16) launch_rows_of<2, true>(a, blocks, st);
     else launch_rows_of<2, false>(a, blocks, st);

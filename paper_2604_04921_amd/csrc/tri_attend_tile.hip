@@ -64,12 +64,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
     w /= a.src.n_split;
     const int head = w % H, s = w / H;
     if (s >= c.n_seqs) return;
-    const TokenRange tr = tokens_of(a, s);
+    const TokenRange tr = tokens_of(a, a.src, s);
     const int rows = tr.n * G, r0 = rt0 * kRows;
     if (r0 >= rows) return;
-    const KeyRange range = keys_of_split(a, s, head, split);
+    const KeyRange range = keys_of_split(a, a.src, s, head, split);
     if (range.lo >= range.hi && a.part_o) {
-        no_keys(a, split, tr.t0, r0, min(rows - r0, kRows), head, Hq);
+        no_keys(a, a.src, split, tr.t0, r0, min(rows - r0, kRows), head, Hq);
         return;
     }
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, h = lane >> 5;

@@ -83,6 +83,8 @@ struct AttendSource {
 };
 struct AttendArgs {
     AttendSource src;
+    AttendSource other;        // attend_rows_kernel: workgroups from first_groups on work on this one
+    uint32_t first_groups;
     BandTurns turns;
     const int32_t *start, *pos;
     const char *q;
@@ -97,25 +99,27 @@ struct AttendArgs {
 };
 
 // Tokens that attend to sequence s of the source.
-__device__ __forceinline__ TokenRange tokens_of(const AttendArgs &a, int s)
+__device__ __forceinline__ TokenRange tokens_of(const AttendArgs &a, const AttendSource &src, int s)
 {
     int lo = s, hi = s + 1;
-    if (a.src.all) lo = 0, hi = a.n_steps_seqs;
-    if (a.src.group) lo = clamp_to(a.src.group[s], a.n_steps_seqs), hi = clamp_to(a.src.group[s + 1], a.n_steps_seqs);
+    if (src.all) lo = 0, hi = a.n_steps_seqs;
+    if (src.group) lo = clamp_to(src.group[s], a.n_steps_seqs), hi = clamp_to(src.group[s + 1], a.n_steps_seqs);
     if (a.start) lo = a.start[lo], hi = a.start[hi];
     lo = clamp_to(lo, a.n_tokens), hi = clamp_to(hi, a.n_tokens);
-    return TokenRange{lo, min(max(hi - lo, 0), a.src.max_tokens)};
+    return TokenRange{lo, min(max(hi - lo, 0), src.max_tokens)};
 }
-__device__ __forceinline__ int keys_of(const AttendArgs &a, int s, int h)
+__device__ __forceinline__ int keys_of(const AttendArgs &a, const AttendSource &src, int s, int h)
 {
-    const CacheView &c = a.src.cache;
-    const int n = a.src.head_len ? a.src.head_len[((int64_t)a.layer * c.n_seqs + s) * c.n_kv_heads + h] : c.seq_len[s];
+    const CacheView &c = src.cache;
+    const int n = src.head_len ? src.head_len[((int64_t)a.layer * c.n_seqs + s) * c.n_kv_heads + h] : c.seq_len[s];
     return clamp_len(n, c.max_seq_len);
 }
 
 // How the keys of a cache are cut: ranges per head, and their least keys (a function of bounds alone, for the workspace's size).
 void attend_split(const tri_model &m, const tri_cache &c, int32_t max_tokens, int32_t n_tokens, int32_t *n_split, int32_t *least_keys);
 tri_status launch_attend(AttendArgs a, const tri_cache &c, hipStream_t st);   // (c: a.src's)
+// a.src and a.other, in one launch where that is worth it
+tri_status launch_attend_both(AttendArgs a, const tri_cache &c, const tri_cache &other, hipStream_t st);
 tri_status launch_join(const AttendArgs &a, int32_t parts, int32_t n_q_heads, int32_t dtype, hipStream_t st);
 
 }  // namespace tri

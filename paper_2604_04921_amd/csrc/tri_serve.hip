@@ -163,13 +163,17 @@ tri_status attend(const tri_model *model, const tri_cache *prefix, const int32_t
     a.causal = at->causal;
     a.rotate_q = !tokens->rotated;
     a.half = model->pairs == TRI_PAIR_HALF;
+    const AttendSource own{make_view(*model, *cache), nullptr, tokens->head_len, cache->n_blocks, 0, most_tokens(*tokens), plan.own_split, 0, plan.own_least};
     if (prefix) {
         a.src = AttendSource{make_view(*model, *prefix), group, nullptr, prefix->n_blocks, group ? 0 : 1, tokens->n_tokens, plan.prefix_split, plan.own_split,
                              plan.prefix_least};
-        if ((rc = launch_attend(a, *prefix, st)) != TRI_OK) return rc;
+        a.other = own;
+        rc = launch_attend_both(a, *prefix, *cache, st);
+    } else {
+        a.src = own;
+        rc = launch_attend(a, *cache, st);
     }
-    a.src = AttendSource{make_view(*model, *cache), nullptr, tokens->head_len, cache->n_blocks, 0, most_tokens(*tokens), plan.own_split, 0, plan.own_least};
-    if ((rc = launch_attend(a, *cache, st)) != TRI_OK) return rc;
+    if (rc != TRI_OK) return rc;
     return plan.parts ? launch_join(a, plan.parts, model->n_q_heads, cache->dtype, st) : TRI_OK;
 }
 

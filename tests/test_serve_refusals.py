@@ -92,7 +92,9 @@ def test_what_good_calls_launch():
     assert len(launches(dict(entry="attend", tokens=0))) == 0
     assert len(launches(dict(entry="attend", n=100, ws=0, ws_bytes=0))) == 1       # short rows: straight to the output
     assert len(launches(dict(entry="attend", n=100000))) == 2
-    assert len(launches(dict(entry="shared"))) == 3
+    assert len(launches(dict(entry="shared"))) == 2                # few workgroups: both caches at once, and the joining
+    assert len(launches(dict(entry="shared", rotated=0))) == 3     # (of two layouts)
+    assert len(launches(dict(entry="shared", tokens=50, most=30))) == 3
 
 
 def test_workspace_size():
