@@ -80,6 +80,7 @@ struct AttendSource {
     int32_t max_tokens;        // tokens that attend to one sequence of this cache, at most
     int32_t n_split, part0;    // its keys are cut into n_split ranges; the results are entries part0 and on of the partial results
     int32_t least_keys;        // of a range that is not the last
+    int32_t scan;              // keys behind the tokens' positions are likely at its end (a chunk's own tokens)
 };
 struct AttendArgs {
     AttendSource src;
