@@ -61,9 +61,9 @@ struct Piece<__bf16> {
 // A thread takes two 16-byte pieces of one K row and of its V row, half a row apart: both parts of its bands lie in them in either
 // pair layout.  Pure streaming: a row is read and written once; the rotation (a sincos per band and row) is not what bounds it.
 // A wave covers 8 (bf16) or 4 (fp32) neighbouring rows; the sequence of its first token is found by all lanes at once (the number of
-// starts at or below it), the others' by going on from there.  The rows are asked for before that: 19972 tokens of four prompts, 8 KV heads, 164 MB read and written, take
-// 28.5 us (5.7 TB/s; 37 with the loads behind the search); non-temporal loads take 34, the rows coming out of a product that has just written them.  A single
-// token's launch takes 3.2 us, 256 sequences' 5.1.
+// starts at or below it), the others' by going on from there.  The rows are asked for before that (four prompts' 19972 tokens, 8 KV heads, 164 MB read and written: 37 us with the
+// loads behind the search, 28.5 with the rows in the caches).  Stores are non-temporal: from memory to memory that call takes 31 us (5.3 TB/s), 39 with plain ones, 34 with non-temporal
+// loads, whatever the stores.  A single token's launch takes 3.1 us, 256 sequences' 4.9.
 template <typename T>
 __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a)
 {
@@ -147,10 +147,10 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a)
         k1 = Piece<T>::put(y);
     }
     char *dk = (char *)c.k + to, *dv = (char *)c.v + to;
-    *reinterpret_cast<uint4 *>(dk) = k0;
-    *reinterpret_cast<uint4 *>(dk + half_row) = k1;
-    *reinterpret_cast<uint4 *>(dv) = v0;
-    *reinterpret_cast<uint4 *>(dv + half_row) = v1;
+    store_stream16(dk, k0);
+    store_stream16(dk + half_row, k1);
+    store_stream16(dv, v0);
+    store_stream16(dv + half_row, v1);
     if (part == 0)
         const_cast<int32_t *>(c.pos)[(int64_t)a.layer * c.pos_stride_layer + (int64_t)h * c.pos_stride_head + block * c.pos_stride_sb + n] = pos;
 }

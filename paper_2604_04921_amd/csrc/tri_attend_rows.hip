@@ -118,7 +118,7 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attend_rows_kernel(AttendArgs
     // key `key` (0 to 31) of the tile from k0 on, its block being with lane `key`: the offset of its row
     auto slot_of = [&](int k0, int key, int block) {
         const int b = __shfl(block, key);
-        return is_block(b) & (k0 + key < k_hi) ? base + (int64_t)b * c.stride_sb + slot_offset(c, (k0 + key) & in_block) : base;
+        return (is_block(b) & (k0 + key < k_hi)) ? base + (int64_t)b * c.stride_sb + slot_offset(c, (k0 + key) & in_block) : base;
     };
     auto load_k = [&](const Rows (&r)[2], int k0, int block) {
 #pragma unroll
@@ -129,7 +129,7 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attend_rows_kernel(AttendArgs
                 const char *p = (const char *)c.k + slot_of(k0, key, block) * 2 + (l >> 4) * 16;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) k[i][j] = load_stream16(p + 64 * j);
-                k_pos[i] = need_pos ? c.pos[pbase + (is_block(b) & (k0 + key < k_hi) ? (int64_t)b * c.pos_stride_sb + ((k0 + key) & in_block) : 0)] : 0;
+                k_pos[i] = need_pos ? c.pos[pbase + ((is_block(b) & (k0 + key < k_hi)) ? (int64_t)b * c.pos_stride_sb + ((k0 + key) & in_block) : 0)] : 0;
                 continue;
             }
             const auto b = rsrc(c.k, r[i].kv, r[i].n);

@@ -44,7 +44,7 @@ struct TileBuffer {
 // operand where the first leaves its scores (lane half h holds keys 8 (i / 4) + 4 h + i % 4; the V operand takes its keys in that order, from transposing LDS reads).  K and V go from memory to LDS without passing
 // through registers; a tile's loads are under way while the last one is worked on.  q (turned by its position), keys turned on the way and the weights are rounded to bf16 once: more bits would double the first
 // product or the LDS that keys take, and a cache of turned keys holds the same.
-// Measured: two chunks of 1024 tokens over up to 8192 keys in pages of 64, 8 x 4 heads, 227 GFLOP: 258 us, 880 TFLOP/s (a library product of 8192 x 8192 matrices runs at 1355 here).  The matrix pipe is busy 36 % of the
+// Measured: two chunks of 1024 tokens over up to 8192 keys in pages of 64, 8 x 4 heads, 227 GFLOP: 262 us, 870 TFLOP/s (a library product of 8192 x 8192 matrices runs at 1355 here).  The matrix pipe is busy 36 % of the
 // time, the vector pipe with softmax 42 %, LDS 33 %, and the two hardly overlap: a wave issues in order, and there are two to a SIMD.  64 rows to a wave (one to a SIMD) took 577 us when 32 took
 // 322, eight waves to a workgroup 382; the loads' issue is a quarter of the time (without them, on stale tiles, 245 of 322).  Without neighbours on one XCD two prompts' 256 sequences take 379 us, with 229.
 template <int PAGES, bool TURN, bool HALF>
