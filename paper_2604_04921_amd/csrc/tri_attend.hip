@@ -294,6 +294,7 @@ __global__ __launch_bounds__(kAttendThreads, NT == 1 ? 2 : 1) void attend_genera
 
 // Joins the parts of a row: sixteen threads have 8 dimensions each, and SPREAD such groups of a workgroup's sixteen share a row's parts, each going through its own in one pass
 // with a running maximum; the groups are joined in LDS.  Sixteen where parts are many: one group alone walks 256 parts of a long cache one memory latency after the other.
+// Bound by latency, then by the parts' bytes: 33 parts of 2048 rows, 35 MB, 9.5 us (13.3 with the maxima looked for first and 147 registers), 64 parts of 64 rows 4.7.
 template <typename T, int SPREAD>
 __global__ __launch_bounds__(kAttendThreads, 6) void join_kernel(const float *part_o, const float2 *part_ml, char *out, int64_t out_stride_token,
                                                                  int64_t out_stride_head, int32_t n_q_heads, int64_t n_rows, int32_t parts, float scale_log2)

@@ -137,6 +137,72 @@ def test_rows_of_a_fused_projection_on_another_stream(dtype):
     check(B, c, [60, 30, 2], k_new=k_new, v_new=v_new, step=step, stream=side)
 
 
+@pytest.mark.parametrize("block", [0, 64])
+def test_offsets_beyond_32_bits(block):
+    """Heads (contiguous) and blocks (paged) that lie more than 2^32 bytes behind the first."""
+    from paper_2604_04921_amd import binding as B
+    c = P.Case(12, (70,), (30,), H=2, layers=1, layer=0, block=block)
+    own = c.own
+    if block:
+        far, farv = (torch.zeros((1, 140000, 2, block, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2))   # 4.6 GB each
+        farp = torch.zeros((1, 140000, 2, block), dtype=torch.int32, device="cuda")
+        n = own["k_gpu"].shape[1]
+        own["table_gpu"] += 140000 - n
+    else:
+        n, rows = own["cap"], (1 << 31) // 128 + 500
+        far, farv = (torch.zeros((1, 1, 2, rows, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        farp = torch.zeros((1, 1, 2, rows), dtype=torch.int32, device="cuda")
+    k_new, v_new = (c.put(c.g.standard_normal((c.T, c.H, 128))) for _ in range(2))
+    near = {f: own[f].nan_to_num_(nan=3.0, posinf=4.0).clone() if f != "pos_gpu" else own[f].clone() for f in ("k_gpu", "v_gpu", "pos_gpu")}
+    part = (slice(None), slice(-n, None)) if block else (slice(None), slice(None), slice(None), slice(0, n))
+    far[part], farv[part], farp[part] = near["k_gpu"], near["v_gpu"], near["pos_gpu"]
+    own.update(k_gpu=far, v_gpu=farv, pos_gpu=farp)
+    append(B, c, [70], None, k_new, v_new)
+    # the same call on the near cache
+    if block:
+        own["table_gpu"] -= 140000 - n
+    own.update(near)
+    append(B, c, [70], None, k_new, v_new)
+    for got, want in ((far, near["k_gpu"]), (farv, near["v_gpu"]), (farp, near["pos_gpu"])):
+        assert torch.equal(got[part], want)
+    assert int(torch.count_nonzero(farp)) == int(torch.count_nonzero(near["pos_gpu"]))   # and nowhere else
+
+
+def test_graph_of_a_step():
+    """An append and the attention over what it wrote, behind a shared prefix, captured once and replayed with other rows, eager work in between."""
+    from paper_2604_04921_amd import binding as B
+    c = P.Case(13, (40, 7, 0), (1, 1, 1), block=16, prefix=(300,), layers=1, layer=0)
+    own = c.own
+    lens = torch.tensor([40, 7, 0], dtype=torch.int32, device="cuda")
+    after = torch.zeros_like(lens)
+    model, tokens = c.model(B), c.step(B)
+    before, behind, prefix = c.descriptor(B, own, lens), c.descriptor(B, own, after), c.descriptor(B, c.prefix)
+    k_new, v_new = (c.put(c.g.standard_normal((c.T, c.H, 128))) for _ in range(2))
+    out = torch.zeros_like(c.q_gpu)
+    ws = torch.empty(B.tri_attend_workspace_size(model, behind, tokens, prefix), dtype=torch.uint8, device="cuda")
+
+    def step(to):
+        B.tri_append(model, before, 0, tokens, k_new, v_new, after)
+        B.tri_attend_shared(model, prefix, None, behind, 0, tokens, c.q_gpu, to, workspace=ws)
+    step(out)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(out)
+    for i in range(4):
+        k_new.mul_(-1.0 if i % 2 else 0.5)
+        v_new.add_(1.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.clone()
+        want = torch.zeros_like(out)
+        after.fill_(-1)
+        step(want)
+        torch.cuda.synchronize()
+        assert torch.equal(got, want) and after.tolist() == [41, 8, 1]
+        ws.fill_(0xff)
+
+
 def test_then_attended():
     """A prompt and single tokens appended call by call give the attention of the cache they make."""
     from paper_2604_04921_amd import binding as B

@@ -93,6 +93,32 @@ def test_every_key_counts_once(dtype, tokens, G):
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("block", [0, 1, 16])
+@pytest.mark.parametrize("backwards", [False, True])
+def test_prompts_over_themselves(dtype, block, backwards):
+    """A prompt's tokens over their own keys, whose later ones most rows leave out: in order, and with the slots of the one sequence turned round (every row then attends to the last slots)."""
+    from paper_2604_04921_amd import binding as B
+    c = P.Case(81, (0, 0, 3), (700, 1300, 90), H=1, G=2, dtype=dtype, block=block, layers=1, layer=0, stored_rotated=block != 16)
+    if backwards:
+        n = c.own["total"][1]
+        for f in ("k", "v", "pos"):
+            c.own[f][1, :, :n] = c.own[f][1][:, :n][:, ::-1].copy()
+        if block:
+            pages = c.own["table"]
+            for f in ("k", "v", "pos"):
+                x = c.own[f][1]
+                x = np.moveaxis(x.reshape((1, -1, block) + x.shape[2:]), 0, 1)
+                x = torch.from_numpy(np.ascontiguousarray(x)).to(c.own[f + "_gpu"].dtype).cuda()
+                keep = c.own[f + "_gpu"][0, pages[1]]
+                live = (torch.arange(x.shape[0] * block, device="cuda") < n).view(x.shape[0], 1, block, *([1] * (x.dim() - 3)))
+                c.own[f + "_gpu"][0, pages[1]] = torch.where(live, x, keep)
+        else:
+            for f in ("k", "v", "pos"):
+                c.own[f + "_gpu"][0, 1, :, :n] = torch.from_numpy(np.ascontiguousarray(c.own[f][1, :, :n])).to(c.own[f + "_gpu"].dtype).cuda()
+    check(run(B, c), c.want(roundings=roundings(c)))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
 @pytest.mark.parametrize("tokens", [(1, 1, 1, 1, 1, 1), (2, 1, 5, 1, 3, 2), (40, 20, 1, 9, 3, 2)])
 @pytest.mark.parametrize("prefix,groups", [((500,), (0, 6)), ((70, 1, 300), (0, 2, 3, 6)), ((40, 0), (0, 6, 6)), ((1000, 33), (0, 1, 6))])
 def test_shared(dtype, tokens, prefix, groups):
