@@ -6,6 +6,7 @@ namespace tri {
 namespace {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 typedef __attribute__((address_space(3))) void lds_void;
@@ -33,24 +34,53 @@ __device__ __forceinline__ void rotate_q(float (*x)[8], int32_t pos, int h, cons
         }
 }
 
+// What is done to keys on their way to the first product.  What has been turned is no bf16 number any more, and where scores are large, rounding it to one shows: outputs 0.0064 and 0.0071 off (root mean square, relative;
+// two pre-RoPE caches) and 0.0034 (q alone turned), where the outputs' own rounding is 0.0017.  The product then runs in fp16, three bits more at the same rate: 0.0021, 0.0022 and 0.0023, for 70 -> 80, 47 -> 53 and
+// 28 -> 31 us.  Rows of q are brought to [1, 2) by a power of two, those of K only where fp16 would not hold them, and the scores get the powers back.
+enum Keys { kAsTheyAre, kWiden, kTurn };   // q as it came; q turned, keys bf16 numbers made fp16; both turned
+
+// The power of two that x / unit_of(x) has a magnitude of [1, 2) with, for x of at least 2^-113; infinities and NaN stay what they are.
+__device__ __forceinline__ float unit_of(float x)
+{
+    const int e = (int)((__float_as_uint(x) >> 23) & 255) - 127;
+    return x == 0.f ? 1.f : __uint_as_float((uint32_t)(min(max(e, -113), 113) + 127) << 23);
+}
+__device__ __forceinline__ float over(float unit) { return __uint_as_float((254u << 23) - __float_as_uint(unit)); }   // 1 / unit
+__device__ __forceinline__ bf16x8 narrow_f16(const float *x, float by)   // (the bits; the type is that of all operands)
+{
+    f16x8 u;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) u[e] = (_Float16)(x[e] * by);
+    return __builtin_bit_cast(bf16x8, u);
+}
+
+template <bool F16>
+__device__ __forceinline__ f32x16 scores(bf16x8 k, bf16x8 q, f32x16 sum)
+{
+    if constexpr (F16) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, k), __builtin_bit_cast(f16x8, q), sum, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q, sum, 0, 0, 0);
+}
+
 struct TileBuffer {
     __bf16 k[kTileKeys * kHeadDim], v[kTileKeys * kHeadDim];
     int32_t pos[kTileKeys];
-    int32_t lim[3 * kWaves];   // of every wave's keys: highest and lowest position, and which are there (a bit each)
+    float unit[kTileKeys];     // fp16: what a key's scores are multiplied by
+    int32_t lim[3 * kWaves];   // of every wave's keys: highest and lowest position, and which are there (a bit each; bit 16: a unit is not one)
 };
 
 // A workgroup has four waves of 32 rows each (token, query head of the group) and goes through the keys 64 at a time, K and V lying in LDS for all four.  S^T[key][row] = K Q^T and
 // O^T[dim][row] = V^T P^T run on v_mfma_f32_32x32x16_bf16: a row is a lane's column throughout, so its maximum and sum are in-lane but for one exchange of the lane's halves, and the weights are the second product's
 // operand where the first leaves its scores (lane half h holds keys 8 (i / 4) + 4 h + i % 4; the V operand takes its keys in that order, from transposing LDS reads).  K and V go from memory to LDS without passing
-// through registers; a tile's loads are under way while the last one is worked on.  q (turned by its position), keys turned on the way and the weights are rounded to bf16 once: more bits would double the first
-// product or the LDS that keys take, and a cache of turned keys holds the same.
+// through registers; a tile's loads are under way while the last one is worked on.  The weights are rounded to bf16 once,
+// an error of its own for every key.
 // Measured: two chunks of 1024 tokens over up to 8192 keys in pages of 64, 8 x 4 heads, 227 GFLOP: 262 us, 870 TFLOP/s (a library product of 8192 x 8192 matrices runs at 1355 here).  The matrix pipe is busy 36 % of the
 // time, the vector pipe with softmax 42 %, LDS 33 %, and the two hardly overlap: a wave issues in order, and there are two to a SIMD.  64 rows to a wave (one to a SIMD) took 577 us when 32 took
 // 322, eight waves to a workgroup 382; the loads' issue is a quarter of the time (without them, on stale tiles, 245 of 322).  Without neighbours on one XCD two prompts' 256 sequences take 379 us, with 229.
-template <int PAGES, bool TURN, bool HALF>
+template <int PAGES, Keys KEYS, bool HALF>
 __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs a)
 {
-    constexpr int kLanes = 64 / kKeys, kPieces = 16 / kLanes;   // TURN: lanes to a row of K, pieces to a lane
+    constexpr bool TURN = KEYS == kTurn, F16 = KEYS != kAsTheyAre;
+    constexpr int kLanes = 64 / kKeys, kPieces = 16 / kLanes;   // F16: lanes to a row of K, pieces to a lane
     __shared__ __align__(16) uint64_t turns[kBands];
     // (two objects and two copies of the loop's body: the compiler then knows that reading one does not have to wait for the loads into the other)
     __shared__ __align__(16) TileBuffer buf0, buf1;
@@ -147,39 +177,51 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
                 for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4 *>(to.v + (kKeys * wave + (l >> 2)) * kHeadDim + 8 * ((l & 3) + 4 * i)) = make_uint4(0, 0, 0, 0);
             }
         }
-        if (TURN) {
-            const int row = lane / kLanes, turn_pos = __shfl(pos_new, row);
+        bool scaled = false;
+        if (F16) {
+            __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
+            const int row = lane / kLanes;
             bf16x8 *k = reinterpret_cast<bf16x8 *>(to.k + (kKeys * wave + row) * kHeadDim);
             float v[kPieces][8];
 #pragma unroll
             for (int i = 0; i < kPieces; ++i) widen8(__builtin_bit_cast(uint4, k[(lane % kLanes + kLanes * i) ^ row]), v[i]);
+            if (TURN) {
+                const int turn_pos = __shfl(pos_new, row);
 #pragma unroll
-            for (int i = 0; i < (HALF ? kPieces / 2 : kPieces); ++i)
+                for (int i = 0; i < (HALF ? kPieces / 2 : kPieces); ++i)
 #pragma unroll
-                for (int e = 0; e < (HALF ? 8 : 4); ++e) {
-                    const int piece = lane % kLanes + kLanes * i;
-                    const uint64_t t = turns[HALF ? 8 * piece + e : 4 * piece + e];
-                    float cs, sn;
-                    turn_fast(phase_of(turn_pos, (uint32_t)t, (uint32_t)(t >> 32)), &cs, &sn);
-                    float &r = HALF ? v[i][e] : v[i][2 * e], &im = HALF ? v[(i + kPieces / 2) % kPieces][e] : v[i][(2 * e + 1) & 7];
-                    const float re = r, im0 = im;
-                    r = fmaf(re, cs, -(im0 * sn));
-                    im = fmaf(re, sn, im0 * cs);
-                }
-#pragma unroll
-            for (int i = 0; i < kPieces; ++i) {
-                bf16x8 u;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) u[e] = (__bf16)v[i][e];
-                k[(lane % kLanes + kLanes * i) ^ row] = u;
+                    for (int e = 0; e < (HALF ? 8 : 4); ++e) {
+                        const int piece = lane % kLanes + kLanes * i;
+                        const uint64_t t = turns[HALF ? 8 * piece + e : 4 * piece + e];
+                        float cs, sn;
+                        turn_fast(phase_of(turn_pos, (uint32_t)t, (uint32_t)(t >> 32)), &cs, &sn);
+                        float &r = HALF ? v[i][e] : v[i][2 * e], &im = HALF ? v[(i + kPieces / 2) % kPieces][e] : v[i][(2 * e + 1) & 7];
+                        const float re = r, im0 = im;
+                        r = fmaf(re, cs, -(im0 * sn));
+                        im = fmaf(re, sn, im0 * cs);
+                    }
             }
+            float most = 0.f, unit = 1.f;
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(v[i][e]));
+#pragma unroll
+            for (int i = 1; i < kLanes; i *= 2) most = fmaxf(most, __shfl_xor(most, i));
+            // fp16 as it is from 2^-6 (below 2^-14 of it bits are lost, 2^-19 of the row's largest at most) to 2^15
+            scaled = __ballot(most >= 0x1p15f || (most < 0x1p-6f && most > 0.f));
+            if (scaled) unit = unit_of(most);
+            const float by = over(unit);
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) k[(lane % kLanes + kLanes * i) ^ row] = narrow_f16(v[i], by);
+            if (lane % kLanes == 0) to.unit[kKeys * wave + row] = unit;
         }
         const bool there = (there_new >> (lane % kKeys)) & 1;   // (lanes kKeys apart hold the same)
         int32_t hi = there ? pos_new : -0x7fffffff - 1, lo = there ? pos_new : 0x7fffffff;
 #pragma unroll
         for (int i = 1; i < kKeys; i *= 2) hi = max(hi, __shfl_xor(hi, i)), lo = min(lo, __shfl_xor(lo, i));
         if (lane < kKeys) to.pos[kKeys * wave + lane] = pos_new;
-        if (lane == 0) to.lim[wave] = hi, to.lim[kWaves + wave] = lo, to.lim[2 * kWaves + wave] = there_new;
+        if (lane == 0) to.lim[wave] = hi, to.lim[kWaves + wave] = lo, to.lim[2 * kWaves + wave] = there_new | (uint32_t)scaled << 16;
     };
 
     // The first tile is asked for before anything is known of the queries.
@@ -197,18 +239,24 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
     const int32_t t_pos = a.causal ? a.pos[t] : 0x7fffffff;
     int32_t first_pos = t_pos, last_pos = real ? t_pos : -0x7fffffff - 1;
     bf16x8 q[8];
+    float unit = 1.f;   // of the row's q
     {
         const char *p = a.q + ((int64_t)t * a.q_stride_token + (int64_t)hq * a.q_stride_head) * 2 + 16 * h;
-        if (a.rotate_q) {
-            float v[8][8];
+        if (F16) {
+            float v[8][8], most = 0.f;
 #pragma unroll
             for (int j = 0; j < 8; ++j) widen8(*reinterpret_cast<const uint4 *>(p + 32 * j), v[j]);
-            if (TURN ? HALF : (bool)a.half) rotate_q<true>(v, a.pos[t], h, turns);
-            else rotate_q<false>(v, a.pos[t], h, turns);
+            if (a.rotate_q) {
+                if (TURN ? HALF : (bool)a.half) rotate_q<true>(v, a.pos[t], h, turns);
+                else rotate_q<false>(v, a.pos[t], h, turns);
+            }
 #pragma unroll
             for (int j = 0; j < 8; ++j)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) q[j][e] = (__bf16)v[j][e];
+                for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(v[j][e]));
+            unit = unit_of(fmaxf(most, __shfl_xor(most, 32)));
+#pragma unroll
+            for (int j = 0; j < 8; ++j) q[j] = narrow_f16(v[j], over(unit));
         } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j) q[j] = *reinterpret_cast<const bf16x8 *>(p + 32 * j);
@@ -266,8 +314,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
     const uint32_t at_k = col * 256 + (h ^ (col & 15)) * 16;
     const uint32_t at_v = row_v0 * 256 + (((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ (2 * row_v0)) * 16) + (lane & 1) * 8;
 
-    // mask: some of the tile's keys are not everyone's
-    auto compute = [&](const TileBuffer &from, const bool mask) __attribute__((always_inline)) {
+    // mask: some of the tile's keys are not everyone's; scaled: some have units
+    auto compute = [&](const TileBuffer &from, const bool mask, const bool scaled) __attribute__((always_inline)) {
         uint32_t ak = at_k, av = at_v;
         fresh(ak), fresh(av);
         f32x16 sc[2];
@@ -294,12 +342,19 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
         __builtin_amdgcn_sched_barrier(0);   // all reads under way before the first product waits for one
         __builtin_amdgcn_s_setprio(1);   // (the products of a wave go before the other's softmax: 263 -> 258 us for two chunks of 1024 tokens over 8192 keys)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[0][j], q[j], sc[0], 0, 0, 0);
+        for (int j = 0; j < 8; ++j) sc[0] = scores<F16>(k[0][j], q[j], sc[0]);
         values(0);   // asked for ahead of the softmax
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sc[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[1][j], q[j], sc[1], 0, 0, 0);
+        for (int j = 0; j < 8; ++j) sc[1] = scores<F16>(k[1][j], q[j], sc[1]);
         __builtin_amdgcn_s_setprio(0);
+        if (F16 && scaled) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sc[u][i] *= from.unit[32 * u + 8 * (i / 4) + 4 * h + i % 4];
+        }
+        const float scale = F16 ? a.scale_log2 * unit : a.scale_log2;
         uint32_t keep = ~0u;   // bit 16 u + i: key 32 u + 8 (i / 4) + 4 h + i % 4 is attended to
         bool hole = false;
         if (mask) {
@@ -329,15 +384,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
         const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(best), __float_as_uint(best), false, false);
         best = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
         // weights are relative to a maximum that scores may pass by a factor of 2^8 before the sums are brought to the new one
-        if (__ballot(best > top && !((best - top) * a.scale_log2 <= kStaleBits))) {
+        if (__ballot(best > top && !((best - top) * scale <= kStaleBits))) {
             const float next = fmaxf(top, best);
-            const float shrink = next == kNoScore ? 1.f : __builtin_amdgcn_exp2f((top - next) * a.scale_log2);
+            const float shrink = next == kNoScore ? 1.f : __builtin_amdgcn_exp2f((top - next) * scale);
             top = next;
             sum *= shrink;
 #pragma unroll
             for (int j = 0; j < 4; ++j) o[j] *= shrink;
         }
-        const float off = (top == kNoScore ? 0.f : top) * a.scale_log2;
+        const float off = (top == kNoScore ? 0.f : top) * scale;
         const bool holes = __ballot(hole);
 #pragma unroll
         for (int U = 0; U < 2; ++U) {
@@ -345,7 +400,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
             if (U == 1) values(1);
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                const float p = __builtin_amdgcn_exp2f(fmaf(sc[U][i], a.scale_log2, -off));
+                const float p = __builtin_amdgcn_exp2f(fmaf(sc[U][i], scale, -off));
                 sum += p;
                 weight[i / 8][i % 8] = (__bf16)p;
             }
@@ -404,7 +459,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
             for (int i = 0; i < kWaves; ++i)
                 hi = max(hi, __builtin_amdgcn_readlane(lim, i)), lo = min(lo, __builtin_amdgcn_readlane(lim, kWaves + i)), any |= __builtin_amdgcn_readlane(lim, 2 * kWaves + i), all &= __builtin_amdgcn_readlane(lim, 2 * kWaves + i);
             // (nothing to do where no key is there, or all are behind the last position of the wave's rows)
-            if (any && lo <= last_pos) compute(here, all != 0xffff || hi > first_pos);
+            if ((any & 0xffff) && lo <= last_pos) compute(here, all != 0xffff || hi > first_pos, any >> 16);
         }
         if (more) put(next);
         k0 += kTileKeys;
@@ -417,7 +472,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
     if (!real) return;
     if (a.part_o) {
         const int64_t row = ((int64_t)(a.src.part0 + split) * a.n_tokens + t) * Hq + hq;
-        if (h == 0) a.part_ml[row] = make_float2(top, total);
+        if (h == 0) a.part_ml[row] = make_float2(top * unit, total);
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -448,9 +503,11 @@ tri_status launch_attend_tile(AttendArgs a, int32_t rows, hipStream_t st)
     const uint32_t blocks = (uint32_t)((groups + 7) / 8 * 8 * a.row_tiles);
     const int shift = a.src.cache.block_shift, pages = shift < 0 ? 0 : shift >= 4 ? 1 : 2;
     const auto launch = [&](auto kernel) { kernel<<<blocks, 64 * kWaves, 0, st>>>(a); };
-    if (a.src.cache.k_rotated) launch(pages == 0 ? attend_tile_kernel<0, false, false> : pages == 1 ? attend_tile_kernel<1, false, false> : attend_tile_kernel<2, false, false>);
-    else if (a.half) launch(pages == 0 ? attend_tile_kernel<0, true, true> : pages == 1 ? attend_tile_kernel<1, true, true> : attend_tile_kernel<2, true, true>);
-    else launch(pages == 0 ? attend_tile_kernel<0, true, false> : pages == 1 ? attend_tile_kernel<1, true, false> : attend_tile_kernel<2, true, false>);
+    const auto of = [&](auto direct, auto paged, auto small) { pages == 0 ? launch(direct) : pages == 1 ? launch(paged) : launch(small); };
+    if (!a.src.cache.k_rotated && a.half) of(attend_tile_kernel<0, kTurn, true>, attend_tile_kernel<1, kTurn, true>, attend_tile_kernel<2, kTurn, true>);
+    else if (!a.src.cache.k_rotated) of(attend_tile_kernel<0, kTurn, false>, attend_tile_kernel<1, kTurn, false>, attend_tile_kernel<2, kTurn, false>);
+    else if (a.rotate_q) of(attend_tile_kernel<0, kWiden, false>, attend_tile_kernel<1, kWiden, false>, attend_tile_kernel<2, kWiden, false>);
+    else of(attend_tile_kernel<0, kAsTheyAre, false>, attend_tile_kernel<1, kAsTheyAre, false>, attend_tile_kernel<2, kAsTheyAre, false>);
     return hip_status("attend_tile_kernel");
 }
 

@@ -306,3 +306,53 @@ def test_same_bits_every_time():
         first = run(B, c)
         for _ in range(3):
             assert torch.equal(run(B, c), first)
+
+
+def exact_and_expected(c, scale):
+    """The output in 64 bits, and the mean square that a row's error may have: output and weights rounded to bf16 (each off by at most 2^-8 of the value, evenly: a third of its square), q and turned keys to fp16 (2^-11), each
+    rounding by itself; a score's error moves the output by weight x (value - output)."""
+    out, square = np.zeros((c.T, c.H * c.G, 128)), np.zeros((c.T, c.H * c.G))
+    q = P.turn(c.q, np.broadcast_to(c.pos[:, None], c.q.shape[:2]), c.theta, c.pairs)
+    n = c.own["total"][0]
+    for hq in range(c.H * c.G):
+        k, v, pos = (c.own[f][0, hq // c.G, :n] for f in ("k", "v", "pos"))
+        if not c.stored_rotated:
+            k = P.turn(k, pos, c.theta, c.pairs)
+        s = np.where(pos[None] <= c.pos[:, None], scale * q[:, hq] @ k.T, -np.inf)
+        w = np.exp(s - s.max(1, keepdims=True))
+        w /= w.sum(1, keepdims=True)
+        o = out[:, hq] = w @ v
+        score = scale ** 2 * ((q[:, hq] ** 2) @ (k ** 2).T) * (1 if c.stored_rotated else 2) * 2.0 ** -22 / 3
+        apart = (v ** 2).sum(1)[None] - 2 * o @ v.T + (o ** 2).sum(1, keepdims=True)
+        square[:, hq] = (w ** 2 * (score + 2.0 ** -16 / 3) * apart).sum(1) + 2.0 ** -16 / 3 * (o ** 2).sum(1)
+    return out, square
+
+
+@pytest.mark.parametrize("stored", [False, True], ids=["pre", "post"])
+@pytest.mark.parametrize("tokens,block,pairs", [(3, 0, 0), (8, 16, 1), (60, 0, 0), (60, 64, 1), (60, 4, 0)])
+def test_large_scores_keep_their_digits(tokens, block, pairs, stored):
+    """Scores whose terms are several times 1: what q and turned keys are rounded to shows in the error of all outputs together."""
+    from paper_2604_04921_amd import binding as B
+    c = P.Case(91, (1500,), (tokens,), G=4, layers=1, layer=0, stored_rotated=stored, block=block, pairs=pairs)
+    ref, square = exact_and_expected(c, 0.3)
+    got = run(B, c, scale=0.3)
+    torch.cuda.synchronize()
+    off = ((got.double().cpu().numpy() - ref) ** 2).sum()
+    print("%.5f of %.5f" % (np.sqrt(off / (ref ** 2).sum()), np.sqrt(square.sum() / (ref ** 2).sum())))
+    assert off <= square.sum()
+
+
+@pytest.mark.parametrize("stored", [False, True], ids=["pre", "post"])
+@pytest.mark.parametrize("power", [-60, -20, 13, 20, 100])
+@pytest.mark.parametrize("tokens", [(3,), (60,)])
+def test_magnitudes(tokens, power, stored):
+    """Keys that fp16 does not hold, large and small, beside a third that is 2^-40 times the others and some zeros; queries the other way round."""
+    from paper_2604_04921_amd import binding as B
+    c = P.Case(92, (700,), tokens, layers=1, layer=0, stored_rotated=stored)
+    by = np.ldexp(1.0, power - 40 * (np.arange(c.own["cap"]) % 3 == 1))
+    by[::50] = 0
+    c.own["k"] *= by[:, None]
+    c.own["k_gpu"] *= torch.from_numpy(by).float().cuda()[:, None]
+    c.q, c.q_gpu = np.ldexp(c.q, -power), torch.ldexp(c.q_gpu.float(), torch.tensor(-power, device="cuda")).to(c.dtype)
+    c.own["k_gpu"] = c.own["k_gpu"].to(c.dtype)
+    check(run(B, c), c.want(roundings=roundings(c)))
