@@ -444,8 +444,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
     __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0): no load into LDS is under way when the workgroup ends without a tile
     if (k0 < k_hi) put(buf0);
     auto step = [&](TileBuffer &here, TileBuffer &next) __attribute__((always_inline)) {
-        // This tile has come, and the last one is read.  The wait is said here: a barrier alone waits for a wave's own LDS accesses, not for its loads into LDS.
-        __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
+        // This tile has come, what put() wrote of it is there, and the last one is read.  Both waits are said here.  A barrier does not wait for loads into LDS; and the wait for the wave's own LDS writes, which
+        // the compiler sets ahead of barriers, it left out of this one on the way round the loop: other waves then met limits and positions of the tile before the last, or keys half turned.
+        __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0) lgkmcnt(0)
         __syncthreads();
         const bool more = k0 + kTileKeys < k_hi;
         if (more) {
