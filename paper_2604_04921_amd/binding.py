@@ -124,14 +124,14 @@ def _check(rc):
 
 
 def _p(t):
-    return None if t is None else ctypes.c_void_p(t.data_ptr())
+    return None if t is None else t.data_ptr()
 
 
 def _stream(stream):
     if stream is None:
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # (the current stream's handle without an object around it: 1 us of a call)
-        return ctypes.c_void_p(raw(-1) if raw is not None else torch.cuda.current_stream().cuda_stream)
-    return ctypes.c_void_p(stream.cuda_stream)
+        return raw(-1) if raw is not None else torch.cuda.current_stream().cuda_stream
+    return stream.cuda_stream
 
 
 def _dtype(t):
@@ -155,10 +155,8 @@ class Model:
         self.c = TriModel(n_layers, n_q_heads, n_kv_heads, head_dim, float(rope_theta), pairs, len(self._offsets),
                           self._offsets.ctypes.data_as(ctypes.c_void_p), int(score_variant),
                           None if head_budgets is None else head_budgets.data_ptr())
-
-    @property
-    def ref(self):
-        return ctypes.byref(self.c)
+        self.n_layers, self.n_q_heads, self.n_kv_heads, self.head_dim = n_layers, n_q_heads, n_kv_heads, head_dim   # (a field of the struct costs a call 0.1 us)
+        self.ref = ctypes.byref(self.c)
 
 
 class Cache:
@@ -173,6 +171,7 @@ class Cache:
         assert v is None or (v.stride() == k.stride() and v.dtype == k.dtype)
         assert pos.dtype == torch.int32 and seq_len.dtype == torch.int32 and cur_pos.dtype == torch.int32
         self.tensors = (k, v, pos, seq_len, cur_pos, block_table)
+        self.n_seqs, self.dtype, self.device = seq_len.numel(), k.dtype, k.device
         bs = 0 if block_table is None else k.shape[3]
         self.c = TriCache(k.data_ptr(), 0 if v is None else v.data_ptr(), pos.data_ptr(), _dtype(k),
                           seq_len.numel(), seq_len.data_ptr(), cur_pos.data_ptr(), int(max_seq_len), bs,
@@ -183,10 +182,7 @@ class Cache:
                           0 if block_table is None else k.shape[1])
         if block_table is not None:
             assert block_table.dtype == torch.int32 and block_table.is_contiguous()
-
-    @property
-    def ref(self):
-        return ctypes.byref(self.c)
+        self.ref = ctypes.byref(self.c)
 
 
 class Tokens:
@@ -199,51 +195,95 @@ class Tokens:
         for t in (pos, start, head_len):
             assert t is None or (t.dtype == torch.int32 and t.is_contiguous())
         self.tensors = (pos, start, head_len)
-        n = pos.numel()
+        self.n_tokens = n = pos.numel()
+        self.starts, self.head_shape, self.device = None if start is None else start.numel(), None if head_len is None else tuple(head_len.shape), pos.device
+        for t in (start, head_len):
+            if t is not None and t.device != pos.device:
+                raise ValueError("start and head_len must lie where pos does, on %s" % pos.device)
         self.c = TriTokens(n, n if max_tokens is None else int(max_tokens), None if start is None else start.data_ptr(), pos.data_ptr(),
                            None if head_len is None else head_len.data_ptr(), int(bool(rotated)))
         self.ref = ctypes.byref(self.c)
 
 
+def _here(t, cache, name):
+    if t.device != cache.device:
+        raise ValueError("%s: on %s, the cache on %s" % (name, t.device, cache.device))
+
+
 def _rows(t, heads, tokens, cache, name):
-    """Strides of rows [T][heads][d] of the cache's type, d dense; any strides of the other two."""
-    strides = t.stride()
-    if t.shape != (tokens.c.n_tokens, heads, 128) or strides[2] != 1:
-        raise ValueError("%s: [%d][%d][128] with dense rows, got %s" % (name, tokens.c.n_tokens, heads, tuple(t.shape)))
-    if t.dtype != cache.tensors[0].dtype:
-        raise TypeError("%s: %s, the cache holds %s" % (name, t.dtype, cache.tensors[0].dtype))
+    """Strides of rows [T][heads][d] of the cache's type and device, d dense; any strides of the other two (0 where there is one token, or head)."""
+    n, strides = tokens.n_tokens, t.stride()
+    if t.shape != (n, heads, 128) or strides[2] != 1:
+        raise ValueError("%s: [%d][%d][128] with dense rows, got %s" % (name, n, heads, tuple(t.shape)))
+    if t.dtype != cache.dtype:
+        raise TypeError("%s: %s, the cache holds %s" % (name, t.dtype, cache.dtype))
+    if t.device != cache.device:
+        _here(t, cache, name)
+    if n == 1 or heads == 1:
+        return strides[0] if n > 1 else 0, strides[1] if heads > 1 else 0
     return strides
 
 
+def _fits(model, cache, tokens):
+    """What the kernels take on trust of the step's arrays: their sizes, and that they lie where the cache does."""
+    if tokens.starts is not None and tokens.starts <= cache.n_seqs:
+        raise ValueError("start: %d entries, not n_seqs + 1 = %d" % (tokens.starts, cache.n_seqs + 1))
+    if tokens.head_shape is not None:
+        got, shape = tokens.head_shape, (model.n_layers, cache.n_seqs, model.n_kv_heads)
+        if got != shape and got != (shape[0] * shape[1] * shape[2],):
+            raise ValueError("head_len: %s, not %s" % (got, shape))
+    if tokens.device != cache.device:
+        _here(tokens, cache, "the step's tokens")
+
+
+def _bytes(workspace, cache):
+    if workspace is None:
+        return 0
+    _here(workspace, cache, "workspace")
+    if not workspace.is_contiguous():
+        raise ValueError("workspace: must be contiguous")
+    return workspace.numel() * workspace.element_size()
+
+
 def tri_append(model, cache, layer, tokens, k_new, v_new, new_seq_len=None, stream=None):
-    """k_new, v_new [T][Hkv][d], with the same strides, to the end of every sequence of layer `layer`."""
-    strides = _rows(k_new, model.c.n_kv_heads, tokens, cache, "k_new")
-    if _rows(v_new, model.c.n_kv_heads, tokens, cache, "v_new") != strides:
+    """k_new, v_new [T][Hkv][d], with the same strides, to the end of every sequence of layer `layer`.  new_seq_len int32 [S] or None."""
+    strides = _rows(k_new, model.n_kv_heads, tokens, cache, "k_new")
+    if _rows(v_new, model.n_kv_heads, tokens, cache, "v_new") != strides:
         raise ValueError("k_new and v_new must have the same strides")
+    _fits(model, cache, tokens)
+    if new_seq_len is not None:
+        _here(new_seq_len, cache, "new_seq_len")
+        if new_seq_len.dtype != torch.int32:
+            raise TypeError("new_seq_len: int32, got %s" % new_seq_len.dtype)
+        if new_seq_len.numel() < cache.n_seqs or not new_seq_len.is_contiguous():
+            raise ValueError("new_seq_len: %d entries side by side, got %s" % (cache.n_seqs, tuple(new_seq_len.shape)))
     _check(lib().tri_append(model.ref, cache.ref, layer, tokens.ref, k_new.data_ptr(), v_new.data_ptr(), strides[0], strides[1],
                             _p(new_seq_len), _stream(stream)))
 
 
 def _attention(model, cache, tokens, q, out, scale, causal):
-    heads = model.c.n_q_heads
+    _fits(model, cache, tokens)
+    heads = model.n_q_heads
     qs, os_ = _rows(q, heads, tokens, cache, "q"), _rows(out, heads, tokens, cache, "out")
-    return TriAttention(q.data_ptr(), out.data_ptr(), qs[0], qs[1], os_[0], os_[1], model.c.head_dim ** -0.5 if scale is None else scale,
+    return TriAttention(q.data_ptr(), out.data_ptr(), qs[0], qs[1], os_[0], os_[1], model.head_dim ** -0.5 if scale is None else scale,
                         1 if causal else 0)
 
 
 def tri_attend(model, cache, layer, tokens, q, out, scale=None, causal=True, workspace=None, stream=None):
     """out [T][Hq][d] <- attention of q [T][Hq][d] over layer `layer` of the cache.  scale None: 1 / sqrt(d)."""
     at = _attention(model, cache, tokens, q, out, scale, causal)
-    _check(lib().tri_attend(model.ref, cache.ref, layer, tokens.ref, ctypes.byref(at), _p(workspace),
-                            0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)))
+    _check(lib().tri_attend(model.ref, cache.ref, layer, tokens.ref, ctypes.byref(at), _p(workspace), _bytes(workspace, cache), _stream(stream)))
 
 
 def tri_attend_shared(model, prefix, group, cache, layer, tokens, q, out, scale=None, causal=True, workspace=None, stream=None):
     """tri_attend with the keys of shared prefixes: group int32 [P + 1] (first sequence of every prefix's), None for one prefix."""
     assert group is None or (group.dtype == torch.int32 and group.is_contiguous() and group.numel() == prefix.c.n_seqs + 1)
     at = _attention(model, cache, tokens, q, out, scale, causal)
+    _here(prefix, cache, "prefix")
+    if group is not None:
+        _here(group, cache, "group")
     _check(lib().tri_attend_shared(model.ref, prefix.ref, _p(group), cache.ref, layer, tokens.ref, ctypes.byref(at), _p(workspace),
-                                   0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)))
+                                   _bytes(workspace, cache), _stream(stream)))
 
 
 def tri_attend_workspace_size(model, cache, tokens, prefix=None):
