@@ -157,10 +157,11 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a)
 
 }  // namespace
 
+int64_t append_threads(int64_t rows, int32_t dtype) { return rows * (dtype == TRI_BF16 ? 8 : 16); }
+
 tri_status launch_append(const AppendArgs &a, int32_t dtype, hipStream_t st)
 {
-    const int64_t per_row = dtype == TRI_BF16 ? 8 : 16;
-    const int64_t threads = std::max<int64_t>((int64_t)a.n_tokens * a.cache.n_kv_heads * per_row, a.new_seq_len ? a.cache.n_seqs : 0);
+    const int64_t threads = std::max<int64_t>(append_threads((int64_t)a.n_tokens * a.cache.n_kv_heads, dtype), a.new_seq_len ? a.cache.n_seqs : 0);
     if (threads == 0) return TRI_OK;
     const uint32_t blocks = (uint32_t)((threads + kAppendThreads - 1) / kAppendThreads);
     if (dtype == TRI_BF16) append_kernel<__bf16><<<blocks, kAppendThreads, 0, st>>>(a);

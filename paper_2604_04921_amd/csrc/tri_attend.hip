@@ -367,6 +367,14 @@ static Kernel kernel_of(const tri_cache &c, int64_t rows)
 // rows leave room for, are worth more (two chunks of 256 tokens over 4352 keys 295 us with 16, 371 with 32).
 static int64_t general_rows(const tri_cache &c, int64_t rows) { return c.dtype == TRI_F32 && rows > 16 && rows <= 32 ? 32 : 16; }
 
+// Row tiles of a sequence, and workgroups of a cache's launch: those of row tiles in whole rounds over the eight XCDs.
+static int64_t row_tiles_of(Kernel kernel, const tri_cache &c, int64_t rows)
+{
+    const int64_t per_tile = kernel == Kernel::general ? general_rows(c, rows) : kernel == Kernel::tile ? kTileRows : rows;
+    return (rows + per_tile - 1) / per_tile;
+}
+static int64_t groups_of(Kernel kernel, int64_t heads, int64_t row_tiles) { return kernel == Kernel::rows ? heads : (heads + 7) / 8 * 8 * row_tiles; }
+
 // Parts.  Two workgroups of either bf16 kernel share a CU, so 512 of them fill the GPU; more even out ragged batches, and each costs what 100 to 200 keys do, and the joining of its
 // results.  Measured, us by parts per head, 8 KV heads, G = 4, bf16 single tokens: 16 x 65536 keys 1023 / 630 / 642 / 637 / 661 / 850 at 1, 2, 8, 16, 48, 128 parts; 16 sequences between
 // 1000 and 65536 keys 938 / 526 / 438 / 399 / 418 / 523 at the same; 16 x 4096 69 / 49 / 61 / 71 at 1, 2, 8, 16; 64 x 2176 90 / 98 / 143 at 1, 2, 8; one of 131072 at G = 8 201 / 114 / 96 /
@@ -374,7 +382,7 @@ static int64_t general_rows(const tri_cache &c, int64_t rows) { return c.dtype =
 // 1253 / 351 / 133 / 111 at 1, 4, 16, 32; two chunks of 1024 tokens over 8192 keys, 480 row tiles, 321 / 364 / 387 at 1, 2, 4; one of 512 over 16384 400 / 201 / 169 / 182 at 1, 3, 4, 8.
 // So: 512 workgroups, or parts of 2800 keys (1400 in fp32, 8192 for row tiles) where that makes more; none below the keys that `least` gives, which the device goes by where the lengths
 // turn out shorter than max_seq_len.
-void attend_split(const tri_model &m, const tri_cache &c, int32_t max_tokens, int32_t n_tokens, int32_t *n_split, int32_t *least_keys)
+AttendSplit attend_split(const tri_model &m, const tri_cache &c, int32_t max_tokens, int32_t n_tokens)
 {
     const int64_t G = m.n_q_heads / m.n_kv_heads, rows = max_tokens * G;
     const Kernel kernel = kernel_of(c, rows);
@@ -387,8 +395,11 @@ void attend_split(const tri_model &m, const tri_cache &c, int32_t max_tokens, in
     const int64_t fill = std::max<int64_t>(1, (512 + units / 2) / units);
     int64_t want = std::max<int64_t>(fill, c.max_seq_len / part);
     if (want * units < 2048) want = want / fill * fill;   // (few rounds: whole ones; 4 x 30238 keys in fp32 178 us with 16 parts, 210 with 21)
-    *least_keys = (int32_t)least;
-    *n_split = (int32_t)std::max<int64_t>(1, std::min<int64_t>({want, (c.max_seq_len + least - 1) / least, 256}));
+    AttendSplit s;
+    s.least_keys = (int32_t)least;
+    s.n_split = (int32_t)std::max<int64_t>(1, std::min<int64_t>({want, (c.max_seq_len + least - 1) / least, 256}));
+    s.groups = groups_of(kernel, (int64_t)s.n_split * m.n_kv_heads * c.n_seqs, row_tiles_of(kernel, c, rows));
+    return s;
 }
 
 tri_status launch_attend(AttendArgs a, const tri_cache &c, hipStream_t st)
@@ -396,14 +407,12 @@ tri_status launch_attend(AttendArgs a, const tri_cache &c, hipStream_t st)
     const int64_t rows = (int64_t)a.src.max_tokens * a.group_size;
     const Kernel kernel = kernel_of(c, rows);
     if (kernel == Kernel::rows) return launch_attend_rows(a, (int32_t)rows, st);
-    if (kernel == Kernel::tile) return launch_attend_tile(a, (int32_t)rows, st);
-    const int64_t per_tile = general_rows(c, rows);
-    a.row_tiles = (int32_t)((rows + per_tile - 1) / per_tile);
-    const int64_t groups = (int64_t)a.src.n_split * a.src.cache.n_kv_heads * a.src.cache.n_seqs;
-    const uint32_t blocks = (uint32_t)((groups + 7) / 8 * 8 * a.row_tiles);
-    const auto launch = [&](auto kernel) { kernel<<<blocks, kAttendThreads, 0, st>>>(a); };
+    a.row_tiles = (int32_t)row_tiles_of(kernel, c, rows);
+    const uint32_t blocks = (uint32_t)groups_of(kernel, (int64_t)a.src.n_split * a.src.cache.n_kv_heads * a.src.cache.n_seqs, a.row_tiles);
+    if (kernel == Kernel::tile) return launch_attend_tile(a, blocks, st);
+    const auto launch = [&](auto variant) { variant<<<blocks, kAttendThreads, 0, st>>>(a); };
     if (c.dtype == TRI_BF16) launch(c.k_rotated ? attend_general_kernel<__bf16, 1, false, false> : a.half ? attend_general_kernel<__bf16, 1, true, true> : attend_general_kernel<__bf16, 1, true, false>);
-    else if (per_tile == 16) launch(c.k_rotated ? attend_general_kernel<float, 1, false, false> : a.half ? attend_general_kernel<float, 1, true, true> : attend_general_kernel<float, 1, true, false>);
+    else if (general_rows(c, rows) == 16) launch(c.k_rotated ? attend_general_kernel<float, 1, false, false> : a.half ? attend_general_kernel<float, 1, true, true> : attend_general_kernel<float, 1, true, false>);
     else launch(c.k_rotated ? attend_general_kernel<float, 2, false, false> : a.half ? attend_general_kernel<float, 2, true, true> : attend_general_kernel<float, 2, true, false>);
     return hip_status("attend_general_kernel");
 }
@@ -428,11 +437,14 @@ tri_status launch_attend_both(AttendArgs a, const tri_cache &c, const tri_cache 
     return launch_attend(a, other, st);
 }
 
+static bool join_spread(int32_t parts) { return parts > 8; }
+int64_t join_groups(int64_t rows, int32_t parts) { return join_spread(parts) ? rows : (rows + kAttendThreads / 16 - 1) / (kAttendThreads / 16); }
+
 tri_status launch_join(const AttendArgs &a, int32_t parts, int32_t n_q_heads, int32_t dtype, hipStream_t st)
 {
     const int64_t rows = (int64_t)a.n_tokens * n_q_heads;
-    const bool spread = parts > 8;
-    const uint32_t blocks = (uint32_t)(spread ? rows : (rows + kAttendThreads / 16 - 1) / (kAttendThreads / 16));
+    const bool spread = join_spread(parts);
+    const uint32_t blocks = (uint32_t)join_groups(rows, parts);
     const auto launch = [&](auto kernel) {
         kernel<<<blocks, kAttendThreads, 0, st>>>(a.part_o, a.part_ml, a.out, a.out_stride_token, a.out_stride_head, n_q_heads, rows, parts, a.scale_log2);
     };

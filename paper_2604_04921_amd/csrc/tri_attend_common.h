@@ -135,7 +135,7 @@ __device__ __forceinline__ void finish_row(const AttendArgs &a, const AttendSour
 }
 
 constexpr int kTileRows = 128;   // rows of a workgroup of the tile kernel
-tri_status launch_attend_tile(AttendArgs a, int32_t rows, hipStream_t st);
+tri_status launch_attend_tile(const AttendArgs &a, int64_t groups, hipStream_t st);
 tri_status launch_attend_rows(AttendArgs a, int32_t rows, hipStream_t st);   // a.src, and a.other where it has sequences
 
 }  // namespace tri

@@ -497,11 +497,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
 
 }  // namespace
 
-tri_status launch_attend_tile(AttendArgs a, int32_t rows, hipStream_t st)
+tri_status launch_attend_tile(const AttendArgs &a, int64_t groups, hipStream_t st)
 {
-    a.row_tiles = (rows + kRows - 1) / kRows;
-    const int64_t groups = (int64_t)a.src.n_split * a.src.cache.n_kv_heads * a.src.cache.n_seqs;
-    const uint32_t blocks = (uint32_t)((groups + 7) / 8 * 8 * a.row_tiles);
+    const uint32_t blocks = (uint32_t)groups;
     const int shift = a.src.cache.block_shift, pages = shift < 0 ? 0 : shift >= 4 ? 1 : 2;
     const auto launch = [&](auto kernel) { kernel<<<blocks, 64 * kWaves, 0, st>>>(a); };
     const auto of = [&](auto direct, auto paged, auto small) { pages == 0 ? launch(direct) : pages == 1 ? launch(paged) : launch(small); };

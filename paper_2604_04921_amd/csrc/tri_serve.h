@@ -116,8 +116,16 @@ __device__ __forceinline__ int keys_of(const AttendArgs &a, const AttendSource &
     return clamp_len(n, c.max_seq_len);
 }
 
-// How the keys of a cache are cut: ranges per head, and their least keys (a function of bounds alone, for the workspace's size).
-void attend_split(const tri_model &m, const tri_cache &c, int32_t max_tokens, int32_t n_tokens, int32_t *n_split, int32_t *least_keys);
+constexpr int64_t kMostGroups = 0xffffffffu / 256;   // workgroups of a launch, which are of 256 threads: HIP takes fewer than 2^32 threads on an axis
+
+// How the keys of a cache are cut: ranges per head, and their least keys (a function of bounds alone, for the workspace's size); the workgroups of its launch.
+struct AttendSplit {
+    int32_t n_split, least_keys;
+    int64_t groups;
+};
+AttendSplit attend_split(const tri_model &m, const tri_cache &c, int32_t max_tokens, int32_t n_tokens);
+int64_t join_groups(int64_t rows, int32_t parts);
+int64_t append_threads(int64_t rows, int32_t dtype);
 tri_status launch_attend(AttendArgs a, const tri_cache &c, hipStream_t st);   // (c: a.src's)
 // a.src and a.other, in one launch where that is worth it
 tri_status launch_attend_both(AttendArgs a, const tri_cache &c, const tri_cache &other, hipStream_t st);

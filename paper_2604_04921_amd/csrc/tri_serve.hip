@@ -8,8 +8,6 @@ namespace tri {
 
 namespace {
 
-constexpr int64_t kMostGroups = 0x7fffffff;   // workgroups of a launch, on its x axis
-
 int elem_bytes(const tri_cache &c) { return c.dtype == TRI_BF16 ? 2 : 4; }
 
 tri_status check_layer(const tri_model *m, const tri_cache *c, int32_t layer, const char *what)
@@ -67,7 +65,9 @@ tri_status check_rows(const void *p, int64_t stride_token, int64_t stride_head, 
 int32_t most_tokens(const tri_tokens &t) { return t.start ? std::max(t.max_tokens, 1) : 1; }
 
 struct AttendPlan {
-    int32_t own_split, own_least, prefix_split, prefix_least, parts;   // parts 0: no partial results
+    AttendSplit own, prefix;
+    int32_t parts;    // 0: no partial results
+    int64_t groups;   // of the largest launch
     size_t o_bytes, ml_bytes, total;
 };
 
@@ -76,11 +76,12 @@ size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 AttendPlan attend_plan(const tri_model &m, const tri_cache *prefix, const tri_cache &c, const tri_tokens &t)
 {
     AttendPlan p{};
-    attend_split(m, c, most_tokens(t), t.n_tokens, &p.own_split, &p.own_least);
-    if (prefix) attend_split(m, *prefix, std::max(t.n_tokens, 1), t.n_tokens, &p.prefix_split, &p.prefix_least);
-    p.parts = p.own_split + p.prefix_split;
+    p.own = attend_split(m, c, most_tokens(t), t.n_tokens);
+    if (prefix) p.prefix = attend_split(m, *prefix, std::max(t.n_tokens, 1), t.n_tokens);
+    p.parts = p.own.n_split + p.prefix.n_split;
     if (p.parts == 1) p.parts = 0;
     const size_t rows = (size_t)t.n_tokens * m.n_q_heads;
+    p.groups = std::max(p.own.groups + p.prefix.groups, p.parts ? join_groups((int64_t)rows, p.parts) : 0);   // (both caches may go in one launch)
     p.o_bytes = up256(p.parts * rows * kHeadDim * sizeof(float));
     p.ml_bytes = up256(p.parts * rows * sizeof(float2));
     p.total = p.o_bytes + p.ml_bytes;
@@ -98,14 +99,19 @@ tri_status check_bounds(const tri_model *model, const tri_cache *prefix, const t
     }
     if ((rc = check_tokens(cache, tokens, what)) != TRI_OK) return rc;
     const int64_t rows = (int64_t)tokens->n_tokens * model->n_q_heads;
-    for (const tri_cache *c : {cache, prefix}) {
-        if (!c) continue;
-        const int64_t tiles = ((int64_t)(c == prefix ? tokens->n_tokens : most_tokens(*tokens)) * (model->n_q_heads / model->n_kv_heads) + 15) / 16;
-        const int64_t units = (int64_t)c->n_seqs * model->n_kv_heads * std::max<int64_t>(tiles, 1);
-        if ((int64_t)c->n_seqs * model->n_kv_heads > 65535 || units > kMostGroups / 256 || rows > kMostGroups) {
-            set_error("%s: %lld row tiles of %d sequences exceed what one call takes; split the batch", what, (long long)units, c->n_seqs);
+    for (const tri_cache *c : {cache, prefix})
+        if (c && (int64_t)c->n_seqs * model->n_kv_heads > 65535) {
+            set_error("%s: n_seqs * n_kv_heads must be below 65536", what);
             return TRI_ERR_UNSUPPORTED;
         }
+    if (rows > 0x7fffffff) {
+        set_error("%s: %lld rows of queries exceed what one call takes; split the batch", what, (long long)rows);
+        return TRI_ERR_UNSUPPORTED;
+    }
+    const int64_t groups = attend_plan(*model, prefix, *cache, *tokens).groups;
+    if (groups > kMostGroups) {
+        set_error("%s: %lld workgroups exceed what one launch takes; split the batch", what, (long long)groups);
+        return TRI_ERR_UNSUPPORTED;
     }
     return TRI_OK;
 }
@@ -163,10 +169,10 @@ tri_status attend(const tri_model *model, const tri_cache *prefix, const int32_t
     a.causal = at->causal;
     a.rotate_q = !tokens->rotated;
     a.half = model->pairs == TRI_PAIR_HALF;
-    const AttendSource own{make_view(*model, *cache), nullptr, tokens->head_len, cache->n_blocks, 0, most_tokens(*tokens), plan.own_split, 0, plan.own_least, most_tokens(*tokens) > 1};
+    const AttendSource own{make_view(*model, *cache), nullptr, tokens->head_len, cache->n_blocks, 0, most_tokens(*tokens), plan.own.n_split, 0, plan.own.least_keys, most_tokens(*tokens) > 1};
     if (prefix) {
-        a.src = AttendSource{make_view(*model, *prefix), group, nullptr, prefix->n_blocks, group ? 0 : 1, tokens->n_tokens, plan.prefix_split, plan.own_split,
-                             plan.prefix_least, 0};
+        a.src = AttendSource{make_view(*model, *prefix), group, nullptr, prefix->n_blocks, group ? 0 : 1, tokens->n_tokens, plan.prefix.n_split, plan.own.n_split,
+                             plan.prefix.least_keys, 0};
         a.other = own;
         rc = launch_attend_both(a, *prefix, *cache, st);
     } else {
@@ -206,7 +212,7 @@ tri_status tri_append(const tri_model *model, const tri_cache *cache, int32_t la
         if ((rc = check_rows(k_new, stride_token, stride_head, eb, "tri_append", "k_new")) != TRI_OK) return rc;
         if ((rc = check_rows(v_new, stride_token, stride_head, eb, "tri_append", "v_new")) != TRI_OK) return rc;
     }
-    if ((int64_t)tokens->n_tokens * model->n_kv_heads > kMostGroups) {
+    if (append_threads((int64_t)tokens->n_tokens * model->n_kv_heads, cache->dtype) > kMostGroups * 256) {
         set_error("tri_append: %d tokens exceed what one call takes; split the batch", tokens->n_tokens);
         return TRI_ERR_UNSUPPORTED;
     }
