@@ -31,7 +31,7 @@ def test_no_launch_is_larger_than_hip_takes():
 
 
 @pytest.mark.parametrize("c", [dict(entry="attend", seqs=256, most=100000, tokens=200000, n=32768), dict(entry="shared", seqs=256, most=1, tokens=200000, pseqs=1000, n=64, pn=4096),
-                               dict(entry="append", seqs=3, tokens=(1 << 25) - 1, most=1 << 25)], ids=["row tiles", "row tiles of prefixes", "rows"])
+                               dict(entry="append", seqs=3, tokens=(1 << 25) - 1, most=1 << 24)], ids=["row tiles", "row tiles of prefixes", "rows"])
 def test_refused(c):
     """More than 2^24 workgroups of 256 threads."""
     status, log = answers([dict(WIDE, **c)])[0]
