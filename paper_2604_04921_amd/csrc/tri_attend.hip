@@ -65,11 +65,9 @@ __global__ __launch_bounds__(kAttendThreads, NT == 1 ? 2 : 1) void attend_genera
     // row tiles of the same keys next to each other on one XCD, as in attend_tile_kernel
     const uint32_t y = blockIdx.x >> 3;
     const int rt = y % a.row_tiles;
-    uint32_t w = (y / a.row_tiles) * 8 + (blockIdx.x & 7);
-    const int split = w % a.src.n_split;
-    w /= a.src.n_split;
-    const int h = w % H, s = w / H;
-    if (s >= c.n_seqs) return;
+    const Unit unit = unit_of(a.src, (y / a.row_tiles) * 8 + (blockIdx.x & 7));
+    const int split = unit.split, h = unit.h, s = unit.s;
+    if (split >= a.src.n_split) return;
     const TokenRange tr = tokens_of(a, a.src, s);
     const int rows = tr.n * G, r0 = rt * kRows;
     if (r0 >= rows) return;

@@ -45,6 +45,17 @@ __device__ __forceinline__ KeyRange keys_of_split(const AttendArgs &a, const Att
     return KeyRange{lo, (int)min(lo + per, (int64_t)n)};
 }
 
+// Which part of which sequence's head workgroup (or group of row tiles) w has.  Parts come last: the first of all heads are spread over the eight XCDs, which workgroups go to in turn, and those
+// that turn out to have no keys end together.  (Two chunks of 1024 tokens over 8192 keys, cut into eight parts of which one had keys: 2013 us with a head's parts next to each other, all work on one XCD then, 365 so.)
+struct Unit {
+    int split, h, s;
+};
+__device__ __forceinline__ Unit unit_of(const AttendSource &src, uint32_t w)
+{
+    const uint32_t H = src.cache.n_kv_heads, S = src.cache.n_seqs;
+    return Unit{(int)(w / H / S), (int)(w % H), (int)(w / H % S)};
+}
+
 // A part without a key says so; its sums are not read.
 __device__ __forceinline__ void no_keys(const AttendArgs &a, const AttendSource &src, int split, int t0, int r0, int rows, int h, int Hq)
 {

@@ -90,11 +90,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
     // Row tiles of the same keys run next to each other on one XCD (workgroups go to the eight in turn), where the keys stay in its L2.
     const uint32_t x = blockIdx.x & 7, y = blockIdx.x >> 3;
     const int rt0 = a.row_tiles - 1 - y % a.row_tiles;   // (a prompt's last rows have the most keys: they begin first)
-    uint32_t w = (y / a.row_tiles) * 8 + x;
-    const int split = w % a.src.n_split;
-    w /= a.src.n_split;
-    const int head = w % H, s = w / H;
-    if (s >= c.n_seqs) return;
+    const Unit unit_here = unit_of(a.src, (y / a.row_tiles) * 8 + x);
+    const int split = unit_here.split, head = unit_here.h, s = unit_here.s;
+    if (split >= a.src.n_split) return;
     const TokenRange tr = tokens_of(a, a.src, s);
     const int rows = tr.n * G, r0 = rt0 * kRows;
     if (r0 >= rows) return;
