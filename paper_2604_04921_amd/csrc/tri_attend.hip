@@ -291,7 +291,8 @@ __global__ __launch_bounds__(kAttendThreads, NT == 1 ? 2 : 1) void attend_genera
 }
 
 // Joins the parts of a row: sixteen threads have 8 dimensions each, and SPREAD such groups of a workgroup's sixteen share a row's parts, each going through its own in one pass
-// with a running maximum; the groups are joined in LDS.  Sixteen where parts are many: one group alone walks 256 parts of a long cache one memory latency after the other.
+// with a running maximum; the groups are joined in LDS.  Sixteen where parts are many: one group alone walks 256 parts of a long cache one memory latency after the other.  A thread's first two parts are read with
+// their maxima, the others only where those say that there is a key (lengths far below max_seq_len leave most parts empty).
 // Bound by latency, then by the parts' bytes: 33 parts of 2048 rows, 35 MB, 9.5 us (13.3 with the maxima looked for first and 147 registers), 64 parts of 64 rows 4.7.
 template <typename T, int SPREAD>
 __global__ __launch_bounds__(kAttendThreads, 6) void join_kernel(const float *part_o, const float2 *part_ml, char *out, int64_t out_stride_token,
@@ -303,15 +304,18 @@ __global__ __launch_bounds__(kAttendThreads, 6) void join_kernel(const float *pa
     const int64_t row = SPREAD > 1 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * (kAttendThreads / 16) + group;
     if (row >= n_rows) return;   // (SPREAD: never)
     float top = kNoScore, total = 0.f, x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    const auto at = [&](int p) { return min(p, parts - 1) * n_rows + row; };
+    float2 ahead[2] = {part_ml[at(first)], part_ml[at(first + SPREAD)]};
     for (int p0 = first; p0 < parts; p0 += 2 * SPREAD) {
-        float2 ml[2];
+        const float2 ml[2] = {ahead[0], ahead[1]};
         f32x4 o[2][2];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {   // (a part without a key is read like any other, whatever its sums hold)
-            const int64_t at = min(p0 + i * SPREAD, parts - 1) * n_rows + row;
-            ml[i] = part_ml[at];
-            const f32x4 *po = reinterpret_cast<const f32x4 *>(part_o + at * kHeadDim + d0);
-            o[i][0] = po[0], o[i][1] = po[1];
+        for (int i = 0; i < 2; ++i) {   // (whatever the sums of a part without a key hold, they are not used)
+            if (p0 == first || ml[i].y != 0.f) {
+                const f32x4 *po = reinterpret_cast<const f32x4 *>(part_o + at(p0 + i * SPREAD) * kHeadDim + d0);
+                o[i][0] = po[0], o[i][1] = po[1];
+            }
+            ahead[i] = part_ml[at(p0 + (2 + i) * SPREAD)];
         }
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -378,8 +382,13 @@ static int64_t groups_of(Kernel kernel, int64_t heads, int64_t row_tiles) { retu
 // 1000 and 65536 keys 938 / 526 / 438 / 399 / 418 / 523 at the same; 16 x 4096 69 / 49 / 61 / 71 at 1, 2, 8, 16; 64 x 2176 90 / 98 / 143 at 1, 2, 8; one of 131072 at G = 8 201 / 114 / 96 /
 // 107 at 16, 32, 64, 128.  fp32: 4 x 30238 1025 / 287 / 178 / 184 at 1, 4, 16, 64; 16 between 300 and 2176 92 / 57 / 51 / 47 / 55 at 1, 2, 3, 4, 8.  The tile kernel: 64 sequences behind 32768 keys
 // 1253 / 351 / 133 / 111 at 1, 4, 16, 32; two chunks of 1024 tokens over 8192 keys, 480 row tiles, 321 / 364 / 387 at 1, 2, 4; one of 512 over 16384 400 / 201 / 169 / 182 at 1, 3, 4, 8.
-// So: 512 workgroups, or parts of 2800 keys (1400 in fp32, 8192 for row tiles) where that makes more; none below the keys that `least` gives, which the device goes by where the lengths
-// turn out shorter than max_seq_len.
+// So: 512 workgroups (`fill` parts), or parts of 2800 keys (1400 in fp32, 8192 for row tiles) where that makes more; none below the keys that `least` gives, which the device goes by where the lengths
+// turn out shorter than max_seq_len, nor, for row tiles, below what the same rule gives for the length there is: max_seq_len is a capacity, and with parts by it two chunks of 1024 tokens over 8192 keys in caches of
+// 131072 were cut into sixteen, the sums of which are 0.5 GB (now 319 us; 303 where the capacity is the length).
+// More than `fill` parts hold kMostPartBytes of sums together at most, a workspace being a user's memory (one fp32 chunk of 8192 tokens in a cache of 131072: 12.7 GB in 93 parts; one part, and no workspace, now).
+// us at 256 / 64 / 16 MiB: two chunks of 1024 tokens over 131072 keys 4851 / 4913 / 4983, over 131072 and 8192 2604 / 2636 / 3173; fp32, two of 256 over 30000 2580 / 2424 / 2362, over 4352 in caches of 131072
+// 512 / 403 / 375.
+constexpr int64_t kMostPartBytes = 64 << 20;
 AttendSplit attend_split(const tri_model &m, const tri_cache &c, int32_t max_tokens, int32_t n_tokens)
 {
     const int64_t G = m.n_q_heads / m.n_kv_heads, rows = max_tokens * G;
@@ -391,10 +400,13 @@ AttendSplit attend_split(const tri_model &m, const tri_cache &c, int32_t max_tok
     const int64_t part = kernel == Kernel::tile ? 8192 : c.dtype == TRI_F32 ? kPartKeys / 2 : kPartKeys;
     const int64_t least = kernel == Kernel::tile ? 256 : std::min<int64_t>(part, std::max<int64_t>(128, part * units / 256));
     const int64_t fill = std::max<int64_t>(1, (512 + units / 2) / units);
-    int64_t want = std::max<int64_t>(fill, c.max_seq_len / part);
+    const int64_t room = kMostPartBytes / (std::max<int64_t>(n_tokens, 1) * m.n_q_heads * kHeadDim * (int64_t)sizeof(float));
+    int64_t want = std::max<int64_t>(fill, std::min<int64_t>(c.max_seq_len / part, room));
     if (want * units < 2048) want = want / fill * fill;   // (few rounds: whole ones; 4 x 30238 keys in fp32 178 us with 16 parts, 210 with 21)
     AttendSplit s;
     s.least_keys = (int32_t)least;
+    s.fill = kernel == Kernel::tile ? (int32_t)fill : 1;
+    s.fill_keys = kernel == Kernel::tile ? (int32_t)part : 0;
     s.n_split = (int32_t)std::max<int64_t>(1, std::min<int64_t>({want, (c.max_seq_len + least - 1) / least, 256}));
     s.groups = groups_of(kernel, (int64_t)s.n_split * m.n_kv_heads * c.n_seqs, row_tiles_of(kernel, c, rows));
     return s;

@@ -32,7 +32,7 @@ __device__ __forceinline__ void widen8(const uint4 &u, float *x)
     for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(w[i] << 16), x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
 }
 
-// The keys of a part: split's share of the sequence's keys, at least src.least_keys where there are so many, in whole groups of 128 (pages of sixteen and more are not cut by a
+// The keys of a part: split's share of the sequence's keys, at least what attend_split says where there are so many, in whole groups of 128 (pages of sixteen and more are not cut by a
 // tile of 32 or 16).
 struct KeyRange {
     int lo, hi;
@@ -40,7 +40,10 @@ struct KeyRange {
 __device__ __forceinline__ KeyRange keys_of_split(const AttendArgs &a, const AttendSource &src, int s, int h, int split)
 {
     const int n = keys_of(a, src, s, h);
-    const int64_t share = max(((int64_t)n + src.n_split - 1) / src.n_split, (int64_t)src.least_keys), per = (share + 127) & ~(int64_t)127;
+    const auto nth = [&](int parts) { return ((uint32_t)n + parts - 1) / (uint32_t)parts; };
+    uint32_t share = max(nth(src.n_split), (uint32_t)src.least_keys);
+    if (src.fill_keys) share = max(share, min(nth(src.fill), (uint32_t)src.fill_keys));
+    const int64_t per = (share + 127) & ~127u;
     const int lo = (int)min(split * per, (int64_t)n);
     return KeyRange{lo, (int)min(lo + per, (int64_t)n)};
 }

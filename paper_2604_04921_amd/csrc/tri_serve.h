@@ -80,6 +80,7 @@ struct AttendSource {
     int32_t max_tokens;        // tokens that attend to one sequence of this cache, at most
     int32_t n_split, part0;    // its keys are cut into n_split ranges; the results are entries part0 and on of the partial results
     int32_t least_keys;        // of a range that is not the last
+    int32_t fill, fill_keys;   // a range is no shorter than the smaller of a fill-th of the keys and fill_keys
     int32_t scan;              // keys behind the tokens' positions are likely at its end (a chunk's own tokens)
 };
 struct AttendArgs {
@@ -120,7 +121,7 @@ constexpr int64_t kMostGroups = 0xffffffffu / 256;   // workgroups of a launch, 
 
 // How the keys of a cache are cut: ranges per head, and their least keys (a function of bounds alone, for the workspace's size); the workgroups of its launch.
 struct AttendSplit {
-    int32_t n_split, least_keys;
+    int32_t n_split, least_keys, fill, fill_keys;
     int64_t groups;
 };
 AttendSplit attend_split(const tri_model &m, const tri_cache &c, int32_t max_tokens, int32_t n_tokens);

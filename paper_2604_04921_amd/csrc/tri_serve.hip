@@ -169,10 +169,11 @@ tri_status attend(const tri_model *model, const tri_cache *prefix, const int32_t
     a.causal = at->causal;
     a.rotate_q = !tokens->rotated;
     a.half = model->pairs == TRI_PAIR_HALF;
-    const AttendSource own{make_view(*model, *cache), nullptr, tokens->head_len, cache->n_blocks, 0, most_tokens(*tokens), plan.own.n_split, 0, plan.own.least_keys, most_tokens(*tokens) > 1};
+    const AttendSource own{make_view(*model, *cache), nullptr, tokens->head_len, cache->n_blocks, 0, most_tokens(*tokens), plan.own.n_split, 0, plan.own.least_keys, plan.own.fill, plan.own.fill_keys,
+                           most_tokens(*tokens) > 1};
     if (prefix) {
         a.src = AttendSource{make_view(*model, *prefix), group, nullptr, prefix->n_blocks, group ? 0 : 1, tokens->n_tokens, plan.prefix.n_split, plan.own.n_split,
-                             plan.prefix.least_keys, 0};
+                             plan.prefix.least_keys, plan.prefix.fill, plan.prefix.fill_keys, 0};
         a.other = own;
         rc = launch_attend_both(a, *prefix, *cache, st);
     } else {
