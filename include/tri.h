@@ -297,9 +297,9 @@ typedef struct tri_attention {
  * occupied slots of the token's own sequence (the step's own tokens among them once tri_append has written them and the lengths count them).
  * A token that attends to no key gets zeros.  What lies in slots that are not occupied is never used, whatever it is; a key or value that is not a
  * number reaches the tokens that attend to it only.  Occupied slots in blocks that there are not (n_blocks) hold no key.  Scores, softmax and sums are
- * held in fp32; results do not depend on anything but the arguments (no atomics).  In bf16, queries and keys rotated on the way enter the products
- * with 16 bits of fraction where a KV head has at most 32 rows (tokens x query heads of the group) and as fp16 numbers (11 bits; rows are scaled by powers of two, so that any
- * magnitude fits) beyond; the weights with 16 bits up to 16 rows and as bf16 numbers beyond.
+ * held in fp32; results do not depend on anything but the arguments (no atomics).  In bf16, where a KV head has at most 32 rows (tokens x query heads of the group;
+ * of a sequence, or of a prefix's sequences together) queries and keys rotated on the way and the weights enter the products with 16 bits of fraction.  Beyond, rotated queries and keys are fp16 numbers there (11 bits; rows
+ * are scaled by powers of two, so that any magnitude fits) and the weights bf16 numbers.
  * workspace as for tri_score, of tri_attend_workspace_size() bytes (which may be 0: NULL will do then).
  */
 tri_status tri_attend(const tri_model *model, const tri_cache *cache, int32_t layer, const tri_tokens *tokens,

@@ -35,7 +35,8 @@ __device__ __forceinline__ void rotate_row(float (*x)[8], int32_t pos, int kq, c
 // or between lanes until the end but the maximum, so waves run on their own, 16 KB of loads under way each, and what bounds the kernel is the cache's bytes.
 // LO: columns 8 to 15 of a tile hold what the rounding to bf16 takes off the rows 0 to 7 (of q turned by its position, and of the weights): the matrix
 // instructions have that room where rows are at most eight to a tile, and both products are as good as in 16 bits of fraction.  Keys turned on the way (TURN)
-// are multiplied as two bf16 numbers for the same reason.  Without LO what is taken off q lies in LDS and is multiplied on its own, and the weights are rounded to bf16 once.
+// are multiplied as two bf16 numbers for the same reason.  Without LO both products are made twice: what is taken off q lies in LDS, what is taken off the weights in registers.  (The matrix pipe has the time: weights
+// rounded to bf16 once, four sequences of 8192 keys and 32 rows take 35.8 us, 35.4 so; and a call's sequences keep their 16 bits when they go in one launch with a prefix of more rows.)
 // Measured (8 KV heads): 32 ragged sequences up to 32768 keys in pages of 16, G = 4, 378 us, 2.29 GB at 6.1 TB/s (read once: 1.14 GB by the counter of fetches, which shows half of what is
 // known to be read; a pure read stream reaches 7.0); the matrix pipe is busy for 4 % of that.  One of 131072 pre-RoPE keys at G = 8 96 us, 5.6 TB/s: 48 % of the time the vector pipe is busy turning keys.  One sequence
 // of 2176 keys: 10 us, nearly all of it one chain of memory latencies.  Two workgroups to a CU: with three (168 registers, what does not fit spilled) the ragged batch takes 490.  Operands of pages
@@ -295,7 +296,7 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attend_rows_kernel(AttendArgs
                     }
                 }
         }
-        bf16x8 weight[NT];
+        bf16x8 weight[NT], weight_low[LO ? 1 : NT];
         float best[NT];
         bool higher = false;
 #pragma unroll
@@ -330,6 +331,7 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attend_rows_kernel(AttendArgs
                     sum[n] += p;
                     const __bf16 hi = (__bf16)p;
                     weight[n][4 * i + d] = LO && m >= 8 ? (__bf16)(p - (float)hi) : hi;
+                    if (!LO) weight_low[n][4 * i + d] = (__bf16)(p - (float)hi);
                 }
         }
         if (__ballot(hole)) {   // (see attend_general_kernel: values that are not finite and not everyone's)
@@ -364,7 +366,10 @@ __global__ __launch_bounds__(kRowsThreads, 2) void attend_rows_kernel(AttendArgs
         for (int e = 0; e < 8; ++e) {
             const bf16x8 x = column(v, e);
 #pragma unroll
-            for (int n = 0; n < NT; ++n) o[n][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, weight[n], o[n][e], 0, 0, 0);
+            for (int n = 0; n < NT; ++n) {
+                o[n][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, weight[n], o[n][e], 0, 0, 0);
+                if (!LO) o[n][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, weight_low[n], o[n][e], 0, 0, 0);
+            }
         }
         load_v(next, k0 + kStep, block_next);
         here[0] = next[0];
