@@ -97,6 +97,10 @@ tri_status check_bounds(const tri_model *model, const tri_cache *prefix, const t
         set_error("%s: caches with n_seqs >= 1 and max_seq_len >= 0 required", what);
         return TRI_ERR_INVALID_ARG;
     }
+    if ((cache->dtype != TRI_F32 && cache->dtype != TRI_BF16) || (prefix && prefix->dtype != cache->dtype)) {
+        set_error("%s: dtype %d, the prefix's %d", what, cache->dtype, prefix ? prefix->dtype : cache->dtype);
+        return TRI_ERR_INVALID_ARG;
+    }
     if ((rc = check_tokens(cache, tokens, what)) != TRI_OK) return rc;
     const int64_t rows = (int64_t)tokens->n_tokens * model->n_q_heads;
     for (const tri_cache *c : {cache, prefix})
@@ -127,8 +131,8 @@ tri_status attend(const tri_model *model, const tri_cache *prefix, const int32_t
     if (prefix) {
         if ((rc = check_cache(model, prefix, true, what)) != TRI_OK) return rc;
         if ((rc = check_layer(model, prefix, layer, what)) != TRI_OK) return rc;
-        if (prefix->dtype != cache->dtype || (!group && prefix->n_seqs != 1)) {
-            set_error("%s: the prefix's dtype must be the cache's, and without group there is one prefix (n_seqs 1, not %d)", what, prefix->n_seqs);
+        if (!group && prefix->n_seqs != 1) {
+            set_error("%s: without group there is one prefix (n_seqs 1, not %d)", what, prefix->n_seqs);
             return TRI_ERR_INVALID_ARG;
         }
     }

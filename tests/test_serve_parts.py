@@ -39,3 +39,9 @@ def test_small_steps_keep_their_parts():
     """A long context is cut for one token as before: its rows are few."""
     few = sizes([dict(tokens=1, most=1, n=n, dtype=1) for n in (2176, 131072)])
     assert few[0] < few[1] <= 32 * 256 * 520 + 1024
+
+
+@pytest.mark.parametrize("c", [dict(dtype=2), dict(dtype=-1), dict(pdtype=7, prefix=True), dict(dtype=1, pdtype=0, prefix=True)])
+def test_types_that_there_are_not(c):
+    """The size goes by the type: one that the calls refuse has none."""
+    assert sizes([dict(tokens=1, most=1, n=131072, **c)]) == [(1 << 64) - 1]
