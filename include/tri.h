@@ -250,7 +250,7 @@ tri_status tri_compress_step_static(const tri_model *model, const float *centers
  * ---- What a serving step does with the cache between two compressions: it appends its tokens' keys and values, and its
  * queries attend to what is cached.  Both work on one layer per call (a model's layers depend on one another) and on caches as
  * the compression leaves them: slots in any order, a position per head and slot, pre- or post-RoPE keys, lengths per sequence or
- * per head.  Rotation means Section 2.1 Eq. 1 with the model's rope_theta and pair layout; angles are exact for every int32 position.
+ * per head.  Rotation means Section 2.1 Eq. 1 with the model's rope_theta and pair layout; angles are within 5e-9 rad for every int32 position.
  *
  * The step's tokens, sequence by sequence.  max_tokens bounds the tokens of one sequence (it sizes grids; tokens beyond it: output
  * unspecified).  Device values are read into their ranges: no token range leaves [0, n_tokens], no length [0, max_seq_len].
@@ -296,9 +296,9 @@ typedef struct tri_attention {
  * out = sum_n p_n v_n, p = softmax over the attended keys n of scale * (q . k_n), both rotated by their positions: the keys of layer `layer` in the
  * occupied slots of the token's own sequence (the step's own tokens among them once tri_append has written them and the lengths count them).
  * A token that attends to no key gets zeros.  What lies in slots that are not occupied is never used, whatever it is; a key or value that is not a
- * number reaches the tokens that attend to it only.  Occupied slots in blocks that there are not (n_blocks) hold no key.  Scores, softmax and sums are
- * held in fp32; results do not depend on anything but the arguments (no atomics).  In bf16, where a KV head has at most 32 rows (tokens x query heads of the group;
- * of a sequence, or of a prefix's sequences together) queries and keys rotated on the way and the weights enter the products with 16 bits of fraction.  Beyond, rotated queries and keys are fp16 numbers there (11 bits; rows
+ * number reaches the tokens that attend to it only (and an infinite key may give those NaN where its score is -inf).  Occupied slots in blocks that there are not (n_blocks) hold no key.  Scores, softmax and sums are
+ * held in fp32; results do not depend on anything but the arguments (no atomics).  In bf16, where a KV head has at most 32 rows (query heads of the group
+ * x max_tokens; x n_tokens for a prefix) queries and keys rotated on the way and the weights enter the products with 16 bits of fraction.  Beyond, rotated queries and keys are fp16 numbers there (11 bits; rows
  * are scaled by powers of two, so that any magnitude fits) and the weights bf16 numbers.
  * workspace as for tri_score, of tri_attend_workspace_size() bytes (which may be 0: NULL will do then).
  */

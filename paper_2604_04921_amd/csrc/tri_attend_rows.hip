@@ -1,4 +1,4 @@
-// Attention with few rows per KV head (decoding): bf16, contiguous caches or pages of at least sixteen slots, up to 32 rows (token, query head of the group).
+// Attention with few rows per KV head (decoding): bf16, contiguous caches and pages of any size, up to 32 rows (token, query head of the group).
 #include <algorithm>
 
 #include "tri_attend_common.h"
@@ -39,7 +39,9 @@ __device__ __forceinline__ void rotate_row(float (*x)[8], int32_t pos, int kq, c
 // rounded to bf16 once, four sequences of 8192 keys and 32 rows take 35.8 us, 35.4 so; and a call's sequences keep their 16 bits when they go in one launch with a prefix of more rows.)
 // Measured (8 KV heads): 32 ragged sequences up to 32768 keys in pages of 16, G = 4, 378 us, 2.29 GB at 6.1 TB/s (read once: 1.14 GB by the counter of fetches, which shows half of what is
 // known to be read; a pure read stream reaches 7.0); the matrix pipe is busy for 4 % of that.  One of 131072 pre-RoPE keys at G = 8 96 us, 5.6 TB/s: 48 % of the time the vector pipe is busy turning keys.  One sequence
-// of 2176 keys: 10 us, nearly all of it one chain of memory latencies.  Two workgroups to a CU: with three (168 registers, what does not fit spilled) the ragged batch takes 490.  Operands of pages
+// of 2176 keys: 10 us, nearly all of it one chain of memory latencies.  Two workgroups to a CU: with three (168 registers, what does not fit spilled) the ragged batch takes 490.  Of the variants for
+// more than eight rows, those that turn keys spill: 2 to 16 registers with LO, 40 to 45 without it in the half-split layout (both halves of a row are under way), none in the interleaved one; four sequences of
+// 8192 keys and 32 rows take 35 us as they are, 45 turned interleaved, 59 turned half-split.  Operands of pages
 // below sixteen slots have addresses of their own, 64 bits each: 452 us for that batch in pages of one slot.
 template <int NT, bool LO, int PAGES, bool TURN, bool HALF>
 __global__ __launch_bounds__(kRowsThreads, 2) void attend_rows_kernel(AttendArgs a)

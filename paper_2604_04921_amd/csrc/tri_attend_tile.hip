@@ -1,4 +1,4 @@
-// Attention with many rows per KV head (chunks of prompts, batches behind a shared prefix): bf16, contiguous caches or pages of at least sixteen slots.
+// Attention with many rows per KV head (chunks of prompts, batches behind a shared prefix): bf16, contiguous caches and pages of any size.
 #include "tri_attend_common.h"
 
 namespace tri {
@@ -68,14 +68,17 @@ struct TileBuffer {
     int32_t lim[3 * kWaves];   // of every wave's keys: highest and lowest position, and which are there (a bit each; bit 16: a unit is not one)
 };
 
-// A workgroup has four waves of 32 rows each (token, query head of the group) and goes through the keys 64 at a time, K and V lying in LDS for all four.  S^T[key][row] = K Q^T and
-// O^T[dim][row] = V^T P^T run on v_mfma_f32_32x32x16_bf16: a row is a lane's column throughout, so its maximum and sum are in-lane but for one exchange of the lane's halves, and the weights are the second product's
+// A workgroup has four waves of 32 rows each (token, query head of the group) and goes through the keys 64 at a time, K and V lying in LDS for all four.  S^T[key][row] = K Q^T runs on
+// v_mfma_f32_32x32x16_bf16, or _f16 where queries or keys are turned on the way (see Keys), O^T[dim][row] = V^T P^T on the former: a row is a lane's column throughout, so its maximum and sum are in-lane but for one exchange of the lane's halves, and the weights are the second product's
 // operand where the first leaves its scores (lane half h holds keys 8 (i / 4) + 4 h + i % 4; the V operand takes its keys in that order, from transposing LDS reads).  K and V go from memory to LDS without passing
-// through registers; a tile's loads are under way while the last one is worked on.  The weights are rounded to bf16 once,
-// an error of its own for every key.
+// through registers; a tile's loads are under way while the last one is worked on.  The weights are rounded to bf16 once:
+// values are bf16 numbers, the instruction takes both operands in one type, and a second product for what is taken off would make half as many matrix instructions again where these bound the kernel (unlike with few
+// rows).  Every key's rounding is its own, so it adds to an output about what its own rounding does: 0.0023 (root mean square, relative) where that alone is 0.0017.
 // Measured: two chunks of 1024 tokens over up to 8192 keys in pages of 64, 8 x 4 heads, 227 GFLOP: 262 us, 870 TFLOP/s (a library product of 8192 x 8192 matrices runs at 1355 here).  The matrix pipe is busy 36 % of the
 // time, the vector pipe with softmax 42 %, LDS 33 %, and the two hardly overlap: a wave issues in order, and there are two to a SIMD.  64 rows to a wave (one to a SIMD) took 577 us when 32 took
 // 322, eight waves to a workgroup 382; the loads' issue is a quarter of the time (without them, on stale tiles, 245 of 322).  Without neighbours on one XCD two prompts' 256 sequences take 379 us, with 229.
+// That is with queries and keys as they are.  Two chunks of 1024 over 8192 keys each, contiguous, take 300 us so, 385 with queries turned on the way and 455 with keys too: every row tile turns its keys again, and what
+// does not fit is spilled (6 to 9 registers with queries turned, 11 to 21 with keys).
 template <int PAGES, Keys KEYS, bool HALF>
 __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs a)
 {

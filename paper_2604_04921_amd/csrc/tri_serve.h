@@ -12,8 +12,8 @@ struct BandTurns {
 BandTurns band_turns(double theta);
 
 // Phase of band w at a position, in 2^-32 revolutions: the position times w modulo one revolution is the low 64 bits of their product,
-// whose upper half is kept.  Exact to 2^-32 revolutions for every int32 position (w is off by less than 2^-62), at the price of two
-// integer multiplications; in double precision the product alone has as many bits only up to positions of 2^20.
+// whose upper half is kept.  Off by less than 2^-32 revolutions (what is not kept) and |pos| 2^-62 (w is off by less than that): 1.5 * 2^-31, 5e-9 rad, for
+// every int32 position, at the price of two integer multiplications; in double precision the product alone has 2^-32 only up to positions of 2^20.
 __device__ __forceinline__ uint32_t phase_of(int32_t pos, uint32_t w_lo, uint32_t w_hi)
 {
     const uint32_t p = (uint32_t)pos;
