@@ -8,14 +8,17 @@ namespace tri {
 
 BandTurns band_turns(double theta)
 {
-    // theta^(-f/64) by products of at most twelve factors (64 calls of powl take 17 us, longer than the kernels of a small step):
-    // off by 12 * 2^-64 of itself
-    long double power[kBands];
-    power[0] = 1.0L;
-    power[1] = powl((long double)theta, -2.0L / kHeadDim);
-    for (int f = 2; f < kBands; ++f) power[f] = power[f / 2] * power[f - f / 2];
+    // theta^(-f/64), as fractions of 2^64, by products of two earlier ones (64 calls of powl take 17 us, longer than the kernels of a small step; the products in long
+    // double 0.6 us or, where the linker had put the code elsewhere, 3.4; so 0.4).  The root is off by 2^-64 of itself and enters f times, as does a product's rounding: 2 f 2^-64 theta^(-f/64), at most 11 * 2^-64 for theta of 100
+    // and more, of which w has 1 / 2 pi.
+    const auto times = [](uint64_t x, uint64_t y) { return (uint64_t)(((unsigned __int128)x * y + ((uint64_t)1 << 63)) >> 64); };
+    const uint64_t turn = (uint64_t)(18446744073709551616.0L / 6.283185307179586476925286766559L + 0.5L);   // 2^64 / 2 pi
+    uint64_t power[kBands];
+    power[1] = (uint64_t)(powl((long double)theta, -2.0L / kHeadDim) * 18446744073709551616.0L);   // (below 2^64: theta is above 1)
+    for (int f = 2; f < kBands; ++f) power[f] = times(power[f / 2], power[f - f / 2]);
     BandTurns t;
-    for (int f = 0; f < kBands; ++f) t.w[f] = (uint64_t)(power[f] * (18446744073709551616.0L / 6.283185307179586476925286766559L) + 0.5L);
+    t.w[0] = turn;
+    for (int f = 1; f < kBands; ++f) t.w[f] = times(power[f], turn);
     return t;
 }
 
