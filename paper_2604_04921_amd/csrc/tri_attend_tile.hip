@@ -74,10 +74,10 @@ struct TileBuffer {
 // through registers; a tile's loads are under way while the last one is worked on.  The weights are rounded to bf16 once:
 // values are bf16 numbers, the instruction takes both operands in one type, and a second product for what is taken off would make half as many matrix instructions again where these bound the kernel (unlike with few
 // rows).  Every key's rounding is its own, so it adds to an output about what its own rounding does: 0.0023 (root mean square, relative) where that alone is 0.0017.
-// Measured: two chunks of 1024 tokens over up to 8192 keys in pages of 64, 8 x 4 heads, 227 GFLOP: 262 us, 870 TFLOP/s (a library product of 8192 x 8192 matrices runs at 1355 here).  The matrix pipe is busy 36 % of the
-// time, the vector pipe with softmax 42 %, LDS 33 %, and the two hardly overlap: a wave issues in order, and there are two to a SIMD.  64 rows to a wave (one to a SIMD) took 577 us when 32 took
+// Measured: two chunks of 1024 tokens over up to 8192 keys in pages of 64, 8 x 4 heads, 227 GFLOP: 259 to 270 us, 840 to 875 TFLOP/s (a library product of 8192 x 8192 matrices runs at 1355 here).  The matrix pipe is busy 35 % of the
+// time, the vector pipe with softmax 41 %, LDS 33 %, and the two hardly overlap: a wave issues in order, and there are two to a SIMD.  64 rows to a wave (one to a SIMD) took 577 us when 32 took
 // 322, eight waves to a workgroup 382; the loads' issue is a quarter of the time (without them, on stale tiles, 245 of 322).  Without neighbours on one XCD two prompts' 256 sequences take 379 us, with 229.
-// That is with queries and keys as they are.  Two chunks of 1024 over 8192 keys each, contiguous, take 300 us so, 385 with queries turned on the way and 455 with keys too: every row tile turns its keys again, and what
+// That is with queries and keys as they are.  Two chunks of 1024 over 8192 keys each, contiguous, take 294 us so, 383 with queries turned on the way and 452 with keys too: every row tile turns its keys again, and what
 // does not fit is spilled (6 to 9 registers with queries turned, 11 to 21 with keys).
 template <int PAGES, Keys KEYS, bool HALF>
 __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs a)
