@@ -152,7 +152,7 @@ def applies(call, mutant):
     return True
 
 
-def judge(call, got, ref, var):
+def wrong(call, got, ref, var):
     """What is wrong with an output: a list of words, empty where nothing is."""
     u = P.HALF[call.c.dtype]
     off = got - ref

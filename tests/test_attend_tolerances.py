@@ -13,9 +13,9 @@ def test_right_and_wrong_kernels(spec):
     call = X.make(spec, "cpu")
     ref, var = call.value()
     to_type = X.to_bf16 if call.c.dtype == torch.bfloat16 else lambda x: x.astype(np.float32).astype(np.float64)
-    assert X.judge(call, to_type(call.value(held=True)[0]), ref, var) == []
+    assert X.wrong(call, to_type(call.value(held=True)[0]), ref, var) == []
     for m in spec["mutants"]:
-        assert not X.applies(call, m) or X.judge(call, to_type(call.value(mutant=m)[0]), ref, var), "nothing says that %r is wrong" % m
+        assert not X.applies(call, m) or X.wrong(call, to_type(call.value(mutant=m)[0]), ref, var), "nothing says that %r is wrong" % m
 
 
 def test_every_mutant_is_told_somewhere():

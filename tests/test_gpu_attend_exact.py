@@ -1,4 +1,4 @@
-"""tri_attend and tri_attend_shared against 64 bits, no further off than the roundings that include/tri.h states (tests/serve_exact.py; tests/test_attend_judge.py says what these tolerances tell apart)."""
+"""tri_attend and tri_attend_shared against 64 bits, no further off than the roundings that include/tri.h states (tests/serve_exact.py; tests/test_attend_tolerances.py says what these tolerances tell apart)."""
 import pytest
 import torch
 
@@ -20,4 +20,4 @@ def test_no_more_roundings_than_stated(spec):
         tokens = c.step(B, head_len=whole)
     out = run(B, c, causal=call.causal, scale=call.scale, shared=call.shared, tokens=tokens)
     torch.cuda.synchronize()
-    assert X.judge(call, out.double().cpu().numpy(), *call.value()) == []
+    assert X.wrong(call, out.double().cpu().numpy(), *call.value()) == []
