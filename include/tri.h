@@ -46,7 +46,7 @@ typedef enum {
     TRI_ERR_HIP = -4          /* a HIP launch reported an error                       */
 } tri_status;
 
-typedef enum { TRI_F32 = 0, TRI_BF16 = 1 } tri_dtype;
+typedef enum { TRI_F32 = 0, TRI_BF16 = 1, TRI_FP4 = 2 } tri_dtype; /* TRI_FP4: inside a tri_cache4 only */
 
 /* which two elements of a head vector form frequency band f */
 typedef enum {
@@ -319,6 +319,57 @@ tri_status tri_attend_shared(const tri_model *model, const tri_cache *prefix, co
 /* Bytes of workspace of tri_attend (prefix NULL) or tri_attend_shared for these geometries (bounds count, not lengths on the device); (size_t)-1 on
  * invalid arguments. */
 size_t tri_attend_workspace_size(const tri_model *model, const tri_cache *prefix, const tri_cache *cache, const tri_tokens *tokens);
+
+/*
+ * ---- Caches held in 4 bits (the fewer bits that a kept key may have, beside the fewer keys): written as they are appended to or packed from a cache in full
+ * precision, read back into one, and attended to as they are.
+ *
+ * A row of head_dim elements is head_dim / 2 bytes of 4-bit numbers -- bit 3 the sign, bits 0 to 2 one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (E2M1); even dimensions in the low halves -- and a word of four
+ * scale bytes, byte g for dimensions 32 g to 32 g + 31: b stands for 2^(b - 127), 255 says that the 32 are not numbers (E8M0).  A slot takes 140 bytes with its position where bf16 takes 516.
+ * Of 32 elements of largest magnitude a, the scale is the least power of two from 2^-124 to 2^125 with a <= 7 scales; an element becomes the nearest number that there is, of two as near the one of even
+ * code, and beyond 6 scales that.  So an element below 7 * 2^125 is off by at most a scale, hence by less than 2 a / 7 (where a >= 7 * 2^-125), by half a scale below 4 and by a quarter below 2 scales.  Where one of
+ * the 32 is not finite (or 2^128 and more once rotated) none of them is a number.  What was read back and is written again stays what it is.
+ * Keys are post-RoPE.  Those that come pre-RoPE are rotated by their position first, and the 4-bit numbers are those of the exactly rotated elements: the kernels work out in double precision what fp32 leaves open.
+ */
+typedef struct tri_cache4 {
+    tri_cache c;              /* k, v: the 4-bit numbers; dtype TRI_FP4; strides in elements, multiples of 32, slots less than 2^24 apart; k_rotated 1 */
+    uint32_t *k_scale, *v_scale; /* device: a slot's word of scale bytes, where pos has its position (the pos_* strides) */
+    int32_t rows;             /* tri_dtype of the rows that come and go: k_new, v_new, q, out */
+} tri_cache4;
+
+/* tri_append for a cache of 4 bits; k_new and v_new are rows of cache->rows. */
+tri_status tri_append4(const tri_model *model, const tri_cache4 *cache, int32_t layer, const tri_tokens *tokens, const void *k_new,
+                       const void *v_new, int64_t stride_token, int64_t stride_head, int32_t *new_seq_len, void *stream);
+
+/*
+ * Slot j of dst <- slot kept_idx[j] of src, j < kept_cnt, for K, V and positions of all layers, into 4 bits (tri_pack4: step 4 of the compression with another destination) and back (tri_unpack4: what the
+ * scores of the next compression are formed of).
+ *   budget    entries of kept_idx per head-instance, and the most slots that one is given (>= 1)
+ *   kept_idx  as tri_select_topk writes it (any order and slots will do); NULL: slots 0, 1, ... in their order
+ *   kept_cnt  as tri_select_topk writes it; NULL: src's lengths.  Read into [0, min(budget, src's max_seq_len)], slot indices into [0, max_seq_len - 1]
+ *   new_seq_len  NULL or device [n_seqs] int32 <- the slots that layer 0, head 0 is given
+ * src and dst must not overlap; dst takes src's n_seqs, its lengths, cur_pos, max_seq_len and tri_cache4::rows are ignored; it needs room for min(max_seq_len, budget) slots per sequence.  Slots in
+ * blocks that there are not (n_blocks of either cache) are not written.  tri_unpack4 writes post-RoPE keys: dst->k_rotated must be 1.
+ */
+tri_status tri_pack4(const tri_model *model, const tri_cache *src, const tri_cache4 *dst, int32_t budget, const int32_t *kept_idx,
+                     const int32_t *kept_cnt, int32_t *new_seq_len, void *stream);
+tri_status tri_unpack4(const tri_model *model, const tri_cache4 *src, const tri_cache *dst, int32_t budget, const int32_t *kept_idx,
+                       const int32_t *kept_cnt, int32_t *new_seq_len, void *stream);
+
+/*
+ * tri_attend over a cache of 4 bits, q and out being rows of cache->rows; and for sequences with caches of their own in full precision (dtype prefix->rows; what was appended since) behind prefixes in 4 bits, by the
+ * rules of tri_attend_shared.  With group 0, 1, 2, ... every sequence has a prefix to itself.
+ * Keys and values enter the products as they are read back.  Queries and weights do as in tri_attend: in bf16, up to 32 rows per KV head, with 16 bits of fraction, and beyond, rotated queries as fp16 numbers and weights as bf16
+ * numbers; in fp32 with 24 bits.
+ */
+tri_status tri_attend4(const tri_model *model, const tri_cache4 *cache, int32_t layer, const tri_tokens *tokens,
+                       const tri_attention *attention, void *workspace, size_t ws_bytes, void *stream);
+tri_status tri_attend4_shared(const tri_model *model, const tri_cache4 *prefix, const int32_t *group, const tri_cache *cache,
+                              int32_t layer, const tri_tokens *tokens, const tri_attention *attention, void *workspace,
+                              size_t ws_bytes, void *stream);
+
+/* Bytes of workspace of tri_attend4 (own NULL) or of tri_attend4_shared (own: the sequences' own caches), as tri_attend_workspace_size. */
+size_t tri_attend4_workspace_size(const tri_model *model, const tri_cache4 *cache, const tri_cache *own, const tri_tokens *tokens);
 
 /*
  * Measurement hook for benchmark harnesses (no counterpart in the paper).  After attaching, the

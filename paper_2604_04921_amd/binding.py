@@ -13,13 +13,14 @@ LIB_PATH = os.path.join(_HERE, "libtri.so")
 
 TRI_OK = 0
 TRI_ERR_INVALID_ARG, TRI_ERR_UNSUPPORTED, TRI_ERR_WORKSPACE, TRI_ERR_HIP = -1, -2, -3, -4
-TRI_F32, TRI_BF16 = 0, 1
+TRI_F32, TRI_BF16, TRI_FP4 = 0, 1, 2
 TRI_PAIR_INTERLEAVED, TRI_PAIR_HALF = 0, 1
 TRI_SCORE_FULL, TRI_SCORE_TRIG_ONLY, TRI_SCORE_NORM_ONLY, TRI_SCORE_NORM_UNWEIGHTED = 0, 1, 2, 3
 
 EXPORTS = ["tri_last_error", "tri_build_centers", "tri_centers_accumulate", "tri_centers_finalize", "tri_band_diagnostics", "tri_workspace_size", "tri_score", "tri_select_topk",
            "tri_compact", "tri_compact_fill", "tri_compress_step", "tri_static_scratch_size", "tri_compress_step_static",
-           "tri_append", "tri_attend", "tri_attend_shared", "tri_attend_workspace_size", "tri_timing_attach", "tri_timing_detach"]
+           "tri_append", "tri_attend", "tri_attend_shared", "tri_attend_workspace_size", "tri_append4", "tri_pack4", "tri_unpack4", "tri_attend4", "tri_attend4_shared",
+           "tri_attend4_workspace_size", "tri_timing_attach", "tri_timing_detach"]
 
 
 class TriModel(ctypes.Structure):
@@ -39,6 +40,10 @@ class TriCache(ctypes.Structure):
                 ("stride_head", ctypes.c_int64), ("stride_slot", ctypes.c_int64),
                 ("pos_stride_layer", ctypes.c_int64), ("pos_stride_seq_or_block", ctypes.c_int64),
                 ("pos_stride_head", ctypes.c_int64), ("k_rotated", ctypes.c_int32), ("n_blocks", ctypes.c_int32)]
+
+
+class TriCache4(ctypes.Structure):
+    _fields_ = [("c", TriCache), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p), ("rows", ctypes.c_int32)]
 
 
 class TriTokens(ctypes.Structure):
@@ -110,6 +115,20 @@ def lib():
         L.tri_attend_workspace_size.restype = ctypes.c_size_t
         L.tri_attend_workspace_size.argtypes = [ctypes.POINTER(TriModel), ctypes.POINTER(TriCache), ctypes.POINTER(TriCache),
                                                 ctypes.POINTER(TriTokens)]
+        c4 = ctypes.POINTER(TriCache4)
+        L.tri_append4.restype = i32
+        L.tri_append4.argtypes = [ctypes.POINTER(TriModel), c4, i32, ctypes.POINTER(TriTokens), vp, vp, i64, i64, vp, vp]
+        L.tri_pack4.restype = i32
+        L.tri_pack4.argtypes = [ctypes.POINTER(TriModel), ctypes.POINTER(TriCache), c4, i32, vp, vp, vp, vp]
+        L.tri_unpack4.restype = i32
+        L.tri_unpack4.argtypes = [ctypes.POINTER(TriModel), c4, ctypes.POINTER(TriCache), i32, vp, vp, vp, vp]
+        L.tri_attend4.restype = i32
+        L.tri_attend4.argtypes = [ctypes.POINTER(TriModel), c4, i32, ctypes.POINTER(TriTokens), ctypes.POINTER(TriAttention), vp, ctypes.c_size_t, vp]
+        L.tri_attend4_shared.restype = i32
+        L.tri_attend4_shared.argtypes = [ctypes.POINTER(TriModel), c4, vp, ctypes.POINTER(TriCache), i32, ctypes.POINTER(TriTokens), ctypes.POINTER(TriAttention), vp,
+                                         ctypes.c_size_t, vp]
+        L.tri_attend4_workspace_size.restype = ctypes.c_size_t
+        L.tri_attend4_workspace_size.argtypes = [ctypes.POINTER(TriModel), c4, ctypes.POINTER(TriCache), ctypes.POINTER(TriTokens)]
         L.tri_timing_attach.restype = i32
         L.tri_timing_attach.argtypes = [vp, i32]
         L.tri_timing_detach.restype = i32
@@ -185,6 +204,39 @@ class Cache:
         self.ref = ctypes.byref(self.c)
 
 
+class Cache4:
+    """tri_cache4 over torch tensors: keys (post-RoPE) and values in 4 bits.
+
+    contiguous: k, v uint8 [L][S][Hkv][N][64], k_scale, v_scale uint8 [L][S][Hkv][N][4], pos int32 [L][S][Hkv][N]
+    paged:      the same over blocks, as Cache
+    Strides are taken from the tensors (k_scale's and v_scale's are four times those of pos); the last dimensions must be dense.  rows: the type of k_new, v_new, q and out (None: bfloat16)."""
+
+    def __init__(self, k, v, k_scale, v_scale, pos, seq_len, cur_pos, max_seq_len, block_table=None, rows=None):
+        for t in (k, v, k_scale, v_scale):
+            if t.dtype != torch.uint8 or t.dim() != 5 or t.stride(4) != 1 or t.device != k.device:
+                raise ValueError("k, v, k_scale, v_scale: uint8 of five dimensions with dense rows, on one device")
+        if k.shape[4] != 64 or v.shape != k.shape or v.stride() != k.stride():
+            raise ValueError("k, v: rows of 64 bytes, of the same shape and strides, got %s and %s" % (tuple(k.shape), tuple(v.shape)))
+        if pos.dtype != torch.int32 or pos.shape != k.shape[:4] or pos.stride(3) != 1 or pos.device != k.device:
+            raise ValueError("pos: int32 %s with dense rows, where k is" % (tuple(k.shape[:4]),))
+        for t in (k_scale, v_scale):
+            if t.shape != pos.shape + (4,) or t.stride()[:4] != tuple(4 * n for n in pos.stride()):
+                raise ValueError("k_scale, v_scale: %s with four times the strides of pos" % (tuple(pos.shape) + (4,),))
+        for t in (seq_len, cur_pos, block_table):
+            if t is not None and (t.dtype != torch.int32 or not t.is_contiguous() or t.device != k.device):
+                raise ValueError("seq_len, cur_pos, block_table: int32, contiguous, where k is")
+        rows = torch.bfloat16 if rows is None else rows
+        if rows not in (torch.bfloat16, torch.float32):
+            raise TypeError("rows: float32 or bfloat16, got %s" % rows)
+        self.tensors = (k, v, k_scale, v_scale, pos, seq_len, cur_pos, block_table)
+        self.n_seqs, self.dtype, self.device = seq_len.numel(), rows, k.device
+        table = (0, 0, 0, 0) if block_table is None else (k.shape[3], block_table.data_ptr(), block_table.shape[1], k.shape[1])
+        c = TriCache(k.data_ptr(), v.data_ptr(), pos.data_ptr(), TRI_FP4, seq_len.numel(), seq_len.data_ptr(), cur_pos.data_ptr(), int(max_seq_len), table[0], table[1], table[2],
+                     *(2 * k.stride(i) for i in range(4)), pos.stride(0), pos.stride(1), pos.stride(2), 1, table[3])
+        self.c = TriCache4(c, k_scale.data_ptr(), v_scale.data_ptr(), TRI_BF16 if rows == torch.bfloat16 else TRI_F32)
+        self.ref = ctypes.byref(self.c)
+
+
 class Tokens:
     """tri_tokens over torch tensors: a step's new tokens, sequence by sequence.
 
@@ -245,20 +297,55 @@ def _bytes(workspace, cache):
     return workspace.numel() * workspace.element_size()
 
 
-def tri_append(model, cache, layer, tokens, k_new, v_new, new_seq_len=None, stream=None):
-    """k_new, v_new [T][Hkv][d], with the same strides, to the end of every sequence of layer `layer`.  new_seq_len int32 [S] or None."""
+def _append(entry, model, cache, layer, tokens, k_new, v_new, new_seq_len, stream):
     strides = _rows(k_new, model.n_kv_heads, tokens, cache, "k_new")
     if _rows(v_new, model.n_kv_heads, tokens, cache, "v_new") != strides:
         raise ValueError("k_new and v_new must have the same strides")
     _fits(model, cache, tokens)
+    _lengths(new_seq_len, cache)
+    _check(entry(model.ref, cache.ref, layer, tokens.ref, k_new.data_ptr(), v_new.data_ptr(), strides[0], strides[1],
+                 _p(new_seq_len), _stream(stream)))
+
+
+def _lengths(new_seq_len, cache):
     if new_seq_len is not None:
         _here(new_seq_len, cache, "new_seq_len")
         if new_seq_len.dtype != torch.int32:
             raise TypeError("new_seq_len: int32, got %s" % new_seq_len.dtype)
         if new_seq_len.numel() < cache.n_seqs or not new_seq_len.is_contiguous():
             raise ValueError("new_seq_len: %d entries side by side, got %s" % (cache.n_seqs, tuple(new_seq_len.shape)))
-    _check(lib().tri_append(model.ref, cache.ref, layer, tokens.ref, k_new.data_ptr(), v_new.data_ptr(), strides[0], strides[1],
-                            _p(new_seq_len), _stream(stream)))
+
+
+def tri_append(model, cache, layer, tokens, k_new, v_new, new_seq_len=None, stream=None):
+    """k_new, v_new [T][Hkv][d], with the same strides, to the end of every sequence of layer `layer`.  new_seq_len int32 [S] or None."""
+    _append(lib().tri_append, model, cache, layer, tokens, k_new, v_new, new_seq_len, stream)
+
+
+def tri_append4(model, cache, layer, tokens, k_new, v_new, new_seq_len=None, stream=None):
+    """tri_append for a Cache4: rows of its `rows` type, rotated on the way where the step's are pre-RoPE, and rounded to 4 bits."""
+    _append(lib().tri_append4, model, cache, layer, tokens, k_new, v_new, new_seq_len, stream)
+
+
+def _move(entry, model, src, dst, budget, kept_idx, kept_cnt, new_seq_len, stream):
+    _here(dst, src, "dst")
+    inst = model.n_layers * src.n_seqs * model.n_kv_heads
+    for t, n, name in ((kept_idx, inst * int(budget), "kept_idx"), (kept_cnt, inst, "kept_cnt")):
+        if t is not None:
+            _here(t, src, name)
+            if t.dtype != torch.int32 or not t.is_contiguous() or t.numel() < n:
+                raise ValueError("%s: int32, %d entries side by side, got %s %s" % (name, n, t.dtype, tuple(t.shape)))
+    _lengths(new_seq_len, src)
+    _check(entry(model.ref, src.ref, dst.ref, int(budget), _p(kept_idx), _p(kept_cnt), _p(new_seq_len), _stream(stream)))
+
+
+def tri_pack4(model, src, dst, budget, kept_idx=None, kept_cnt=None, new_seq_len=None, stream=None):
+    """Slots of a Cache into a Cache4, all layers: those that kept_idx [L][S][Hkv][budget] and kept_cnt [L][S][Hkv] name, or the first min(length, budget)."""
+    _move(lib().tri_pack4, model, src, dst, budget, kept_idx, kept_cnt, new_seq_len, stream)
+
+
+def tri_unpack4(model, src, dst, budget, kept_idx=None, kept_cnt=None, new_seq_len=None, stream=None):
+    """Slots of a Cache4 into a Cache (k_rotated), as tri_pack4."""
+    _move(lib().tri_unpack4, model, src, dst, budget, kept_idx, kept_cnt, new_seq_len, stream)
 
 
 def _attention(model, cache, tokens, q, out, scale, causal):
@@ -288,6 +375,32 @@ def tri_attend_shared(model, prefix, group, cache, layer, tokens, q, out, scale=
 
 def tri_attend_workspace_size(model, cache, tokens, prefix=None):
     n = int(lib().tri_attend_workspace_size(model.ref, None if prefix is None else prefix.ref, cache.ref, tokens.ref))
+    if n == ctypes.c_size_t(-1).value:
+        raise TriError(TRI_ERR_INVALID_ARG, lib().tri_last_error().decode())
+    return n
+
+
+def tri_attend4(model, cache, layer, tokens, q, out, scale=None, causal=True, workspace=None, stream=None):
+    """tri_attend over a Cache4; q and out of its `rows` type."""
+    at = _attention(model, cache, tokens, q, out, scale, causal)
+    _check(lib().tri_attend4(model.ref, cache.ref, layer, tokens.ref, ctypes.byref(at), _p(workspace), _bytes(workspace, cache), _stream(stream)))
+
+
+def tri_attend4_shared(model, prefix, group, cache, layer, tokens, q, out, scale=None, causal=True, workspace=None, stream=None):
+    """tri_attend_shared with the prefixes in a Cache4, the sequences' own keys in a Cache of the prefix's `rows` type."""
+    if group is not None and (group.dtype != torch.int32 or not group.is_contiguous() or group.numel() != prefix.n_seqs + 1):
+        raise ValueError("group: int32, %d entries side by side" % (prefix.n_seqs + 1))
+    at = _attention(model, cache, tokens, q, out, scale, causal)
+    _here(prefix, cache, "prefix")
+    if group is not None:
+        _here(group, cache, "group")
+    _check(lib().tri_attend4_shared(model.ref, prefix.ref, _p(group), cache.ref, layer, tokens.ref, ctypes.byref(at), _p(workspace),
+                                    _bytes(workspace, cache), _stream(stream)))
+
+
+def tri_attend4_workspace_size(model, cache, tokens, own=None):
+    """Bytes for tri_attend4, or (own: the sequences' Cache, `cache` being the prefixes') for tri_attend4_shared."""
+    n = int(lib().tri_attend4_workspace_size(model.ref, cache.ref, None if own is None else own.ref, tokens.ref))
     if n == ctypes.c_size_t(-1).value:
         raise TriError(TRI_ERR_INVALID_ARG, lib().tri_last_error().decode())
     return n

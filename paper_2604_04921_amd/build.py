@@ -8,7 +8,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libtri.so")
 SOURCES = ["tri_api.hip", "tri_centers.hip", "tri_score.hip", "tri_score_mfma.hip", "tri_select.hip", "tri_compact.hip", "tri_append.hip",
-           "tri_attend.hip", "tri_attend_rows.hip", "tri_attend_tile.hip", "tri_serve.hip"]
+           "tri_attend.hip", "tri_attend_rows.hip", "tri_attend_tile.hip", "tri_serve.hip",
+           "tri_append4.hip", "tri_attend4.hip", "tri_serve4.hip"]
 # (source, flags): the general score kernel's variants, a compilation per group size
 UNITS = [("tri_score_lane.hip", ["-DTRI_LANE_GROUP=%d" % g]) for g in (8, 7, 6, 5, 4, 3, 2, 1)] + [(s, []) for s in SOURCES]
 

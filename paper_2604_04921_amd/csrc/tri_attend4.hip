@@ -1,0 +1,465 @@
+// Attention over caches held in 4 bits.
+#include <algorithm>
+
+#include "tri_attend_common.h"
+#include "tri_serve4.h"
+
+namespace tri {
+
+namespace {
+
+constexpr int kThreads = 256, kTile = 64;   // keys that a wave takes at a time
+constexpr int kWaves = kThreads / 64;
+
+template <typename T>
+__device__ __forceinline__ void load_q8(const char *p, float *x)
+{
+    if constexpr (sizeof(T) == 2) {
+        widen8(*reinterpret_cast<const uint4 *>(p), x);
+    } else {
+        const f32x4 a = reinterpret_cast<const f32x4 *>(p)[0], b = reinterpret_cast<const f32x4 *>(p)[1];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = a[e], x[4 + e] = b[e];
+    }
+}
+
+// A lane's 32 elements of a row of q: x[j][e] is dimension 32 kq + 8 j + e, rotated by pos.
+template <typename T>
+__device__ __forceinline__ void load_q(const char *row, int kq, bool rotate, bool half, int32_t pos, const uint64_t *turns, float (*x)[8])
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j) load_q8<T>(row + (32 * kq + 8 * j) * sizeof(T), x[j]);
+    if (!rotate) return;
+    const auto turn = [&](int f, float *c, float *s) {
+        const uint64_t w = turns[f];
+        const uint32_t phase = phase_of(pos, (uint32_t)w, (uint32_t)(w >> 32));
+        if (sizeof(T) == 2) turn_fast(phase, c, s);
+        else turn_exact(phase, c, s);
+    };
+    if (half) {   // the other part of a band lies half a row away
+        const bool im = kq >= 2;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float y[8];
+            load_q8<T>(row + (32 * (kq ^ 2) + 8 * j) * sizeof(T), y);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                float c, s;
+                turn(32 * (kq & 1) + 8 * j + e, &c, &s);
+                x[j][e] = im ? fmaf(y[e], s, x[j][e] * c) : fmaf(x[j][e], c, -(y[e] * s));
+            }
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float c, s;
+                turn(16 * kq + 4 * j + e, &c, &s);
+                const float re = x[j][2 * e], i = x[j][2 * e + 1];
+                x[j][2 * e] = fmaf(re, c, -(i * s));
+                x[j][2 * e + 1] = fmaf(re, s, i * c);
+            }
+    }
+}
+
+// NT column tiles of sixteen rows against 64 keys at a time; S^T[key][row] = K Q^T and O^T[dim][row] = V^T P^T run on v_mfma_f32_16x16x32_bf16.  Keys and values become bf16 numbers in registers, exactly (a conversion
+// for two of them, scale and all).  A lane (m = lane & 15, kq = lane >> 4) holds the 32 dimensions from 32 kq on of key 4 (m & 3) + m / 4 of each sixteen, so that the first product leaves with it scores of keys 4 d + kq, and
+// the rows of V that a load takes for them (dimensions 8 m to 8 m + 7 of four keys) are four neighbouring slots.  A lane has the words (position, scales, block) of one of the tile's 64 keys.
+// Queries and weights are PARTS numbers of bf16 each.  LO (PARTS 2): columns 8 to 15 of a tile hold the second parts of the rows 0 to 7, and one product does both; else every part has a product of its own.
+template <typename T, int NT, int PARTS, bool LO, int PAGES>
+__global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(Attend4Args args)
+{
+    constexpr int kCols = LO ? 8 : 16, kRows = kCols * NT, kProducts = LO ? 1 : PARTS;
+    __shared__ __align__(16) uint64_t turns[kBands];
+    __shared__ float wave_m[kWaves][kRows], wave_l[kWaves][kRows];
+    __shared__ __align__(16) float wave_o[kWaves][kRows][kHeadDim + 4];
+    const AttendArgs &a = args.a;
+    const AttendSource &src = a.src;
+    const CacheView &c = src.cache;
+    const int H = c.n_kv_heads, G = a.group_size, Hq = H * G;
+    // Row tiles of the same keys run next to each other on one XCD; a head's parts next to each other, which part comes first going round the heads (see attend_rows_kernel).
+    const uint32_t x8 = blockIdx.x & 7, y8 = blockIdx.x >> 3;
+    const uint32_t row_tile = y8 % (uint32_t)a.row_tiles, w = y8 / (uint32_t)a.row_tiles * 8 + x8;
+    const uint32_t n = src.n_split, head = w / n, even = min(n & -n, 32u);
+    if (head >= (uint32_t)(H * c.n_seqs)) return;
+    const uint32_t turned = w - head * n + ((head * even / 32) & (even - 1));
+    const int split = turned < n ? turned : turned - n, h = head % H, s = head / H;
+    const TokenRange tr = tokens_of(a, src, s);
+    const int r0 = (int)row_tile * kRows, all_rows = tr.n * G, rows = min(all_rows - r0, kRows);
+    if (rows <= 0) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15, kq = lane >> 4;
+    const KeyRange range = keys_of_split(a, src, s, h, split);
+    if (range.lo >= range.hi && a.part_o) {
+        no_keys(a, src, split, tr.t0, r0, rows, h, Hq);
+        return;
+    }
+    const int k_hi = __builtin_amdgcn_readfirstlane(range.hi);
+    const int64_t base = ((int64_t)a.layer * c.stride_layer + (int64_t)h * c.stride_head) / 2;   // bytes
+    const int64_t pbase = (int64_t)a.layer * c.pos_stride_layer + (int64_t)h * c.pos_stride_head;
+    const uint32_t sb = (uint32_t)c.stride_slot / 2u;
+    const int in_block = PAGES ? (1 << c.block_shift) - 1 : 0;
+    const int my_key = 4 * (m & 3) + (m >> 2);   // of each sixteen, whose row this lane loads
+    auto is_block = [&](int b) { return (b >= 0) & ((src.n_blocks == 0) | (b < src.n_blocks)); };
+    // the block of the lane's key of the 64 from k0 on
+    auto block_at = [&](int k0) { return PAGES ? c.block_table[(int64_t)s * c.max_blocks + (min(k0 + lane, max(k_hi - 1, 0)) >> c.block_shift)] : 0; };
+    auto there_of = [&](int k0, int block) { return __ballot((k0 + lane < k_hi) & (!PAGES || is_block(block))); };
+
+    struct Words {
+        int32_t pos;
+        uint32_t k, v;
+    };
+    auto load_words = [&](int k0, int block, uint64_t there) {
+        Words r{0, 0, 0};
+        if ((there >> lane) & 1) {
+            const int64_t at = pbase + (PAGES ? (int64_t)block * c.pos_stride_sb + ((k0 + lane) & in_block) : (int64_t)s * c.pos_stride_sb + k0 + lane);
+            r.pos = a.causal ? c.pos[at] : 0;
+            r.k = args.k_scale[at];
+            r.v = args.v_scale[at];
+        }
+        return r;
+    };
+    auto rsrc = [&](const void *p, int64_t at, int keys) {
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>((const char *)p) + at, 0, __builtin_amdgcn_readfirstlane(keys > 0 ? (keys - 1) * sb + kHeadDim / 2 : 0), 0x00027000);
+    };
+    // where sixteen keys lie, and how many of them there are
+    auto place = [&](int k0, int i, int block, int *keys) {
+        const int first = k0 + 16 * i;
+        int left = __builtin_amdgcn_readfirstlane(min(max(k_hi - first, 0), 16));
+        int64_t at = base;
+        if (PAGES) {
+            const int b = __builtin_amdgcn_readlane(block, 16 * i);
+            if (!is_block(b)) left = 0;
+            at += ((int64_t)(left ? b : 0) * c.stride_sb + (int64_t)(first & in_block) * c.stride_slot) / 2;
+        } else {
+            at += ((int64_t)s * c.stride_sb + (int64_t)first * c.stride_slot) / 2;
+        }
+        *keys = left;
+        return at;
+    };
+    // (PAGES 2: below sixteen slots) the row of the tile's key `key`; keys that are not there bring the pool's first row, with scales of zero
+    auto slot_of = [&](int k0, int key, int block, uint64_t there) {
+        const int b = __shfl(block, key);
+        return (there >> key) & 1 ? base + ((int64_t)b * c.stride_sb + slot_offset(c, (k0 + key) & in_block)) / 2 : base;
+    };
+    uint4 k[4];
+    uint32_t v[4][4];
+    auto load_k = [&](int k0, int block, uint64_t there) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (PAGES == 2) {
+                k[i] = load_stream16((const char *)c.k + slot_of(k0, 16 * i + my_key, block, there) + 16 * kq);
+                continue;
+            }
+            int keys;
+            const int64_t at = place(k0, i, block, &keys);
+            k[i] = as_uint4(__builtin_amdgcn_raw_buffer_load_b128(rsrc(c.k, at, keys), my_key * sb + 16 * kq, 0, kNonTemporal));
+        }
+    };
+    auto load_v = [&](int k0, int block, uint64_t there) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (PAGES == 2) {
+#pragma unroll
+                for (int d = 0; d < 4; ++d) v[i][d] = *reinterpret_cast<const uint32_t *>((const char *)c.v + slot_of(k0, 16 * i + 4 * d + kq, block, there) + 4 * m);
+                continue;
+            }
+            int keys;
+            const int64_t at = place(k0, i, block, &keys);
+            const auto b = rsrc(c.v, at, keys);
+#pragma unroll
+            for (int d = 0; d < 4; ++d) v[i][d] = __builtin_amdgcn_raw_buffer_load_b32(b, (4 * d + kq) * sb + 4 * m, 0, kNonTemporal);
+        }
+    };
+    constexpr int kStep = kWaves * kTile;
+    int k0 = __builtin_amdgcn_readfirstlane(range.lo) + kTile * wave;
+    // The first tile is asked for before anything is known of the queries.
+    int block = block_at(k0);
+    uint64_t there = there_of(k0, block);
+    Words words = load_words(k0, block, there);
+    load_k(k0, block, there);
+    load_v(k0, block, there);
+    int ahead = block_at(k0 + kStep);
+    if (tid < kBands) turns[tid] = a.turns.w[tid];
+    __syncthreads();
+
+    // this lane's rows: columns m of the column tiles
+    bf16x8 q[NT][kProducts][4];
+    int32_t t_pos[NT], first_pos = 0x7fffffff;
+    bool real[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const int at = t * kCols + (LO ? m & 7 : m), r = r0 + min(at, rows - 1), token = tr.t0 + r / G, hq = h * G + r % G;
+        real[t] = at < rows;
+        t_pos[t] = a.causal ? a.pos[token] : 0x7fffffff;
+        first_pos = min(first_pos, t_pos[t]);
+        float x[4][8];
+        load_q<T>(a.q + ((int64_t)token * a.q_stride_token + (int64_t)hq * a.q_stride_head) * (int64_t)sizeof(T), kq, a.rotate_q, a.half, a.rotate_q ? a.pos[token] : 0, turns, x);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const __bf16 hi = (__bf16)x[j][e];
+                float rest = x[j][e] - (float)hi;
+                if (LO) {
+                    q[t][0][j][e] = m >= 8 ? (__bf16)rest : hi;
+                } else {
+                    q[t][0][j][e] = hi;
+#pragma unroll
+                    for (int p = 1; p < PARTS; ++p) {
+                        const __bf16 next = (__bf16)rest;
+                        q[t][p % kProducts][j][e] = next;
+                        rest -= (float)next;
+                    }
+                }
+            }
+    }
+#pragma unroll
+    for (int i = 1; i < 16; i *= 2) first_pos = min(first_pos, __shfl_xor(first_pos, i));
+    first_pos = __builtin_amdgcn_readfirstlane(first_pos);
+
+    f32x4 o[NT][8];
+    float top[NT], sum[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        top[t] = kNoScore;
+        sum[t] = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[t][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    for (; k0 < k_hi; k0 += kStep) {
+        const int block_next = ahead;
+        const uint64_t there_next = there_of(k0 + kStep, block_next);
+        ahead = block_at(k0 + 2 * kStep);
+        f32x4 sc[4][NT];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float scale = scale_at(__shfl(words.k, 16 * i + my_key), kq);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) sc[i][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+            const uint32_t kw[4] = {k[i].x, k[i].y, k[i].z, k[i].w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const bf16x8 x = __builtin_bit_cast(bf16x8, read8(kw[j], scale));
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int p = kProducts - 1; p >= 0; --p) sc[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, q[t][p][j], sc[i][t], 0, 0, 0);
+            }
+        }
+        const Words here = words;
+        words = load_words(k0 + kStep, block_next, there_next);
+        load_k(k0 + kStep, block_next, there_next);
+        if (LO) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int d = 0; d < 4; ++d) sc[i][t][d] += across_8(sc[i][t][d]);
+        }
+        // keys that are not there, or behind the position of one of the rows
+        const bool late = a.causal && __ballot(((there >> lane) & 1) && here.pos > first_pos);
+        uint32_t keep[NT];   // bit 4 i + d: key 16 i + 4 d + kq is attended to
+        bool hole = false;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) keep[t] = 0xffffu;
+        if (late || there != ~0ull) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int d = 0; d < 4; ++d) {
+                    const int key = 16 * i + 4 * d + kq;
+                    const bool is = (there >> key) & 1;
+                    const int32_t p = __shfl(here.pos, key);
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        const bool on = is && (!a.causal || p <= t_pos[t]);
+                        if (!on) keep[t] &= ~(1u << (4 * i + d)), sc[i][t][d] = kNoScore;
+                        hole |= is && !on && real[t];
+                    }
+                }
+        }
+        float best[NT];
+        bool higher = false;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            best[t] = kNoScore;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int d = 0; d < 4; ++d) best[t] = fmaxf(best[t], sc[i][t][d]);
+            best[t] = max_over_kq(best[t]);
+            higher |= best[t] > top[t];
+        }
+        if (__ballot(higher)) {   // (rare after the first tiles)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const float next_top = fmaxf(top[t], best[t]);
+                const float shrink = next_top == kNoScore ? 1.f : __builtin_amdgcn_exp2f((top[t] - next_top) * a.scale_log2);
+                top[t] = next_top;
+                sum[t] *= shrink;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) o[t][e] *= shrink;
+            }
+        }
+        // values that are not numbers, of keys that are not everyone's
+        const uint32_t ff = here.v & ((here.v & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+        const bool odd = __ballot(ff != 0) && __ballot(hole);
+#pragma unroll
+        for (int U = 0; U < 2; ++U) {   // 32 keys
+            bf16x8 weight[NT][kProducts];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const float ref = top[t] == kNoScore ? 0.f : top[t];
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int d = 0; d < 4; ++d) {
+                        const float p = __builtin_amdgcn_exp2f((sc[2 * U + i][t][d] - ref) * a.scale_log2);
+                        sum[t] += p;
+                        const __bf16 hi = (__bf16)p;
+                        float rest = p - (float)hi;
+                        if (LO) {
+                            weight[t][0][4 * i + d] = m >= 8 ? (__bf16)rest : hi;
+                        } else {
+                            weight[t][0][4 * i + d] = hi;
+#pragma unroll
+                            for (int u = 1; u < PARTS; ++u) {
+                                const __bf16 next = (__bf16)rest;
+                                weight[t][u % kProducts][4 * i + d] = next;
+                                rest -= (float)next;
+                            }
+                        }
+                    }
+            }
+            uint4 values[2][4];
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int d = 0; d < 4; ++d) values[i][d] = read8(v[2 * U + i][d], scale_at(__shfl(here.v, 32 * U + 16 * i + 4 * d + kq), m >> 2));
+            if (odd) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        bf16x8 on;
+#pragma unroll
+                        for (int d = 0; d < 8; ++d) on[d] = (keep[t] >> (8 * U + d)) & 1 ? (__bf16)1.f : (__bf16)0.f;
+                        const f32x4 some = __builtin_amdgcn_mfma_f32_16x16x32_bf16(where_not_below(column(values, e), 0x7f80), on, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+                        for (int d = 0; d < 4; ++d) o[t][e][d] += some[d] > 0.f ? __builtin_nanf("") : 0.f;
+                        __builtin_amdgcn_sched_barrier(0);   // (one after the other: few registers, and time does not matter here)
+                    }
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int d = 0; d < 4; ++d) values[i][d] = finite_only(values[i][d]);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const bf16x8 x = column(values, e);
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int p = kProducts - 1; p >= 0; --p) o[t][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, weight[t][p], o[t][e], 0, 0, 0);
+            }
+        }
+        load_v(k0 + kStep, block_next, there_next);
+        block = block_next;
+        there = there_next;
+    }
+    // join the waves: O's lane has dimensions 32 kq + 8 d + e of its row
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        sum[t] += __shfl_xor(sum[t], 16);
+        sum[t] += __shfl_xor(sum[t], 32);
+        if (kq == 0 && (!LO || m < 8)) wave_m[wave][t * kCols + m] = top[t], wave_l[wave][t * kCols + m] = sum[t];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const int at = t * kCols + (LO ? m & 7 : m);
+        float all = kNoScore;
+#pragma unroll
+        for (int j = 0; j < kWaves; ++j) all = fmaxf(all, wave_m[j][at]);
+        const float mine = __builtin_amdgcn_exp2f((top[t] - (all == kNoScore ? 0.f : all)) * a.scale_log2);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+#pragma unroll
+            for (int d = 0; d < 4; ++d) o[t][e][d] = (LO ? o[t][e][d] + across_8(o[t][e][d]) : o[t][e][d]) * mine;
+        if (!LO || m < 8)
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+#pragma unroll
+                for (int e = 0; e < 8; e += 4)
+                    *reinterpret_cast<f32x4 *>(&wave_o[wave][at][32 * kq + 8 * d + e]) = f32x4{o[t][e][d], o[t][e + 1][d], o[t][e + 2][d], o[t][e + 3][d]};
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < (kRows + 15) / 16; ++i) {
+        const int row = 16 * i + (tid >> 4), d0 = 8 * (tid & 15);
+        if (row >= rows) break;
+        float best = kNoScore, total = 0.f, x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < kWaves; ++j) best = fmaxf(best, wave_m[j][row]);
+        const float ref = best == kNoScore ? 0.f : best;
+#pragma unroll
+        for (int j = 0; j < kWaves; ++j) {
+            total += wave_l[j][row] * __builtin_amdgcn_exp2f((wave_m[j][row] - ref) * a.scale_log2);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] += wave_o[j][row][d0 + e];
+        }
+        const int r = r0 + row;
+        finish_row<T>(a, src, split, tr.t0 + r / G, h * G + r % G, Hq, d0, best, total, x);
+    }
+}
+
+// Rows that a workgroup takes.
+int64_t tile_rows(int32_t type, int64_t rows) { return type == TRI_F32 ? 16 : rows <= 8 ? 8 : rows <= 16 ? 16 : 32; }
+
+int64_t row_tiles_of(int32_t type, int64_t rows)
+{
+    const int64_t per = tile_rows(type, rows);
+    return (rows + per - 1) / per;
+}
+
+}  // namespace
+
+AttendSplit attend4_split(const tri_model &m, const tri_cache &c, int32_t max_tokens, int32_t n_tokens, int32_t type)
+{
+    constexpr int64_t part = 4096;
+    const int64_t G = m.n_q_heads / m.n_kv_heads, rows = max_tokens * G, per = tile_rows(type, rows);
+    const int64_t tiles = std::max<int64_t>(c.n_seqs, (n_tokens * G + per - 1) / per + c.n_seqs / 2);
+    const int64_t units = m.n_kv_heads * tiles;
+    const int64_t least = std::min<int64_t>(part, std::max<int64_t>(256, part * units / 256));
+    const int64_t fill = std::max<int64_t>(1, (512 + units / 2) / units);
+    const int64_t room = ((int64_t)64 << 20) / (std::max<int64_t>(n_tokens, 1) * m.n_q_heads * kHeadDim * (int64_t)sizeof(float));
+    int64_t want = std::max<int64_t>(fill, std::min<int64_t>(c.max_seq_len / part, room));
+    if (want * units < 2048) want = want / fill * fill;
+    AttendSplit s{};
+    s.least_keys = (int32_t)least;
+    s.fill = 1;
+    s.fill_keys = 0;
+    s.n_split = (int32_t)std::max<int64_t>(1, std::min<int64_t>({want, (c.max_seq_len + least - 1) / least, 256}));
+    s.groups = ((int64_t)s.n_split * m.n_kv_heads * c.n_seqs + 7) / 8 * 8 * row_tiles_of(type, rows);
+    return s;
+}
+
+tri_status launch_attend4(Attend4Args args, int32_t type, hipStream_t st)
+{
+    AttendArgs &a = args.a;
+    const int64_t rows = (int64_t)a.src.max_tokens * a.group_size;
+    a.row_tiles = (int32_t)row_tiles_of(type, rows);
+    const uint32_t blocks = (uint32_t)(((int64_t)a.src.n_split * a.src.cache.n_kv_heads * a.src.cache.n_seqs + 7) / 8 * 8 * a.row_tiles);
+    const int shift = a.src.cache.block_shift;
+    const auto launch = [&](auto kernel) { kernel<<<blocks, kThreads, 0, st>>>(args); };
+    const auto of = [&](auto direct, auto paged, auto small) { shift < 0 ? launch(direct) : shift >= 4 ? launch(paged) : launch(small); };
+    if (type == TRI_F32) of(attend4_rows_kernel<float, 1, 3, false, 0>, attend4_rows_kernel<float, 1, 3, false, 1>, attend4_rows_kernel<float, 1, 3, false, 2>);
+    else if (rows <= 8) of(attend4_rows_kernel<__bf16, 1, 2, true, 0>, attend4_rows_kernel<__bf16, 1, 2, true, 1>, attend4_rows_kernel<__bf16, 1, 2, true, 2>);
+    else if (rows <= 16) of(attend4_rows_kernel<__bf16, 2, 2, true, 0>, attend4_rows_kernel<__bf16, 2, 2, true, 1>, attend4_rows_kernel<__bf16, 2, 2, true, 2>);
+    else of(attend4_rows_kernel<__bf16, 2, 2, false, 0>, attend4_rows_kernel<__bf16, 2, 2, false, 1>, attend4_rows_kernel<__bf16, 2, 2, false, 2>);
+    return hip_status("attend4_rows_kernel");
+}
+
+}  // namespace tri

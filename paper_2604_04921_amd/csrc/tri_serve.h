@@ -117,6 +117,12 @@ __device__ __forceinline__ int keys_of(const AttendArgs &a, const AttendSource &
     return clamp_len(n, c.max_seq_len);
 }
 
+// Checks that the entry points of a serving step share.
+tri_status check_layer(const tri_model *m, const tri_cache *c, int32_t layer, const char *what);
+tri_status check_tokens(const tri_cache *c, const tri_tokens *t, const char *what);
+tri_status check_rows(const void *p, int64_t stride_token, int64_t stride_head, int elem_bytes, const char *what, const char *which);
+int32_t most_tokens(const tri_tokens &t);
+
 constexpr int64_t kMostGroups = 0xffffffffu / 256;   // workgroups of a launch, which are of 256 threads: HIP takes fewer than 2^32 threads on an axis
 
 // How the keys of a cache are cut: ranges per head, and their least keys (a function of bounds alone, for the workspace's size); the workgroups of its launch.

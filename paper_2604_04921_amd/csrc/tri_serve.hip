@@ -6,9 +6,7 @@
 
 namespace tri {
 
-namespace {
-
-int elem_bytes(const tri_cache &c) { return c.dtype == TRI_BF16 ? 2 : 4; }
+static int elem_bytes(const tri_cache &c) { return c.dtype == TRI_BF16 ? 2 : 4; }
 
 tri_status check_layer(const tri_model *m, const tri_cache *c, int32_t layer, const char *what)
 {
@@ -63,6 +61,8 @@ tri_status check_rows(const void *p, int64_t stride_token, int64_t stride_head, 
 }
 
 int32_t most_tokens(const tri_tokens &t) { return t.start ? std::max(t.max_tokens, 1) : 1; }
+
+namespace {
 
 struct AttendPlan {
     AttendSplit own, prefix;
