@@ -68,13 +68,12 @@ __device__ __forceinline__ void load_q(const char *row, int kq, bool rotate, boo
 // the rows of V that a load takes for them (dimensions 8 m to 8 m + 7 of four keys) are four neighbouring slots.  A lane has the words (position, scales, block) of one of the tile's 64 keys.
 // Queries and weights are PARTS numbers of bf16 each.  LO (PARTS 2): columns 8 to 15 of a tile hold the second parts of the rows 0 to 7, and one product does both; else every part has a product of its own.
 template <typename T, int NT, int PARTS, bool LO, int PAGES>
-__global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(Attend4Args args)
+__global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
 {
     constexpr int kCols = LO ? 8 : 16, kRows = kCols * NT, kProducts = LO ? 1 : PARTS;
     __shared__ __align__(16) uint64_t turns[kBands];
     __shared__ float wave_m[kWaves][kRows], wave_l[kWaves][kRows];
     __shared__ __align__(16) float wave_o[kWaves][kRows][kHeadDim + 4];
-    const AttendArgs &a = args.a;
     const AttendSource &src = a.src;
     const CacheView &c = src.cache;
     const int H = c.n_kv_heads, G = a.group_size, Hq = H * G;
@@ -114,8 +113,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(Attend4Args a
         if ((there >> lane) & 1) {
             const int64_t at = pbase + (PAGES ? (int64_t)block * c.pos_stride_sb + ((k0 + lane) & in_block) : (int64_t)s * c.pos_stride_sb + k0 + lane);
             r.pos = a.causal ? c.pos[at] : 0;
-            r.k = args.k_scale[at];
-            r.v = args.v_scale[at];
+            r.k = a.k_scale[at];
+            r.v = a.v_scale[at];
         }
         return r;
     };
@@ -415,8 +414,9 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(Attend4Args a
     }
 }
 
-// Rows that a workgroup takes.
-int64_t tile_rows(int32_t type, int64_t rows) { return type == TRI_F32 ? 16 : rows <= 8 ? 8 : rows <= 16 ? 16 : 32; }
+// Rows that a workgroup takes; more than 32 in bf16 are attend_tile_kernel's.
+bool is_tile(int32_t type, int64_t rows) { return type == TRI_BF16 && rows > 32; }
+int64_t tile_rows(int32_t type, int64_t rows) { return is_tile(type, rows) ? kTileRows : type == TRI_F32 ? 16 : rows <= 8 ? 8 : rows <= 16 ? 16 : 32; }
 
 int64_t row_tiles_of(int32_t type, int64_t rows)
 {
@@ -428,33 +428,34 @@ int64_t row_tiles_of(int32_t type, int64_t rows)
 
 AttendSplit attend4_split(const tri_model &m, const tri_cache &c, int32_t max_tokens, int32_t n_tokens, int32_t type)
 {
-    constexpr int64_t part = 4096;
     const int64_t G = m.n_q_heads / m.n_kv_heads, rows = max_tokens * G, per = tile_rows(type, rows);
+    const bool tile = is_tile(type, rows);
+    const int64_t part = tile ? 8192 : 4096;
     const int64_t tiles = std::max<int64_t>(c.n_seqs, (n_tokens * G + per - 1) / per + c.n_seqs / 2);
     const int64_t units = m.n_kv_heads * tiles;
-    const int64_t least = std::min<int64_t>(part, std::max<int64_t>(256, part * units / 256));
+    const int64_t least = tile ? 256 : std::min<int64_t>(part, std::max<int64_t>(256, part * units / 256));
     const int64_t fill = std::max<int64_t>(1, (512 + units / 2) / units);
     const int64_t room = ((int64_t)64 << 20) / (std::max<int64_t>(n_tokens, 1) * m.n_q_heads * kHeadDim * (int64_t)sizeof(float));
     int64_t want = std::max<int64_t>(fill, std::min<int64_t>(c.max_seq_len / part, room));
     if (want * units < 2048) want = want / fill * fill;
     AttendSplit s{};
     s.least_keys = (int32_t)least;
-    s.fill = 1;
-    s.fill_keys = 0;
+    s.fill = tile ? (int32_t)fill : 1;
+    s.fill_keys = tile ? (int32_t)part : 0;
     s.n_split = (int32_t)std::max<int64_t>(1, std::min<int64_t>({want, (c.max_seq_len + least - 1) / least, 256}));
     s.groups = ((int64_t)s.n_split * m.n_kv_heads * c.n_seqs + 7) / 8 * 8 * row_tiles_of(type, rows);
     return s;
 }
 
-tri_status launch_attend4(Attend4Args args, int32_t type, hipStream_t st)
+tri_status launch_attend4(AttendArgs a, int32_t type, hipStream_t st)
 {
-    AttendArgs &a = args.a;
     const int64_t rows = (int64_t)a.src.max_tokens * a.group_size;
     a.row_tiles = (int32_t)row_tiles_of(type, rows);
     const uint32_t blocks = (uint32_t)(((int64_t)a.src.n_split * a.src.cache.n_kv_heads * a.src.cache.n_seqs + 7) / 8 * 8 * a.row_tiles);
     const int shift = a.src.cache.block_shift;
-    const auto launch = [&](auto kernel) { kernel<<<blocks, kThreads, 0, st>>>(args); };
+    const auto launch = [&](auto kernel) { kernel<<<blocks, kThreads, 0, st>>>(a); };
     const auto of = [&](auto direct, auto paged, auto small) { shift < 0 ? launch(direct) : shift >= 4 ? launch(paged) : launch(small); };
+    if (is_tile(type, rows)) return launch_attend4_tile(a, blocks, st);
     if (type == TRI_F32) of(attend4_rows_kernel<float, 1, 3, false, 0>, attend4_rows_kernel<float, 1, 3, false, 1>, attend4_rows_kernel<float, 1, 3, false, 2>);
     else if (rows <= 8) of(attend4_rows_kernel<__bf16, 1, 2, true, 0>, attend4_rows_kernel<__bf16, 1, 2, true, 1>, attend4_rows_kernel<__bf16, 1, 2, true, 2>);
     else if (rows <= 16) of(attend4_rows_kernel<__bf16, 2, 2, true, 0>, attend4_rows_kernel<__bf16, 2, 2, true, 1>, attend4_rows_kernel<__bf16, 2, 2, true, 2>);

@@ -1,5 +1,6 @@
 // Attention with many rows per KV head (chunks of prompts, batches behind a shared prefix): bf16, contiguous caches and pages of any size.
 #include "tri_attend_common.h"
+#include "tri_serve4.h"
 
 namespace tri {
 
@@ -79,7 +80,8 @@ struct TileBuffer {
 // 322, eight waves to a workgroup 382; the loads' issue is a quarter of the time (without them, on stale tiles, 245 of 322).  Without neighbours on one XCD two prompts' 256 sequences take 379 us, with 229.
 // That is with queries and keys as they are.  Two chunks of 1024 over 8192 keys each, contiguous, take 294 us so, 383 with queries turned on the way and 452 with keys too: every row tile turns its keys again, and what
 // does not fit is spilled (6 to 9 registers with queries turned, 11 to 21 with keys).
-template <int PAGES, Keys KEYS, bool HALF>
+// FOUR: keys and values are held in 4 bits.  A lane brings 32 elements of a row, which have one scale, and put() writes what they stand for into LDS: bf16 numbers or, where queries are turned, fp16 ones.
+template <int PAGES, Keys KEYS, bool HALF, bool FOUR = false>
 __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs a)
 {
     constexpr bool TURN = KEYS == kTurn, F16 = KEYS != kAsTheyAre;
@@ -109,7 +111,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
     int k_hi = __builtin_amdgcn_readfirstlane(range.hi);
     const int64_t base = (int64_t)a.layer * c.stride_layer + (int64_t)head * c.stride_head;
     const int64_t pbase = (int64_t)a.layer * c.pos_stride_layer + (int64_t)head * c.pos_stride_head;
-    const uint32_t sb = (uint32_t)c.stride_slot * 2u;
+    const uint32_t sb = FOUR ? (uint32_t)c.stride_slot / 2u : (uint32_t)c.stride_slot * 2u;
     // Lane offsets, as the part that the others follow from by exclusive or: the compiler would keep all of them in registers that it does not have (fresh() hides that
     // they stay the same from tile to tile).  Pieces of 16 bytes lie in LDS at their number exclusive-or the row (K) or twice the row (V), so that eight lanes of a 16-byte
     // read of neighbouring rows, and sixteen of a transposing 8-byte read of four rows, meet different banks.
@@ -124,7 +126,49 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
     };
     int32_t pos_new = 0;
     uint32_t there_new = 0;
+    uint4 k_new, v_new;              // FOUR: elements 32 (lane & 3) and on of the wave's key lane / 4, and its words of scales
+    uint32_t k_scale_new = 0, v_scale_new = 0;
+    auto load4 = [&](int k0, int block_loaded) __attribute__((always_inline)) {
+        int n = __builtin_amdgcn_readfirstlane(min(max(k_hi - k0, 0), kKeys));
+        const uint32_t l = lane_again(), row = l >> 2;
+        if (PAGES == 2) {   // keys that are not there bring the pool's first row, with scales of zero
+            const bool mine = ((int)(l & 15) < n) & is_block(block_loaded);
+            there_new = (uint32_t)__ballot(mine) & 0xffffu;
+            const bool there = (there_new >> row) & 1;
+            const int b = __shfl(block_loaded, (int)row), in = (k0 + row) & in_block;
+            const int64_t at = (there ? base + (int64_t)b * c.stride_sb + slot_offset(c, in) : base) / 2 + 16 * (l & 3);
+            k_new = *reinterpret_cast<const uint4 *>((const char *)c.k + at);
+            v_new = *reinterpret_cast<const uint4 *>((const char *)c.v + at);
+            const int64_t word = pbase + (there ? (int64_t)b * c.pos_stride_sb + in : 0);
+            k_scale_new = there ? a.k_scale[word] : 0;
+            v_scale_new = there ? a.v_scale[word] : 0;
+            pos_new = a.causal ? c.pos[pbase + (mine ? (int64_t)block_loaded * c.pos_stride_sb + ((k0 + (l & 15)) & in_block) : 0)] : 0;
+            return;
+        }
+        int64_t kv, at;
+        if (PAGES == 1) {
+            const int block = __builtin_amdgcn_readfirstlane(block_loaded);
+            const int in = k0 & in_block;
+            if (!is_block(block)) n = 0;
+            const int b = n ? block : 0;
+            kv = base + (int64_t)b * c.stride_sb + (int64_t)in * c.stride_slot;
+            at = pbase + (int64_t)b * c.pos_stride_sb + in;
+        } else {
+            kv = base + (int64_t)s * c.stride_sb + (int64_t)k0 * c.stride_slot;
+            at = pbase + (int64_t)s * c.pos_stride_sb + k0;
+        }
+        there_new = (1u << n) - 1;
+        const uint32_t bytes = __builtin_amdgcn_readfirstlane(n > 0 ? (n - 1) * sb + kHeadDim / 2 : 0), words = __builtin_amdgcn_readfirstlane(n * 4);   // (lanes beyond bring zeros)
+        const auto rsrc = [&](const void *p, int64_t offset, uint32_t size) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>((const char *)p) + offset, 0, size, 0x00027000); };
+        const uint32_t from = row * sb + 16 * (l & 3);
+        k_new = as_uint4(__builtin_amdgcn_raw_buffer_load_b128(rsrc(c.k, kv / 2, bytes), from, 0, 0));
+        k_scale_new = __builtin_amdgcn_raw_buffer_load_b32(rsrc(a.k_scale, at * 4, words), row * 4, 0, 0);
+        v_new = as_uint4(__builtin_amdgcn_raw_buffer_load_b128(rsrc(c.v, kv / 2, bytes), from, 0, 0));
+        v_scale_new = __builtin_amdgcn_raw_buffer_load_b32(rsrc(a.v_scale, at * 4, words), row * 4, 0, 0);
+        pos_new = __builtin_amdgcn_raw_buffer_load_b32(rsrc(c.pos, at * 4, a.causal ? words : 0), (l % kKeys) * 4, 0, 0);
+    };
     auto load = [&](TileBuffer &to, int k0, int block_loaded) __attribute__((always_inline)) {   // k0: this wave's first key
+        if constexpr (FOUR) return load4(k0, block_loaded);
         int n = __builtin_amdgcn_readfirstlane(min(max(k_hi - k0, 0), kKeys));
         if (PAGES == 2) {   // every row has an address of its own; keys that are not there bring the pool's first row, which put() clears
             const uint32_t l = lane_again();
@@ -170,6 +214,39 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
     };
     // What the loads have brought, when it has come: the wave's own keys are turned where they lie, their positions written down.
     auto put = [&](TileBuffer &to) __attribute__((always_inline)) {
+        bool scaled = false;
+        if constexpr (FOUR) {
+            const uint32_t l = lane_again(), row = l >> 2, g = l & 3;
+            uint4 *k = reinterpret_cast<uint4 *>(to.k + (kKeys * wave + row) * kHeadDim), *v = reinterpret_cast<uint4 *>(to.v + (kKeys * wave + row) * kHeadDim);
+            const uint32_t kw[4] = {k_new.x, k_new.y, k_new.z, k_new.w}, vw[4] = {v_new.x, v_new.y, v_new.z, v_new.w};
+            if (F16) {
+                // fp16 as they are from scales of 2^-8 (below 2^-23 bits are lost, 2^-19 of the row's largest at most) to 2^12; else the row's largest scale is its unit
+                const int byte = (k_scale_new >> (8 * g)) & 255;
+                int most = byte == kScaleNaN ? 0 : byte;
+                most = max(most, __builtin_amdgcn_update_dpp(0, most, 0xb1, 0xf, 0xf, false));   // (lane ^ 1, lane ^ 2)
+                most = max(most, __builtin_amdgcn_update_dpp(0, most, 0x4e, 0xf, 0xf, false));
+                scaled = __ballot(most > 127 + 12 || (most < 127 - 8 && most > kScaleLeast));
+                const int unit = scaled && most > kScaleLeast ? most : 127;
+                const float scale = __uint_as_float((uint32_t)(byte == kScaleNaN ? byte : max(byte - unit + 127, 0)) << 23);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    uint4 x;
+                    x.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(kw[j], scale, 0));
+                    x.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(kw[j], scale, 1));
+                    x.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(kw[j], scale, 2));
+                    x.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(kw[j], scale, 3));
+                    k[(4 * g + j) ^ row] = x;
+                }
+                if (g == 0) to.unit[kKeys * wave + row] = __uint_as_float((uint32_t)unit << 23);
+            } else {
+                const float scale = scale_at(k_scale_new, g);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) k[(4 * g + j) ^ row] = read8(kw[j], scale);
+            }
+            const float scale = scale_at(v_scale_new, g);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[(4 * g + j) ^ (2 * (row & 7))] = read8(vw[j], scale);
+        } else {
         if (PAGES == 2 && there_new != 0xffffu) {
             __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0): the rows have come
             const uint32_t l = lane_again();
@@ -178,7 +255,6 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
                 for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4 *>(to.v + (kKeys * wave + (l >> 2)) * kHeadDim + 8 * ((l & 3) + 4 * i)) = make_uint4(0, 0, 0, 0);
             }
         }
-        bool scaled = false;
         if (F16) {
             __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
             const int row = lane / kLanes;
@@ -216,6 +292,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
 #pragma unroll
             for (int i = 0; i < kPieces; ++i) k[(lane % kLanes + kLanes * i) ^ row] = narrow_f16(v[i], by);
             if (lane % kLanes == 0) to.unit[kKeys * wave + row] = unit;
+        }
         }
         const bool there = (there_new >> (lane % kKeys)) & 1;   // (lanes kKeys apart hold the same)
         int32_t hi = there ? pos_new : -0x7fffffff - 1, lo = there ? pos_new : 0x7fffffff;
@@ -508,6 +585,17 @@ tri_status launch_attend_tile(const AttendArgs &a, int64_t groups, hipStream_t s
     else if (!a.src.cache.k_rotated) of(attend_tile_kernel<0, kTurn, false>, attend_tile_kernel<1, kTurn, false>, attend_tile_kernel<2, kTurn, false>);
     else if (a.rotate_q) of(attend_tile_kernel<0, kWiden, false>, attend_tile_kernel<1, kWiden, false>, attend_tile_kernel<2, kWiden, false>);
     else of(attend_tile_kernel<0, kAsTheyAre, false>, attend_tile_kernel<1, kAsTheyAre, false>, attend_tile_kernel<2, kAsTheyAre, false>);
+    return hip_status("attend_tile_kernel");
+}
+
+tri_status launch_attend4_tile(const AttendArgs &a, int64_t groups, hipStream_t st)
+{
+    const uint32_t blocks = (uint32_t)groups;
+    const int shift = a.src.cache.block_shift;
+    const auto launch = [&](auto kernel) { kernel<<<blocks, 64 * kWaves, 0, st>>>(a); };
+    const auto of = [&](auto direct, auto paged, auto small) { shift < 0 ? launch(direct) : shift >= 4 ? launch(paged) : launch(small); };
+    if (a.rotate_q) of(attend_tile_kernel<0, kWiden, false, true>, attend_tile_kernel<1, kWiden, false, true>, attend_tile_kernel<2, kWiden, false, true>);
+    else of(attend_tile_kernel<0, kAsTheyAre, false, true>, attend_tile_kernel<1, kAsTheyAre, false, true>, attend_tile_kernel<2, kAsTheyAre, false, true>);
     return hip_status("attend_tile_kernel");
 }
 

@@ -85,6 +85,7 @@ struct AttendSource {
 };
 struct AttendArgs {
     AttendSource src;
+    const uint32_t *k_scale, *v_scale;   // of src, where it is held in 4 bits
     AttendSource other;        // attend_rows_kernel: workgroups from first_groups on work on this one
     uint32_t first_groups;
     BandTurns turns;

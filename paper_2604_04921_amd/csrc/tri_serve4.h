@@ -61,11 +61,7 @@ int32_t unpack4_row_blocks(int32_t slots);
 tri_status launch_pack4(const Pack4Args &a, int64_t groups, int32_t dtype, bool turn, bool half, hipStream_t st);   // (dtype: of the cache in full precision)
 tri_status launch_unpack4(const Pack4Args &a, int64_t groups, int32_t dtype, hipStream_t st);
 
-struct Attend4Args {
-    AttendArgs a;   // a.src.cache: the 4-bit numbers'
-    const uint32_t *k_scale, *v_scale;
-};
 AttendSplit attend4_split(const tri_model &m, const tri_cache &c, int32_t max_tokens, int32_t n_tokens, int32_t rows);
-tri_status launch_attend4(Attend4Args a, int32_t rows, hipStream_t st);
+tri_status launch_attend4(AttendArgs a, int32_t rows, hipStream_t st);   // (a.src.cache: the 4-bit numbers')
 
 }  // namespace tri

@@ -145,10 +145,9 @@ tri_status attend4(const tri_model *model, const tri_cache4 *x, const int32_t *g
         return TRI_ERR_WORKSPACE;
     }
     const tri_cache &steps = own ? *own : x->c;   // whose sequences the tokens are
-    Attend4Args args{};
-    AttendArgs &a = args.a;
-    args.k_scale = x->k_scale;
-    args.v_scale = x->v_scale;
+    AttendArgs a{};
+    a.k_scale = x->k_scale;
+    a.v_scale = x->v_scale;
     a.turns = band_turns(model->rope_theta);
     a.start = tokens->start;
     a.pos = tokens->pos ? tokens->pos : steps.cur_pos;
@@ -170,7 +169,7 @@ tri_status attend4(const tri_model *model, const tri_cache4 *x, const int32_t *g
     a.half = model->pairs == TRI_PAIR_HALF;
     a.src = AttendSource{make_view(*model, x->c), own ? group : nullptr, own ? nullptr : tokens->head_len, x->c.n_blocks, own && !group ? 1 : 0, own ? tokens->n_tokens : most_tokens(*tokens),
                          plan.packed.n_split, 0, plan.packed.least_keys, plan.packed.fill, plan.packed.fill_keys, !own && most_tokens(*tokens) > 1};
-    if ((rc = launch_attend4(args, x->rows, st)) != TRI_OK) return rc;
+    if ((rc = launch_attend4(a, x->rows, st)) != TRI_OK) return rc;
     if (own) {
         a.src = AttendSource{make_view(*model, *own), nullptr, tokens->head_len, own->n_blocks, 0, most_tokens(*tokens), plan.own.n_split, plan.packed.n_split, plan.own.least_keys, plan.own.fill,
                              plan.own.fill_keys, most_tokens(*tokens) > 1};
