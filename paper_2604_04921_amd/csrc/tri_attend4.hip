@@ -1,5 +1,7 @@
 // Attention over caches held in 4 bits.
 #include <algorithm>
+#include <type_traits>
+#include <utility>
 
 #include "tri_attend_common.h"
 #include "tri_serve4.h"
@@ -11,66 +13,71 @@ namespace {
 constexpr int kThreads = 256, kTile = 64;   // keys that a wave takes at a time
 constexpr int kWaves = kThreads / 64;
 
-template <typename T>
-__device__ __forceinline__ void load_q8(const char *p, float *x)
-{
-    if constexpr (sizeof(T) == 2) {
-        widen8(*reinterpret_cast<const uint4 *>(p), x);
-    } else {
-        const f32x4 a = reinterpret_cast<const f32x4 *>(p)[0], b = reinterpret_cast<const f32x4 *>(p)[1];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = a[e], x[4 + e] = b[e];
-    }
-}
+typedef int i32x8 __attribute__((ext_vector_type(8)));
 
-// A lane's 32 elements of a row of q: x[j][e] is dimension 32 kq + 8 j + e, rotated by pos.
+// A lane's 32 elements of a row of q, rotated by pos: x[0] to x[15] are dimensions 16 kq and on, x[16] to x[31] those 64 further on (both parts of a band are among them in either pair layout).
 template <typename T>
-__device__ __forceinline__ void load_q(const char *row, int kq, bool rotate, bool half, int32_t pos, const uint64_t *turns, float (*x)[8])
+__device__ __forceinline__ void load_q(const char *row, int kq, bool rotate, bool half, int32_t pos, const uint64_t *turns, float *x)
 {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) load_q8<T>(row + (32 * kq + 8 * j) * sizeof(T), x[j]);
+    for (int j = 0; j < 4; ++j) {
+        const char *p = row + (64 * (j / 2) + 16 * kq + 8 * (j % 2)) * sizeof(T);
+        if constexpr (sizeof(T) == 2) {
+            widen8(*reinterpret_cast<const uint4 *>(p), x + 8 * j);
+        } else {
+            const f32x4 a = reinterpret_cast<const f32x4 *>(p)[0], b = reinterpret_cast<const f32x4 *>(p)[1];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[8 * j + e] = a[e], x[8 * j + 4 + e] = b[e];
+        }
+    }
     if (!rotate) return;
-    const auto turn = [&](int f, float *c, float *s) {
+    const auto turn = [&](int f, float &re, float &im) {
         const uint64_t w = turns[f];
         const uint32_t phase = phase_of(pos, (uint32_t)w, (uint32_t)(w >> 32));
-        if (sizeof(T) == 2) turn_fast(phase, c, s);
-        else turn_exact(phase, c, s);
+        float c, s;
+        if (sizeof(T) == 2) turn_fast(phase, &c, &s);
+        else turn_exact(phase, &c, &s);
+        const float r = re, i = im;
+        re = fmaf(r, c, -(i * s));
+        im = fmaf(r, s, i * c);
     };
-    if (half) {   // the other part of a band lies half a row away
-        const bool im = kq >= 2;
+    // (four at a time: the compiler would have all of them under way, in registers that there are not)
+    if (half) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            float y[8];
-            load_q8<T>(row + (32 * (kq ^ 2) + 8 * j) * sizeof(T), y);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                float c, s;
-                turn(32 * (kq & 1) + 8 * j + e, &c, &s);
-                x[j][e] = im ? fmaf(y[e], s, x[j][e] * c) : fmaf(x[j][e], c, -(y[e] * s));
-            }
+        for (int e = 0; e < 16; ++e) {
+            turn(16 * kq + e, x[e], x[16 + e]);
+            if (e % 4 == 3) __builtin_amdgcn_sched_barrier(0);
         }
     } else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                float c, s;
-                turn(16 * kq + 4 * j + e, &c, &s);
-                const float re = x[j][2 * e], i = x[j][2 * e + 1];
-                x[j][2 * e] = fmaf(re, c, -(i * s));
-                x[j][2 * e + 1] = fmaf(re, s, i * c);
-            }
+        for (int e = 0; e < 16; ++e) {
+            turn(32 * (e / 8) + 8 * kq + e % 8, x[2 * e], x[2 * e + 1]);
+            if (e % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+        }
     }
 }
 
-// NT column tiles of sixteen rows against 64 keys at a time; S^T[key][row] = K Q^T and O^T[dim][row] = V^T P^T run on v_mfma_f32_16x16x32_bf16.  Keys and values become bf16 numbers in registers, exactly (a conversion
-// for two of them, scale and all).  A lane (m = lane & 15, kq = lane >> 4) holds the 32 dimensions from 32 kq on of key 4 (m & 3) + m / 4 of each sixteen, so that the first product leaves with it scores of keys 4 d + kq, and
-// the rows of V that a load takes for them (dimensions 8 m to 8 m + 7 of four keys) are four neighbouring slots.  A lane has the words (position, scales, block) of one of the tile's 64 keys.
-// Queries and weights are PARTS numbers of bf16 each.  LO (PARTS 2): columns 8 to 15 of a tile hold the second parts of the rows 0 to 7, and one product does both; else every part has a product of its own.
-template <typename T, int NT, int PARTS, bool LO, int PAGES>
+// x of lanes FIRST + 0, 1, ... of each sixteen
+template <int FIRST, int... N>
+__device__ __forceinline__ void spread(uint32_t x, uint32_t *out, std::integer_sequence<int, N...>)
+{
+    ((out[N] = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x150 + FIRST + N, 0xf, 0xf, false)), ...);
+}
+
+// NT column tiles of sixteen rows against 64 keys at a time.  S^T[key][row] = K Q^T runs on v_mfma_scale_f32_16x16x128_f8f6f4, which takes the keys as they lie in memory -- a lane (m = lane & 15, kq = lane >> 4) has the
+// 32 dimensions from 32 kq on of its key, and their scale -- and queries as e4m3 numbers: QPARTS of them to an element, each of what rounding left of the one before, four bits each (a part's scale is 2^-4 of the last
+// one's, the first's brings the row's largest to [128, 256)).  O^T[dim][row] = V^T P^T runs on v_mfma_f32_16x16x32_bf16: values become bf16 numbers in registers, exactly (a conversion for two of them, scale and all),
+// weights are WPARTS bf16 numbers each.  A lane's key is 4 (m & 3) + m / 4 of each sixteen, so that the first product leaves with it scores of keys 4 d + kq, and the rows of V that a load takes for them (dimensions
+// 8 m to 8 m + 7 of four keys) are four neighbouring slots.  A lane has the words (position, scales, block) of one of the tile's 64 keys.
+// LO: columns 8 to 15 of a tile hold every second part of the rows 0 to 7, and one product does for two parts.
+template <typename T, int NT, bool LO, int PAGES>
 __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
 {
-    constexpr int kCols = LO ? 8 : 16, kRows = kCols * NT, kProducts = LO ? 1 : PARTS;
+    constexpr bool DIRECT = sizeof(T) == 2;
+    constexpr int QPARTS = DIRECT ? 4 : 3, WPARTS = DIRECT ? 2 : 3;
+    constexpr int kQ = LO ? (QPARTS + 1) / 2 : QPARTS, kW = LO ? (WPARTS + 1) / 2 : WPARTS;   // products
+    typedef std::conditional_t<DIRECT, i32x8, uint4[4]> Row;
+    constexpr int kCols = LO ? 8 : 16, kRows = kCols * NT;
     __shared__ __align__(16) uint64_t turns[kBands];
     __shared__ float wave_m[kWaves][kRows], wave_l[kWaves][kRows];
     __shared__ __align__(16) float wave_o[kWaves][kRows][kHeadDim + 4];
@@ -99,10 +106,13 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
     const uint32_t sb = (uint32_t)c.stride_slot / 2u;
     const int in_block = PAGES ? (1 << c.block_shift) - 1 : 0;
     const int my_key = 4 * (m & 3) + (m >> 2);   // of each sixteen, whose row this lane loads
+    // A lane has the words of the tile's key 4 m + kq, so that those of keys 16 i + 4 d + kq lie with lane 4 i + d of each sixteen.
+    auto lane_of = [&](int key) { return 16 * (key & 3) + (key >> 2); };
+    auto of_my_key = [&](uint32_t x, int i) { return (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (16 * (m >> 2) + (m & 3) + 4 * i), (int)x); };   // of key 16 i + my_key
     auto is_block = [&](int b) { return (b >= 0) & ((src.n_blocks == 0) | (b < src.n_blocks)); };
     // the block of the lane's key of the 64 from k0 on
-    auto block_at = [&](int k0) { return PAGES ? c.block_table[(int64_t)s * c.max_blocks + (min(k0 + lane, max(k_hi - 1, 0)) >> c.block_shift)] : 0; };
-    auto there_of = [&](int k0, int block) { return __ballot((k0 + lane < k_hi) & (!PAGES || is_block(block))); };
+    auto block_at = [&](int k0) { return PAGES ? c.block_table[(int64_t)s * c.max_blocks + (min(k0 + 4 * m + kq, max(k_hi - 1, 0)) >> c.block_shift)] : 0; };
+    auto there_of = [&](int k0, int block) { return __ballot((k0 + 4 * m + kq < k_hi) & (!PAGES || is_block(block))); };
 
     struct Words {
         int32_t pos;
@@ -111,7 +121,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
     auto load_words = [&](int k0, int block, uint64_t there) {
         Words r{0, 0, 0};
         if ((there >> lane) & 1) {
-            const int64_t at = pbase + (PAGES ? (int64_t)block * c.pos_stride_sb + ((k0 + lane) & in_block) : (int64_t)s * c.pos_stride_sb + k0 + lane);
+            const int key = k0 + 4 * m + kq;
+            const int64_t at = pbase + (PAGES ? (int64_t)block * c.pos_stride_sb + (key & in_block) : (int64_t)s * c.pos_stride_sb + key);
             r.pos = a.causal ? c.pos[at] : 0;
             r.k = a.k_scale[at];
             r.v = a.v_scale[at];
@@ -127,7 +138,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
         int left = __builtin_amdgcn_readfirstlane(min(max(k_hi - first, 0), 16));
         int64_t at = base;
         if (PAGES) {
-            const int b = __builtin_amdgcn_readlane(block, 16 * i);
+            const int b = __builtin_amdgcn_readlane(block, 4 * i);
             if (!is_block(b)) left = 0;
             at += ((int64_t)(left ? b : 0) * c.stride_sb + (int64_t)(first & in_block) * c.stride_slot) / 2;
         } else {
@@ -138,21 +149,34 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
     };
     // (PAGES 2: below sixteen slots) the row of the tile's key `key`; keys that are not there bring the pool's first row, with scales of zero
     auto slot_of = [&](int k0, int key, int block, uint64_t there) {
-        const int b = __shfl(block, key);
-        return (there >> key) & 1 ? base + ((int64_t)b * c.stride_sb + slot_offset(c, (k0 + key) & in_block)) / 2 : base;
+        const int from = lane_of(key), b = __shfl(block, from);
+        return (there >> from) & 1 ? base + ((int64_t)b * c.stride_sb + slot_offset(c, (k0 + key) & in_block)) / 2 : base;
     };
     uint4 k[4];
     uint32_t v[4][4];
     auto load_k = [&](int k0, int block, uint64_t there) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
+            typedef uint32_t uint2v __attribute__((ext_vector_type(2)));
             if (PAGES == 2) {
-                k[i] = load_stream16((const char *)c.k + slot_of(k0, 16 * i + my_key, block, there) + 16 * kq);
+                const char *p = (const char *)c.k + slot_of(k0, 16 * i + my_key, block, there);
+                if (DIRECT) {
+                    k[i] = load_stream16(p + 16 * kq);
+                } else {
+                    const uint2v x = *reinterpret_cast<const uint2v *>(p + 8 * kq), y = *reinterpret_cast<const uint2v *>(p + 32 + 8 * kq);
+                    k[i] = make_uint4(x.x, x.y, y.x, y.y);
+                }
                 continue;
             }
             int keys;
             const int64_t at = place(k0, i, block, &keys);
-            k[i] = as_uint4(__builtin_amdgcn_raw_buffer_load_b128(rsrc(c.k, at, keys), my_key * sb + 16 * kq, 0, kNonTemporal));
+            const auto b = rsrc(c.k, at, keys);
+            if (DIRECT) {
+                k[i] = as_uint4(__builtin_amdgcn_raw_buffer_load_b128(b, my_key * sb + 16 * kq, 0, kNonTemporal));
+            } else {
+                const uint2v x = __builtin_bit_cast(uint2v, __builtin_amdgcn_raw_buffer_load_b64(b, my_key * sb + 8 * kq, 0, 0)), y = __builtin_bit_cast(uint2v, __builtin_amdgcn_raw_buffer_load_b64(b, my_key * sb + 32 + 8 * kq, 0, 0));
+                k[i] = make_uint4(x.x, x.y, y.x, y.y);
+            }
         }
     };
     auto load_v = [&](int k0, int block, uint64_t there) {
@@ -167,7 +191,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
             const int64_t at = place(k0, i, block, &keys);
             const auto b = rsrc(c.v, at, keys);
 #pragma unroll
-            for (int d = 0; d < 4; ++d) v[i][d] = __builtin_amdgcn_raw_buffer_load_b32(b, (4 * d + kq) * sb + 4 * m, 0, kNonTemporal);
+            for (int d = 0; d < 4; ++d) v[i][d] = __builtin_amdgcn_raw_buffer_load_b32(b, kq * sb + 4 * m, 4 * d * sb, kNonTemporal);
         }
     };
     constexpr int kStep = kWaves * kTile;
@@ -183,35 +207,61 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
     __syncthreads();
 
     // this lane's rows: columns m of the column tiles
-    bf16x8 q[NT][kProducts][4];
+    Row q[NT][kQ];
+    uint32_t q_scale[NT];   // a byte for every part
     int32_t t_pos[NT], first_pos = 0x7fffffff;
-    bool real[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         const int at = t * kCols + (LO ? m & 7 : m), r = r0 + min(at, rows - 1), token = tr.t0 + r / G, hq = h * G + r % G;
-        real[t] = at < rows;
         t_pos[t] = a.causal ? a.pos[token] : 0x7fffffff;
         first_pos = min(first_pos, t_pos[t]);
-        float x[4][8];
+        float x[32];
         load_q<T>(a.q + ((int64_t)token * a.q_stride_token + (int64_t)hq * a.q_stride_head) * (int64_t)sizeof(T), kq, a.rotate_q, a.half, a.rotate_q ? a.pos[token] : 0, turns, x);
+        if constexpr (DIRECT) {
+            float most = 0.f;
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+            for (int e = 0; e < 32; ++e) most = fmaxf(most, fabsf(x[e]));
+            most = max_over_kq(most);
+            // the power of two of the row's largest, at least what leaves the last part a scale
+            const int unit = max((int)(__float_as_uint(most) >> 23), 127 - 99);
+            const float by = __uint_as_float((uint32_t)(261 - unit) << 23);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const __bf16 hi = (__bf16)x[j][e];
-                float rest = x[j][e] - (float)hi;
-                if (LO) {
-                    q[t][0][j][e] = m >= 8 ? (__bf16)rest : hi;
-                } else {
-                    q[t][0][j][e] = hi;
+            for (int e = 0; e < 32; ++e) x[e] *= by;
 #pragma unroll
-                    for (int p = 1; p < PARTS; ++p) {
-                        const __bf16 next = (__bf16)rest;
-                        q[t][p % kProducts][j][e] = next;
-                        rest -= (float)next;
-                    }
+            for (int p = 0; p < QPARTS; ++p)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    int w = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * j], x[4 * j + 1], 0, false);
+                    w = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * j + 2], x[4 * j + 3], w, true);
+                    if (!LO) q[t][p % kQ][j] = w;
+                    else if (p % 2 == 0) q[t][p / 2][j] = w;
+                    else q[t][p / 2][j] = m >= 8 ? w : q[t][p / 2][j];
+                    x[4 * j] = (x[4 * j] - __builtin_amdgcn_cvt_f32_fp8(w, 0)) * 16.f;
+                    x[4 * j + 1] = (x[4 * j + 1] - __builtin_amdgcn_cvt_f32_fp8(w, 1)) * 16.f;
+                    x[4 * j + 2] = (x[4 * j + 2] - __builtin_amdgcn_cvt_f32_fp8(w, 2)) * 16.f;
+                    x[4 * j + 3] = (x[4 * j + 3] - __builtin_amdgcn_cvt_f32_fp8(w, 3)) * 16.f;
                 }
-            }
+            const uint32_t first = unit - 7 - (LO && m >= 8 ? 4 : 0), apart = LO ? 8 : 4;
+            q_scale[t] = 0;
+#pragma unroll
+            for (int p = 0; p < kQ; ++p) q_scale[t] |= (first - apart * p) << (8 * p);
+        } else {
+#pragma unroll
+            for (int p = 0; p < QPARTS; ++p)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    bf16x8 part;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        part[e] = (__bf16)x[8 * j + e];
+                        x[8 * j + e] -= (float)part[e];
+                    }
+                    const uint4 w = __builtin_bit_cast(uint4, part), none = make_uint4(0, 0, 0, 0);
+                    if (!LO) q[t][p % kQ][j] = w;
+                    else if (p % 2 == 0) q[t][p / 2][j] = p + 1 < QPARTS || m < 8 ? w : none;
+                    else q[t][p / 2][j] = m >= 8 ? w : q[t][p / 2][j];
+                }
+        }
     }
 #pragma unroll
     for (int i = 1; i < 16; i *= 2) first_pos = min(first_pos, __shfl_xor(first_pos, i));
@@ -219,8 +269,10 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
 
     f32x4 o[NT][8];
     float top[NT], sum[NT];
+    uint32_t not_numbers[NT];   // bit 8 g + 7: dimensions 32 g and on of a value that the row attends to are none
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
+        not_numbers[t] = 0;
         top[t] = kNoScore;
         sum[t] = 0.f;
 #pragma unroll
@@ -233,20 +285,34 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
         f32x4 sc[4][NT];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float scale = scale_at(__shfl(words.k, 16 * i + my_key), kq);
+            const uint32_t word = of_my_key(words.k, i);
 #pragma unroll
             for (int t = 0; t < NT; ++t) sc[i][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-            const uint32_t kw[4] = {k[i].x, k[i].y, k[i].z, k[i].w};
+            if constexpr (DIRECT) {
+                const uint32_t scale = word >> (8 * kq);
+                const i32x8 x{(int)k[i].x, (int)k[i].y, (int)k[i].z, (int)k[i].w, 0, 0, 0, 0};
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const bf16x8 x = __builtin_bit_cast(bf16x8, read8(kw[j], scale));
+                for (int t = 0; t < NT; ++t) {
+                    const auto product = [&](auto part) {   // (e2m1 times e4m3)
+                        constexpr int p = decltype(part)::value;
+                        if constexpr (p < kQ) sc[i][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, q[t][p], sc[i][t], 4, 0, 0, scale, p, q_scale[t]);
+                    };
+                    product(std::integral_constant<int, 3>()), product(std::integral_constant<int, 2>()), product(std::integral_constant<int, 1>()), product(std::integral_constant<int, 0>());
+                }
+            } else {
+                const uint32_t kw[4] = {k[i].x, k[i].y, k[i].z, k[i].w};
 #pragma unroll
-                for (int t = 0; t < NT; ++t)
+                for (int j = 0; j < 4; ++j) {
+                    const bf16x8 x = __builtin_bit_cast(bf16x8, read8(kw[j], scale_at(word, j / 2 * 2 + kq / 2)));
 #pragma unroll
-                    for (int p = kProducts - 1; p >= 0; --p) sc[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, q[t][p][j], sc[i][t], 0, 0, 0);
+                    for (int t = 0; t < NT; ++t)
+#pragma unroll
+                        for (int p = kQ - 1; p >= 0; --p) sc[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, __builtin_bit_cast(bf16x8, q[t][p][j]), sc[i][t], 0, 0, 0);
+                }
             }
         }
-        const Words here = words;
+        __builtin_amdgcn_sched_barrier(0);   // (phases are kept apart: the compiler would have all of a tile's conversions under way at once)
+        Words here = words;
         words = load_words(k0 + kStep, block_next, there_next);
         load_k(k0 + kStep, block_next, there_next);
         if (LO) {
@@ -259,25 +325,15 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
         }
         // keys that are not there, or behind the position of one of the rows
         const bool late = a.causal && __ballot(((there >> lane) & 1) && here.pos > first_pos);
-        uint32_t keep[NT];   // bit 4 i + d: key 16 i + 4 d + kq is attended to
-        bool hole = false;
-#pragma unroll
-        for (int t = 0; t < NT; ++t) keep[t] = 0xffffu;
         if (late || there != ~0ull) {
+            const uint32_t is = (uint32_t)(there >> (16 * kq));   // bit 4 i + d
+            int32_t p[16];
+            spread<0>((uint32_t)here.pos, reinterpret_cast<uint32_t *>(p), std::make_integer_sequence<int, 16>());
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int n = 0; n < 16; ++n)
 #pragma unroll
-                for (int d = 0; d < 4; ++d) {
-                    const int key = 16 * i + 4 * d + kq;
-                    const bool is = (there >> key) & 1;
-                    const int32_t p = __shfl(here.pos, key);
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) {
-                        const bool on = is && (!a.causal || p <= t_pos[t]);
-                        if (!on) keep[t] &= ~(1u << (4 * i + d)), sc[i][t][d] = kNoScore;
-                        hole |= is && !on && real[t];
-                    }
-                }
+                for (int t = 0; t < NT; ++t)
+                    if (!((is >> n) & 1) || (a.causal && p[n] > t_pos[t])) sc[n / 4][t][n % 4] = kNoScore;
         }
         float best[NT];
         bool higher = false;
@@ -302,12 +358,21 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
                 for (int e = 0; e < 8; ++e) o[t][e] *= shrink;
             }
         }
-        // values that are not numbers, of keys that are not everyone's
+        // Values that are not numbers (a scale byte of 255) make the sums of their 32 dimensions no numbers in the rows that attend to their key: that is written down, and they are left out of the product.
         const uint32_t ff = here.v & ((here.v & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
-        const bool odd = __ballot(ff != 0) && __ballot(hole);
+        for (uint64_t odd = __ballot(ff != 0); odd; odd &= odd - 1) {
+            const int key = __builtin_ctzll(odd);
+            const uint32_t which = __builtin_amdgcn_readlane(ff, key);
+            const int32_t p = __builtin_amdgcn_readlane(here.pos, key);
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+                if (!a.causal || p <= t_pos[t]) not_numbers[t] |= which;
+        }
+        here.v &= ~((ff << 1) - (ff >> 7));
 #pragma unroll
         for (int U = 0; U < 2; ++U) {   // 32 keys
-            bf16x8 weight[NT][kProducts];
+            __builtin_amdgcn_sched_barrier(0);
+            bf16x8 weight[NT][kW];
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
                 const float ref = top[t] == kNoScore ? 0.f : top[t];
@@ -317,51 +382,32 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
                     for (int d = 0; d < 4; ++d) {
                         const float p = __builtin_amdgcn_exp2f((sc[2 * U + i][t][d] - ref) * a.scale_log2);
                         sum[t] += p;
-                        const __bf16 hi = (__bf16)p;
-                        float rest = p - (float)hi;
-                        if (LO) {
-                            weight[t][0][4 * i + d] = m >= 8 ? (__bf16)rest : hi;
-                        } else {
-                            weight[t][0][4 * i + d] = hi;
+                        float rest = p;
 #pragma unroll
-                            for (int u = 1; u < PARTS; ++u) {
-                                const __bf16 next = (__bf16)rest;
-                                weight[t][u % kProducts][4 * i + d] = next;
-                                rest -= (float)next;
-                            }
+                        for (int u = 0; u < WPARTS; ++u) {
+                            const __bf16 part = (__bf16)rest;
+                            if (!LO) weight[t][u % kW][4 * i + d] = part;
+                            else if (u % 2 == 0) weight[t][u / 2][4 * i + d] = u + 1 < WPARTS || m < 8 ? part : (__bf16)0.f;
+                            else weight[t][u / 2][4 * i + d] = m >= 8 ? part : weight[t][u / 2][4 * i + d];
+                            rest -= (float)part;
                         }
                     }
             }
+            uint32_t scales[8];
+            if (U == 0) spread<0>(here.v, scales, std::make_integer_sequence<int, 8>());
+            else spread<8>(here.v, scales, std::make_integer_sequence<int, 8>());
             uint4 values[2][4];
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
-                for (int d = 0; d < 4; ++d) values[i][d] = read8(v[2 * U + i][d], scale_at(__shfl(here.v, 32 * U + 16 * i + 4 * d + kq), m >> 2));
-            if (odd) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) {
-                        bf16x8 on;
-#pragma unroll
-                        for (int d = 0; d < 8; ++d) on[d] = (keep[t] >> (8 * U + d)) & 1 ? (__bf16)1.f : (__bf16)0.f;
-                        const f32x4 some = __builtin_amdgcn_mfma_f32_16x16x32_bf16(where_not_below(column(values, e), 0x7f80), on, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-#pragma unroll
-                        for (int d = 0; d < 4; ++d) o[t][e][d] += some[d] > 0.f ? __builtin_nanf("") : 0.f;
-                        __builtin_amdgcn_sched_barrier(0);   // (one after the other: few registers, and time does not matter here)
-                    }
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-#pragma unroll
-                    for (int d = 0; d < 4; ++d) values[i][d] = finite_only(values[i][d]);
-            }
+                for (int d = 0; d < 4; ++d) values[i][d] = read8(v[2 * U + i][d], scale_at(scales[4 * i + d], m >> 2));
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const bf16x8 x = column(values, e);
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
-                    for (int p = kProducts - 1; p >= 0; --p) o[t][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, weight[t][p], o[t][e], 0, 0, 0);
+                    for (int p = kW - 1; p >= 0; --p) o[t][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, weight[t][p], o[t][e], 0, 0, 0);
             }
         }
         load_v(k0 + kStep, block_next, there_next);
@@ -386,7 +432,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
 #pragma unroll
         for (int e = 0; e < 8; ++e)
 #pragma unroll
-            for (int d = 0; d < 4; ++d) o[t][e][d] = (LO ? o[t][e][d] + across_8(o[t][e][d]) : o[t][e][d]) * mine;
+            for (int d = 0; d < 4; ++d) o[t][e][d] = (not_numbers[t] >> (8 * kq + 7)) & 1 ? __builtin_nanf("") : (LO ? o[t][e][d] + across_8(o[t][e][d]) : o[t][e][d]) * mine;
         if (!LO || m < 8)
 #pragma unroll
             for (int d = 0; d < 4; ++d)
@@ -416,7 +462,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
 
 // Rows that a workgroup takes; more than 32 in bf16 are attend_tile_kernel's.
 bool is_tile(int32_t type, int64_t rows) { return type == TRI_BF16 && rows > 32; }
-int64_t tile_rows(int32_t type, int64_t rows) { return is_tile(type, rows) ? kTileRows : type == TRI_F32 ? 16 : rows <= 8 ? 8 : rows <= 16 ? 16 : 32; }
+int64_t tile_rows(int32_t type, int64_t rows) { return is_tile(type, rows) ? kTileRows : rows <= 8 ? 8 : type == TRI_F32 || rows <= 16 ? 16 : 32; }
 
 int64_t row_tiles_of(int32_t type, int64_t rows)
 {
@@ -456,10 +502,11 @@ tri_status launch_attend4(AttendArgs a, int32_t type, hipStream_t st)
     const auto launch = [&](auto kernel) { kernel<<<blocks, kThreads, 0, st>>>(a); };
     const auto of = [&](auto direct, auto paged, auto small) { shift < 0 ? launch(direct) : shift >= 4 ? launch(paged) : launch(small); };
     if (is_tile(type, rows)) return launch_attend4_tile(a, blocks, st);
-    if (type == TRI_F32) of(attend4_rows_kernel<float, 1, 3, false, 0>, attend4_rows_kernel<float, 1, 3, false, 1>, attend4_rows_kernel<float, 1, 3, false, 2>);
-    else if (rows <= 8) of(attend4_rows_kernel<__bf16, 1, 2, true, 0>, attend4_rows_kernel<__bf16, 1, 2, true, 1>, attend4_rows_kernel<__bf16, 1, 2, true, 2>);
-    else if (rows <= 16) of(attend4_rows_kernel<__bf16, 2, 2, true, 0>, attend4_rows_kernel<__bf16, 2, 2, true, 1>, attend4_rows_kernel<__bf16, 2, 2, true, 2>);
-    else of(attend4_rows_kernel<__bf16, 2, 2, false, 0>, attend4_rows_kernel<__bf16, 2, 2, false, 1>, attend4_rows_kernel<__bf16, 2, 2, false, 2>);
+    if (type == TRI_F32 && rows <= 8) of(attend4_rows_kernel<float, 1, true, 0>, attend4_rows_kernel<float, 1, true, 1>, attend4_rows_kernel<float, 1, true, 2>);
+    else if (type == TRI_F32) of(attend4_rows_kernel<float, 1, false, 0>, attend4_rows_kernel<float, 1, false, 1>, attend4_rows_kernel<float, 1, false, 2>);
+    else if (rows <= 8) of(attend4_rows_kernel<__bf16, 1, true, 0>, attend4_rows_kernel<__bf16, 1, true, 1>, attend4_rows_kernel<__bf16, 1, true, 2>);
+    else if (rows <= 16) of(attend4_rows_kernel<__bf16, 2, true, 0>, attend4_rows_kernel<__bf16, 2, true, 1>, attend4_rows_kernel<__bf16, 2, true, 2>);
+    else of(attend4_rows_kernel<__bf16, 2, false, 0>, attend4_rows_kernel<__bf16, 2, false, 1>, attend4_rows_kernel<__bf16, 2, false, 2>);
     return hip_status("attend4_rows_kernel");
 }
 
