@@ -11,6 +11,7 @@ namespace tri {
 namespace {
 
 constexpr int kThreads = 256, kTile = 64;   // keys that a wave takes at a time
+constexpr float kStaleBits = 8.f;   // powers of two by which a score may pass the maximum that weights are relative to
 constexpr int kWaves = kThreads / 64;
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
@@ -61,23 +62,30 @@ __device__ __forceinline__ void load_q(const char *row, int kq, bool rotate, boo
 template <int FIRST, int... N>
 __device__ __forceinline__ void spread(uint32_t x, uint32_t *out, std::integer_sequence<int, N...>)
 {
-    ((out[N] = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x150 + FIRST + N, 0xf, 0xf, false)), ...);
+    ((out[N] = (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x150 + FIRST + N, 0xf, 0xf, false)), ...);
 }
+// x + that of lane ^ 8 of each sixteen
+__device__ __forceinline__ float add_across_8(float x) { return x + __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x128, 0xf, 0xf, false)); }
+// x + that of lane ^ 4
+__device__ __forceinline__ float add_across_4(float x) { return x + __shfl_xor(x, 4); }
 
 // NT column tiles of sixteen rows against 64 keys at a time.  S^T[key][row] = K Q^T runs on v_mfma_scale_f32_16x16x128_f8f6f4, which takes the keys as they lie in memory -- a lane (m = lane & 15, kq = lane >> 4) has the
 // 32 dimensions from 32 kq on of its key, and their scale -- and queries as e4m3 numbers: QPARTS of them to an element, each of what rounding left of the one before, four bits each (a part's scale is 2^-4 of the last
 // one's, the first's brings the row's largest to [128, 256)).  O^T[dim][row] = V^T P^T runs on v_mfma_f32_16x16x32_bf16: values become bf16 numbers in registers, exactly (a conversion for two of them, scale and all),
 // weights are WPARTS bf16 numbers each.  A lane's key is 4 (m & 3) + m / 4 of each sixteen, so that the first product leaves with it scores of keys 4 d + kq, and the rows of V that a load takes for them (dimensions
 // 8 m to 8 m + 7 of four keys) are four neighbouring slots.  A lane has the words (position, scales, block) of one of the tile's 64 keys.
-// LO: columns 8 to 15 of a tile hold every second part of the rows 0 to 7, and one product does for two parts.
-template <typename T, int NT, bool LO, int PAGES>
+// COLS rows to a column tile.  8: columns 8 to 15 hold every second part of the rows, and one product does for two parts.  4: so do they for the first product; in the second, columns 4 to 7 and 12 to 15 hold second parts, and
+// of each pair of dimensions that a conversion leaves in a register columns 0 to 7 have weights for the even one and zeros for the other, columns 8 to 15 the other way round, so that values need not be brought into the
+// order of keys.
+template <typename T, int NT, int COLS, int PAGES>
 __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
 {
-    constexpr bool DIRECT = sizeof(T) == 2;
+    constexpr bool DIRECT = sizeof(T) == 2, LO = COLS < 16, QUAD = COLS == 4;
+    static_assert(!QUAD || (DIRECT && NT == 1), "");
     constexpr int QPARTS = DIRECT ? 4 : 3, WPARTS = DIRECT ? 2 : 3;
     constexpr int kQ = LO ? (QPARTS + 1) / 2 : QPARTS, kW = LO ? (WPARTS + 1) / 2 : WPARTS;   // products
     typedef std::conditional_t<DIRECT, i32x8, uint4[4]> Row;
-    constexpr int kCols = LO ? 8 : 16, kRows = kCols * NT;
+    constexpr int kRows = COLS * NT, kSums = QUAD ? 4 : 8;
     __shared__ __align__(16) uint64_t turns[kBands];
     __shared__ float wave_m[kWaves][kRows], wave_l[kWaves][kRows];
     __shared__ __align__(16) float wave_o[kWaves][kRows][kHeadDim + 4];
@@ -135,12 +143,12 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
     // where sixteen keys lie, and how many of them there are
     auto place = [&](int k0, int i, int block, int *keys) {
         const int first = k0 + 16 * i;
-        int left = __builtin_amdgcn_readfirstlane(min(max(k_hi - first, 0), 16));
+        int left = min(k_hi - first, 16);   // (what is below one makes no descriptor)
         int64_t at = base;
         if (PAGES) {
             const int b = __builtin_amdgcn_readlane(block, 4 * i);
             if (!is_block(b)) left = 0;
-            at += ((int64_t)(left ? b : 0) * c.stride_sb + (int64_t)(first & in_block) * c.stride_slot) / 2;
+            at += ((int64_t)(left > 0 ? b : 0) * c.stride_sb + (int64_t)(first & in_block) * c.stride_slot) / 2;
         } else {
             at += ((int64_t)s * c.stride_sb + (int64_t)first * c.stride_slot) / 2;
         }
@@ -212,7 +220,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
     int32_t t_pos[NT], first_pos = 0x7fffffff;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-        const int at = t * kCols + (LO ? m & 7 : m), r = r0 + min(at, rows - 1), token = tr.t0 + r / G, hq = h * G + r % G;
+        const int at = t * COLS + (m & (COLS - 1)), r = r0 + min(at, rows - 1), token = tr.t0 + r / G, hq = h * G + r % G;
         t_pos[t] = a.causal ? a.pos[token] : 0x7fffffff;
         first_pos = min(first_pos, t_pos[t]);
         float x[32];
@@ -267,7 +275,10 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
     for (int i = 1; i < 16; i *= 2) first_pos = min(first_pos, __shfl_xor(first_pos, i));
     first_pos = __builtin_amdgcn_readfirstlane(first_pos);
 
-    f32x4 o[NT][8];
+    // (QUAD) bytes 1, 0 below zeros or above them; of the upper half
+    const uint32_t pick = m < 8 ? 0x0c0c0100u : 0x01000c0cu, pick_next = m < 8 ? 0x0202u : 0x02020000u;
+    const float second = m & (QUAD ? 4 : 8) ? 1.f : 0.f;   // whether this column has second parts of weights
+    f32x4 o[NT][kSums];
     float top[NT], sum[NT];
     uint32_t not_numbers[NT];   // bit 8 g + 7: dimensions 32 g and on of a value that the row attends to are none
 #pragma unroll
@@ -276,12 +287,13 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
         top[t] = kNoScore;
         sum[t] = 0.f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) o[t][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int e = 0; e < kSums; ++e) o[t][e] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
     for (; k0 < k_hi; k0 += kStep) {
         const int block_next = ahead;
         const uint64_t there_next = there_of(k0 + kStep, block_next);
         ahead = block_at(k0 + 2 * kStep);
+        const Words words_next = load_words(k0 + kStep, block_next, there_next);
         f32x4 sc[4][NT];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -313,7 +325,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
         }
         __builtin_amdgcn_sched_barrier(0);   // (phases are kept apart: the compiler would have all of a tile's conversions under way at once)
         Words here = words;
-        words = load_words(k0 + kStep, block_next, there_next);
+        words = words_next;
         load_k(k0 + kStep, block_next, there_next);
         if (LO) {
 #pragma unroll
@@ -321,7 +333,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
-                    for (int d = 0; d < 4; ++d) sc[i][t][d] += across_8(sc[i][t][d]);
+                    for (int d = 0; d < 4; ++d) sc[i][t][d] = add_across_8(sc[i][t][d]);
         }
         // keys that are not there, or behind the position of one of the rows
         const bool late = a.causal && __ballot(((there >> lane) & 1) && here.pos > first_pos);
@@ -345,9 +357,9 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
 #pragma unroll
                 for (int d = 0; d < 4; ++d) best[t] = fmaxf(best[t], sc[i][t][d]);
             best[t] = max_over_kq(best[t]);
-            higher |= best[t] > top[t];
+            higher |= best[t] > top[t] && !((best[t] - top[t]) * a.scale_log2 <= kStaleBits);
         }
-        if (__ballot(higher)) {   // (rare after the first tiles)
+        if (__ballot(higher)) {   // (rare after the first tile: weights are relative to a maximum that scores may pass by a factor of 2^8)
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
                 const float next_top = fmaxf(top[t], best[t]);
@@ -355,7 +367,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
                 top[t] = next_top;
                 sum[t] *= shrink;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) o[t][e] *= shrink;
+                for (int e = 0; e < kSums; ++e) o[t][e] *= shrink;
             }
         }
         // Values that are not numbers (a scale byte of 255) make the sums of their 32 dimensions no numbers in the rows that attend to their key: that is written down, and they are left out of the product.
@@ -373,23 +385,45 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
         for (int U = 0; U < 2; ++U) {   // 32 keys
             __builtin_amdgcn_sched_barrier(0);
             bf16x8 weight[NT][kW];
+            uint32_t pair[8];   // QUAD: a key's weight and zero, or zero and the weight
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
-                const float ref = top[t] == kNoScore ? 0.f : top[t];
+                const float ref = top[t] == kNoScore ? 0.f : top[t], off = ref * a.scale_log2;
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
 #pragma unroll
-                    for (int d = 0; d < 4; ++d) {
-                        const float p = __builtin_amdgcn_exp2f((sc[2 * U + i][t][d] - ref) * a.scale_log2);
-                        sum[t] += p;
-                        float rest = p;
+                    for (int d = 0; d < 4; d += 2) {
+                        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+                        float p[2];
 #pragma unroll
-                        for (int u = 0; u < WPARTS; ++u) {
-                            const __bf16 part = (__bf16)rest;
-                            if (!LO) weight[t][u % kW][4 * i + d] = part;
-                            else if (u % 2 == 0) weight[t][u / 2][4 * i + d] = u + 1 < WPARTS || m < 8 ? part : (__bf16)0.f;
-                            else weight[t][u / 2][4 * i + d] = m >= 8 ? part : weight[t][u / 2][4 * i + d];
-                            rest -= (float)part;
+                        for (int e = 0; e < 2; ++e) {
+                            // (in fp32 a difference before the product: its rounding is not the product's)
+                            p[e] = __builtin_amdgcn_exp2f(DIRECT ? fmaf(sc[2 * U + i][t][d + e], a.scale_log2, -off) : (sc[2 * U + i][t][d + e] - ref) * a.scale_log2);
+                            sum[t] += p[e];
+                        }
+#pragma unroll
+                        for (int u = 0; u < kW; ++u) {
+                            bf16x2 part{(__bf16)p[0], (__bf16)p[1]};
+                            if (LO) {   // lanes of the second eight columns have the part behind this one
+#pragma unroll
+                                for (int e = 0; e < 2; ++e) {
+                                    const float rest = fmaf(-(float)part[e], second, p[e]);
+                                    p[e] -= (float)part[e];
+                                    part[e] = (__bf16)rest;
+                                    if (u + 1 < kW) p[e] -= (float)(__bf16)p[e];
+                                }
+                            } else if (u + 1 < kW) {
+#pragma unroll
+                                for (int e = 0; e < 2; ++e) p[e] -= (float)part[e];
+                            }
+                            if (QUAD) {
+                                const uint32_t both = __builtin_bit_cast(uint32_t, part);
+                                pair[4 * i + d] = __builtin_amdgcn_perm(0, both, pick);
+                                pair[4 * i + d + 1] = __builtin_amdgcn_perm(0, both, pick + pick_next);
+                            } else {
+                                weight[t][u][4 * i + d] = part[0];
+                                weight[t][u][4 * i + d + 1] = part[1];
+                            }
                         }
                     }
             }
@@ -401,6 +435,19 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
             for (int i = 0; i < 2; ++i)
 #pragma unroll
                 for (int d = 0; d < 4; ++d) values[i][d] = read8(v[2 * U + i][d], scale_at(scales[4 * i + d], m >> 2));
+            if (QUAD) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const bf16x8 w = __builtin_bit_cast(bf16x8, make_uint4(pair[4 * i], pair[4 * i + 1], pair[4 * i + 2], pair[4 * i + 3]));
+                    const auto word = [](const uint4 &x, int e) { return e == 0 ? x.x : e == 1 ? x.y : e == 2 ? x.z : x.w; };
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint4 x = make_uint4(word(values[i][0], e), word(values[i][1], e), word(values[i][2], e), word(values[i][3], e));
+                        o[0][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), w, o[0][e], 0, 0, 0);
+                    }
+                }
+                continue;
+            }
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const bf16x8 x = column(values, e);
@@ -419,26 +466,34 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
     for (int t = 0; t < NT; ++t) {
         sum[t] += __shfl_xor(sum[t], 16);
         sum[t] += __shfl_xor(sum[t], 32);
-        if (kq == 0 && (!LO || m < 8)) wave_m[wave][t * kCols + m] = top[t], wave_l[wave][t * kCols + m] = sum[t];
+        if (kq == 0 && m < COLS) wave_m[wave][t * COLS + m] = top[t], wave_l[wave][t * COLS + m] = sum[t];
     }
     __syncthreads();
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-        const int at = t * kCols + (LO ? m & 7 : m);
+        const int at = t * COLS + (m & (COLS - 1));
         float all = kNoScore;
 #pragma unroll
         for (int j = 0; j < kWaves; ++j) all = fmaxf(all, wave_m[j][at]);
         const float mine = __builtin_amdgcn_exp2f((top[t] - (all == kNoScore ? 0.f : all)) * a.scale_log2);
+        const bool none = (not_numbers[t] >> (8 * kq + 7)) & 1;
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
+        for (int e = 0; e < kSums; ++e)
 #pragma unroll
-            for (int d = 0; d < 4; ++d) o[t][e][d] = (not_numbers[t] >> (8 * kq + 7)) & 1 ? __builtin_nanf("") : (LO ? o[t][e][d] + across_8(o[t][e][d]) : o[t][e][d]) * mine;
-        if (!LO || m < 8)
+            for (int d = 0; d < 4; ++d) o[t][e][d] = none ? __builtin_nanf("") : (QUAD ? add_across_4(o[t][e][d]) : LO ? add_across_8(o[t][e][d]) : o[t][e][d]) * mine;
 #pragma unroll
-            for (int d = 0; d < 4; ++d)
+        for (int d = 0; d < 4; ++d) {
+            if (QUAD) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (!(m & 4)) wave_o[wave][at][32 * kq + 8 * d + 2 * e + (m >> 3)] = o[t][e % kSums][d];
+            } else {
 #pragma unroll
                 for (int e = 0; e < 8; e += 4)
-                    *reinterpret_cast<f32x4 *>(&wave_o[wave][at][32 * kq + 8 * d + e]) = f32x4{o[t][e][d], o[t][e + 1][d], o[t][e + 2][d], o[t][e + 3][d]};
+                    if (m < COLS)
+                        *reinterpret_cast<f32x4 *>(&wave_o[wave][at][32 * kq + 8 * d + e]) = f32x4{o[t][e % kSums][d], o[t][(e + 1) % kSums][d], o[t][(e + 2) % kSums][d], o[t][(e + 3) % kSums][d]};
+            }
+        }
     }
     __syncthreads();
 #pragma unroll
@@ -502,11 +557,12 @@ tri_status launch_attend4(AttendArgs a, int32_t type, hipStream_t st)
     const auto launch = [&](auto kernel) { kernel<<<blocks, kThreads, 0, st>>>(a); };
     const auto of = [&](auto direct, auto paged, auto small) { shift < 0 ? launch(direct) : shift >= 4 ? launch(paged) : launch(small); };
     if (is_tile(type, rows)) return launch_attend4_tile(a, blocks, st);
-    if (type == TRI_F32 && rows <= 8) of(attend4_rows_kernel<float, 1, true, 0>, attend4_rows_kernel<float, 1, true, 1>, attend4_rows_kernel<float, 1, true, 2>);
-    else if (type == TRI_F32) of(attend4_rows_kernel<float, 1, false, 0>, attend4_rows_kernel<float, 1, false, 1>, attend4_rows_kernel<float, 1, false, 2>);
-    else if (rows <= 8) of(attend4_rows_kernel<__bf16, 1, true, 0>, attend4_rows_kernel<__bf16, 1, true, 1>, attend4_rows_kernel<__bf16, 1, true, 2>);
-    else if (rows <= 16) of(attend4_rows_kernel<__bf16, 2, true, 0>, attend4_rows_kernel<__bf16, 2, true, 1>, attend4_rows_kernel<__bf16, 2, true, 2>);
-    else of(attend4_rows_kernel<__bf16, 2, false, 0>, attend4_rows_kernel<__bf16, 2, false, 1>, attend4_rows_kernel<__bf16, 2, false, 2>);
+    if (type == TRI_F32 && rows <= 8) of(attend4_rows_kernel<float, 1, 8, 0>, attend4_rows_kernel<float, 1, 8, 1>, attend4_rows_kernel<float, 1, 8, 2>);
+    else if (type == TRI_F32) of(attend4_rows_kernel<float, 1, 16, 0>, attend4_rows_kernel<float, 1, 16, 1>, attend4_rows_kernel<float, 1, 16, 2>);
+    else if (rows <= 4) of(attend4_rows_kernel<__bf16, 1, 4, 0>, attend4_rows_kernel<__bf16, 1, 4, 1>, attend4_rows_kernel<__bf16, 1, 4, 2>);
+    else if (rows <= 8) of(attend4_rows_kernel<__bf16, 1, 8, 0>, attend4_rows_kernel<__bf16, 1, 8, 1>, attend4_rows_kernel<__bf16, 1, 8, 2>);
+    else if (rows <= 16) of(attend4_rows_kernel<__bf16, 2, 8, 0>, attend4_rows_kernel<__bf16, 2, 8, 1>, attend4_rows_kernel<__bf16, 2, 8, 2>);
+    else of(attend4_rows_kernel<__bf16, 2, 16, 0>, attend4_rows_kernel<__bf16, 2, 16, 1>, attend4_rows_kernel<__bf16, 2, 16, 2>);
     return hip_status("attend4_rows_kernel");
 }
 
