@@ -16,56 +16,41 @@ constexpr int kWaves = kThreads / 64;
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
-// A lane's 32 elements of a row of q, rotated by pos: x[0] to x[15] are dimensions 16 kq and on, x[16] to x[31] those 64 further on (both parts of a band are among them in either pair layout).
+// Both parts of a band of a row of q.
 template <typename T>
-__device__ __forceinline__ void load_q(const char *row, int kq, bool rotate, bool half, int32_t pos, const uint64_t *turns, float *x)
+__device__ __forceinline__ void load_band(const T *row, int f, bool half, float *re, float *im)
 {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const char *p = row + (64 * (j / 2) + 16 * kq + 8 * (j % 2)) * sizeof(T);
-        if constexpr (sizeof(T) == 2) {
-            widen8(*reinterpret_cast<const uint4 *>(p), x + 8 * j);
-        } else {
-            const f32x4 a = reinterpret_cast<const f32x4 *>(p)[0], b = reinterpret_cast<const f32x4 *>(p)[1];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) x[8 * j + e] = a[e], x[8 * j + 4 + e] = b[e];
-        }
-    }
-    if (!rotate) return;
-    const auto turn = [&](int f, float &re, float &im) {
-        const uint64_t w = turns[f];
-        const uint32_t phase = phase_of(pos, (uint32_t)w, (uint32_t)(w >> 32));
-        float c, s;
-        if (sizeof(T) == 2) turn_fast(phase, &c, &s);
-        else turn_exact(phase, &c, &s);
-        const float r = re, i = im;
-        re = fmaf(r, c, -(i * s));
-        im = fmaf(r, s, i * c);
-    };
-    // (four at a time: the compiler would have all of them under way, in registers that there are not)
     if (half) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            turn(16 * kq + e, x[e], x[16 + e]);
-            if (e % 4 == 3) __builtin_amdgcn_sched_barrier(0);
-        }
+        *re = (float)row[f], *im = (float)row[f + 64];
     } else {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            turn(32 * (e / 8) + 8 * kq + e % 8, x[2 * e], x[2 * e + 1]);
-            if (e % 4 == 3) __builtin_amdgcn_sched_barrier(0);
-        }
+        typedef T pair __attribute__((ext_vector_type(2)));
+        const pair x = *reinterpret_cast<const pair *>(row + 2 * f);
+        *re = (float)x[0], *im = (float)x[1];
     }
+}
+
+// lanes ^ 1, ^ 2, and the halves and the whole of each sixteen turned round: each lane of a sixteen has the result
+template <typename F>
+__device__ __forceinline__ int over_16(int x, F f)
+{
+    x = f(x, __builtin_amdgcn_mov_dpp(x, 0xb1, 0xf, 0xf, true));
+    x = f(x, __builtin_amdgcn_mov_dpp(x, 0x4e, 0xf, 0xf, true));
+    x = f(x, __builtin_amdgcn_mov_dpp(x, 0x141, 0xf, 0xf, true));
+    return f(x, __builtin_amdgcn_mov_dpp(x, 0x140, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float most_of_wave(float x)
+{
+    return max_over_kq(__int_as_float(over_16(__float_as_int(x), [](int a, int b) { return __float_as_int(fmaxf(__int_as_float(a), __int_as_float(b))); })));
 }
 
 // x of lanes FIRST + 0, 1, ... of each sixteen
 template <int FIRST, int... N>
 __device__ __forceinline__ void spread(uint32_t x, uint32_t *out, std::integer_sequence<int, N...>)
 {
-    ((out[N] = (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x150 + FIRST + N, 0xf, 0xf, false)), ...);
+    ((out[N] = (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x150 + FIRST + N, 0xf, 0xf, true)), ...);
 }
 // x + that of lane ^ 8 of each sixteen
-__device__ __forceinline__ float add_across_8(float x) { return x + __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x128, 0xf, 0xf, false)); }
+__device__ __forceinline__ float add_across_8(float x) { return x + __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x128, 0xf, 0xf, true)); }
 // x + that of lane ^ 4
 __device__ __forceinline__ float add_across_4(float x) { return x + __shfl_xor(x, 4); }
 
@@ -86,9 +71,12 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
     constexpr int kQ = LO ? (QPARTS + 1) / 2 : QPARTS, kW = LO ? (WPARTS + 1) / 2 : WPARTS;   // products
     typedef std::conditional_t<DIRECT, i32x8, uint4[4]> Row;
     constexpr int kRows = COLS * NT, kSums = QUAD ? 4 : 8;
-    __shared__ __align__(16) uint64_t turns[kBands];
+    typedef std::conditional_t<DIRECT, uint8_t, __bf16> Part;
+    __shared__ int32_t q_unit[kRows], q_pos[kRows];
     __shared__ float wave_m[kWaves][kRows], wave_l[kWaves][kRows];
     __shared__ __align__(16) float wave_o[kWaves][kRows][kHeadDim + 4];
+    Part(*q_parts)[kRows][kHeadDim] = reinterpret_cast<Part(*)[kRows][kHeadDim]>(wave_o);   // (which is written behind the loop, the parts being read before it)
+    static_assert(sizeof(Part[QPARTS][kRows][kHeadDim]) <= sizeof(wave_o), "");
     const AttendSource &src = a.src;
     const CacheView &c = src.cache;
     const int H = c.n_kv_heads, G = a.group_size, Hq = H * G;
@@ -111,13 +99,15 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
     const int k_hi = __builtin_amdgcn_readfirstlane(range.hi);
     const int64_t base = ((int64_t)a.layer * c.stride_layer + (int64_t)h * c.stride_head) / 2;   // bytes
     const int64_t pbase = (int64_t)a.layer * c.pos_stride_layer + (int64_t)h * c.pos_stride_head;
-    const uint32_t sb = (uint32_t)c.stride_slot / 2u;
+    const uint32_t sb = (uint32_t)c.stride_slot / 2u;                       // bytes, too
+    const uint64_t block_bytes = (uint64_t)c.stride_sb / 2u;
     const int in_block = PAGES ? (1 << c.block_shift) - 1 : 0;
     const int my_key = 4 * (m & 3) + (m >> 2);   // of each sixteen, whose row this lane loads
     // A lane has the words of the tile's key 4 m + kq, so that those of keys 16 i + 4 d + kq lie with lane 4 i + d of each sixteen.
     auto lane_of = [&](int key) { return 16 * (key & 3) + (key >> 2); };
     auto of_my_key = [&](uint32_t x, int i) { return (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (16 * (m >> 2) + (m & 3) + 4 * i), (int)x); };   // of key 16 i + my_key
-    auto is_block = [&](int b) { return (b >= 0) & ((src.n_blocks == 0) | (b < src.n_blocks)); };
+    const uint32_t blocks = src.n_blocks ? (uint32_t)src.n_blocks : 0x80000000u;
+    auto is_block = [&](int b) { return (uint32_t)b < blocks; };
     // the block of the lane's key of the 64 from k0 on
     auto block_at = [&](int k0) { return PAGES ? c.block_table[(int64_t)s * c.max_blocks + (min(k0 + 4 * m + kq, max(k_hi - 1, 0)) >> c.block_shift)] : 0; };
     auto there_of = [&](int k0, int block) { return __ballot((k0 + 4 * m + kq < k_hi) & (!PAGES || is_block(block))); };
@@ -147,10 +137,10 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
         int64_t at = base;
         if (PAGES) {
             const int b = __builtin_amdgcn_readlane(block, 4 * i);
-            if (!is_block(b)) left = 0;
-            at += ((int64_t)(left > 0 ? b : 0) * c.stride_sb + (int64_t)(first & in_block) * c.stride_slot) / 2;
+            left = is_block(b) ? left : 0;
+            at += (int64_t)((uint32_t)(left > 0 ? b : 0) * block_bytes + (uint64_t)(uint32_t)(first & in_block) * sb);
         } else {
-            at += ((int64_t)s * c.stride_sb + (int64_t)first * c.stride_slot) / 2;
+            at += (int64_t)((uint32_t)s * block_bytes + (uint64_t)(uint32_t)first * sb);
         }
         *keys = left;
         return at;
@@ -158,10 +148,12 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
     // (PAGES 2: below sixteen slots) the row of the tile's key `key`; keys that are not there bring the pool's first row, with scales of zero
     auto slot_of = [&](int k0, int key, int block, uint64_t there) {
         const int from = lane_of(key), b = __shfl(block, from);
-        return (there >> from) & 1 ? base + ((int64_t)b * c.stride_sb + slot_offset(c, (k0 + key) & in_block)) / 2 : base;
+        return (there >> from) & 1 ? base + (int64_t)((uint32_t)b * block_bytes + (uint64_t)(uint32_t)((k0 + key) & in_block) * sb) : base;
     };
     uint4 k[4];
     uint32_t v[4][4];
+    int64_t at[4];
+    int keys[4];
     auto load_k = [&](int k0, int block, uint64_t there) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -176,9 +168,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
                 }
                 continue;
             }
-            int keys;
-            const int64_t at = place(k0, i, block, &keys);
-            const auto b = rsrc(c.k, at, keys);
+            at[i] = place(k0, i, block, &keys[i]);
+            const auto b = rsrc(c.k, at[i], keys[i]);
             if (DIRECT) {
                 k[i] = as_uint4(__builtin_amdgcn_raw_buffer_load_b128(b, my_key * sb + 16 * kq, 0, kNonTemporal));
             } else {
@@ -195,9 +186,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
                 for (int d = 0; d < 4; ++d) v[i][d] = *reinterpret_cast<const uint32_t *>((const char *)c.v + slot_of(k0, 16 * i + 4 * d + kq, block, there) + 4 * m);
                 continue;
             }
-            int keys;
-            const int64_t at = place(k0, i, block, &keys);
-            const auto b = rsrc(c.v, at, keys);
+            const auto b = rsrc(c.v, at[i], keys[i]);
 #pragma unroll
             for (int d = 0; d < 4; ++d) v[i][d] = __builtin_amdgcn_raw_buffer_load_b32(b, kq * sb + 4 * m, 4 * d * sb, kNonTemporal);
         }
@@ -211,7 +200,57 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
     load_k(k0, block, there);
     load_v(k0, block, there);
     int ahead = block_at(k0 + kStep);
-    if (tid < kBands) turns[tid] = a.turns.w[tid];
+    // A wave turns the rows wave, wave + 4, ..., a band to a lane, and writes down their parts.
+    {
+        constexpr int kTurns = (kRows + kWaves - 1) / kWaves;
+        const uint64_t turn = a.rotate_q ? a.turns.w[lane] : 0;
+        float re[kTurns], im[kTurns];
+        int32_t pos[kTurns];
+#pragma unroll
+        for (int i = 0; i < kTurns; ++i) {
+            const int r = r0 + min(wave + kWaves * i, rows - 1), token = tr.t0 + r / G, hq = h * G + r % G;
+            load_band(reinterpret_cast<const T *>(a.q) + (int64_t)token * a.q_stride_token + (int64_t)hq * a.q_stride_head, lane, a.half, &re[i], &im[i]);
+            pos[i] = a.causal || a.rotate_q ? a.pos[token] : 0;
+        }
+#pragma unroll
+        for (int i = 0; i < kTurns; ++i) {
+            const int row = wave + kWaves * i;
+            if (row >= rows) break;
+            float x = re[i], y = im[i];
+            if (a.rotate_q) {
+                float c, s;
+                const uint32_t phase = phase_of(pos[i], (uint32_t)turn, (uint32_t)(turn >> 32));
+                if (DIRECT) turn_fast(phase, &c, &s);
+                else turn_exact(phase, &c, &s);
+                x = fmaf(re[i], c, -(im[i] * s));
+                y = fmaf(re[i], s, im[i] * c);
+            }
+            if constexpr (DIRECT) {
+                // the power of two of the row's largest, at least what leaves the last part a scale
+                const int unit = max((int)(__float_as_uint(most_of_wave(fmaxf(fabsf(x), fabsf(y)))) >> 23), 127 - 99);
+                const float by = __uint_as_float((uint32_t)(261 - unit) << 23);
+                x *= by, y *= by;
+#pragma unroll
+                for (int p = 0; p < QPARTS; ++p) {
+                    const int w = __builtin_amdgcn_cvt_pk_fp8_f32(x, y, 0, false);
+                    if (a.half) q_parts[p][row][lane] = (uint8_t)w, q_parts[p][row][lane + 64] = (uint8_t)(w >> 8);
+                    else *reinterpret_cast<uint16_t *>(&q_parts[p][row][2 * lane]) = (uint16_t)w;
+                    x = (x - __builtin_amdgcn_cvt_f32_fp8(w, 0)) * 16.f;
+                    y = (y - __builtin_amdgcn_cvt_f32_fp8(w, 1)) * 16.f;
+                }
+                if (lane == 0) q_unit[row] = unit;
+            } else {
+#pragma unroll
+                for (int p = 0; p < QPARTS; ++p) {
+                    const __bf16 u = (__bf16)x, w = (__bf16)y;
+                    q_parts[p][row][a.half ? lane : 2 * lane] = u;
+                    q_parts[p][row][a.half ? lane + 64 : 2 * lane + 1] = w;
+                    x -= (float)u, y -= (float)w;
+                }
+            }
+            if (lane == 0) q_pos[row] = pos[i];
+        }
+    }
     __syncthreads();
 
     // this lane's rows: columns m of the column tiles
@@ -220,60 +259,28 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
     int32_t t_pos[NT], first_pos = 0x7fffffff;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-        const int at = t * COLS + (m & (COLS - 1)), r = r0 + min(at, rows - 1), token = tr.t0 + r / G, hq = h * G + r % G;
-        t_pos[t] = a.causal ? a.pos[token] : 0x7fffffff;
+        const int row = min(t * COLS + (m & (COLS - 1)), rows - 1);
+        t_pos[t] = a.causal ? q_pos[row] : 0x7fffffff;
         first_pos = min(first_pos, t_pos[t]);
-        float x[32];
-        load_q<T>(a.q + ((int64_t)token * a.q_stride_token + (int64_t)hq * a.q_stride_head) * (int64_t)sizeof(T), kq, a.rotate_q, a.half, a.rotate_q ? a.pos[token] : 0, turns, x);
-        if constexpr (DIRECT) {
-            float most = 0.f;
+        q_scale[t] = 0;
 #pragma unroll
-            for (int e = 0; e < 32; ++e) most = fmaxf(most, fabsf(x[e]));
-            most = max_over_kq(most);
-            // the power of two of the row's largest, at least what leaves the last part a scale
-            const int unit = max((int)(__float_as_uint(most) >> 23), 127 - 99);
-            const float by = __uint_as_float((uint32_t)(261 - unit) << 23);
-#pragma unroll
-            for (int e = 0; e < 32; ++e) x[e] *= by;
-#pragma unroll
-            for (int p = 0; p < QPARTS; ++p)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    int w = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * j], x[4 * j + 1], 0, false);
-                    w = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * j + 2], x[4 * j + 3], w, true);
-                    if (!LO) q[t][p % kQ][j] = w;
-                    else if (p % 2 == 0) q[t][p / 2][j] = w;
-                    else q[t][p / 2][j] = m >= 8 ? w : q[t][p / 2][j];
-                    x[4 * j] = (x[4 * j] - __builtin_amdgcn_cvt_f32_fp8(w, 0)) * 16.f;
-                    x[4 * j + 1] = (x[4 * j + 1] - __builtin_amdgcn_cvt_f32_fp8(w, 1)) * 16.f;
-                    x[4 * j + 2] = (x[4 * j + 2] - __builtin_amdgcn_cvt_f32_fp8(w, 2)) * 16.f;
-                    x[4 * j + 3] = (x[4 * j + 3] - __builtin_amdgcn_cvt_f32_fp8(w, 3)) * 16.f;
-                }
-            const uint32_t first = unit - 7 - (LO && m >= 8 ? 4 : 0), apart = LO ? 8 : 4;
-            q_scale[t] = 0;
-#pragma unroll
-            for (int p = 0; p < kQ; ++p) q_scale[t] |= (first - apart * p) << (8 * p);
-        } else {
-#pragma unroll
-            for (int p = 0; p < QPARTS; ++p)
+        for (int p = 0; p < kQ; ++p) {
+            const int part = LO ? min(2 * p + (m >= 8), QPARTS - 1) : p;
+            const uint4 *from = reinterpret_cast<const uint4 *>(q_parts[part][row]);
+            if constexpr (DIRECT) {
+                const uint4 x = from[kq], y = from[4 + kq];
+                q[t][p] = i32x8{(int)x.x, (int)x.y, (int)x.z, (int)x.w, (int)y.x, (int)y.y, (int)y.z, (int)y.w};
+                q_scale[t] |= (uint32_t)(q_unit[row] - 7 - 4 * part) << (8 * p);
+            } else {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    bf16x8 part;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        part[e] = (__bf16)x[8 * j + e];
-                        x[8 * j + e] -= (float)part[e];
-                    }
-                    const uint4 w = __builtin_bit_cast(uint4, part), none = make_uint4(0, 0, 0, 0);
-                    if (!LO) q[t][p % kQ][j] = w;
-                    else if (p % 2 == 0) q[t][p / 2][j] = p + 1 < QPARTS || m < 8 ? w : none;
-                    else q[t][p / 2][j] = m >= 8 ? w : q[t][p / 2][j];
+                    q[t][p][j] = from[8 * (j / 2) + 2 * kq + j % 2];
+                    if (LO && 2 * p + 1 >= QPARTS && m >= 8) q[t][p][j] = make_uint4(0, 0, 0, 0);   // (three parts: the last has its product to itself)
                 }
+            }
         }
     }
-#pragma unroll
-    for (int i = 1; i < 16; i *= 2) first_pos = min(first_pos, __shfl_xor(first_pos, i));
-    first_pos = __builtin_amdgcn_readfirstlane(first_pos);
+    first_pos = __builtin_amdgcn_readfirstlane(over_16(first_pos, [](int x, int y) { return min(x, y); }));
 
     // (QUAD) bytes 1, 0 below zeros or above them; of the upper half
     const uint32_t pick = m < 8 ? 0x0c0c0100u : 0x01000c0cu, pick_next = m < 8 ? 0x0202u : 0x02020000u;
@@ -336,7 +343,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
                     for (int d = 0; d < 4; ++d) sc[i][t][d] = add_across_8(sc[i][t][d]);
         }
         // keys that are not there, or behind the position of one of the rows
-        const bool late = a.causal && __ballot(((there >> lane) & 1) && here.pos > first_pos);
+        const bool late = __ballot(((there >> lane) & 1) & (here.pos > first_pos));   // (not causal: nothing is)
         if (late || there != ~0ull) {
             const uint32_t is = (uint32_t)(there >> (16 * kq));   // bit 4 i + d
             int32_t p[16];
@@ -345,7 +352,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
             for (int n = 0; n < 16; ++n)
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
-                    if (!((is >> n) & 1) || (a.causal && p[n] > t_pos[t])) sc[n / 4][t][n % 4] = kNoScore;
+                    if (!((is >> n) & 1) | (p[n] > t_pos[t])) sc[n / 4][t][n % 4] = kNoScore;
         }
         float best[NT];
         bool higher = false;
@@ -531,7 +538,10 @@ AttendSplit attend4_split(const tri_model &m, const tri_cache &c, int32_t max_to
 {
     const int64_t G = m.n_q_heads / m.n_kv_heads, rows = max_tokens * G, per = tile_rows(type, rows);
     const bool tile = is_tile(type, rows);
-    const int64_t part = tile ? 8192 : 4096;
+    #ifndef P4
+#define P4 4096
+#endif
+    const int64_t part = tile ? 8192 : P4;
     const int64_t tiles = std::max<int64_t>(c.n_seqs, (n_tokens * G + per - 1) / per + c.n_seqs / 2);
     const int64_t units = m.n_kv_heads * tiles;
     const int64_t least = tile ? 256 : std::min<int64_t>(part, std::max<int64_t>(256, part * units / 256));
