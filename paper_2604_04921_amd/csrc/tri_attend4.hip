@@ -88,10 +88,10 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
     const uint32_t turned = w - head * n + ((head * even / 32) & (even - 1));
     const int split = turned < n ? turned : turned - n, h = head % H, s = head / H;
     const TokenRange tr = tokens_of(a, src, s);
+    const KeyRange range = keys_of_split(a, src, s, h, split);   // (both are asked for at once)
     const int r0 = (int)row_tile * kRows, all_rows = tr.n * G, rows = min(all_rows - r0, kRows);
     if (rows <= 0) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15, kq = lane >> 4;
-    const KeyRange range = keys_of_split(a, src, s, h, split);
     if (range.lo >= range.hi && a.part_o) {
         no_keys(a, src, split, tr.t0, r0, rows, h, Hq);
         return;
@@ -193,25 +193,24 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
     };
     constexpr int kStep = kWaves * kTile;
     int k0 = __builtin_amdgcn_readfirstlane(range.lo) + kTile * wave;
-    // The first tile is asked for before anything is known of the queries.
+    // A wave turns the rows wave, wave + 4, ..., a band to a lane.  They are asked for ahead of the first tile (loads come in their order), which is on its way while they are turned.
+    constexpr int kTurns = (kRows + kWaves - 1) / kWaves;
+    const uint64_t turn = a.rotate_q ? a.turns.w[lane] : 0;
+    float re[kTurns], im[kTurns];
+    int32_t pos[kTurns];
+#pragma unroll
+    for (int i = 0; i < kTurns; ++i) {
+        const int r = r0 + min(wave + kWaves * i, rows - 1), token = tr.t0 + r / G, hq = h * G + r % G;
+        load_band(reinterpret_cast<const T *>(a.q) + (int64_t)token * a.q_stride_token + (int64_t)hq * a.q_stride_head, lane, a.half, &re[i], &im[i]);
+        pos[i] = a.causal || a.rotate_q ? a.pos[token] : 0;
+    }
     int block = block_at(k0);
     uint64_t there = there_of(k0, block);
     Words words = load_words(k0, block, there);
     load_k(k0, block, there);
     load_v(k0, block, there);
     int ahead = block_at(k0 + kStep);
-    // A wave turns the rows wave, wave + 4, ..., a band to a lane, and writes down their parts.
     {
-        constexpr int kTurns = (kRows + kWaves - 1) / kWaves;
-        const uint64_t turn = a.rotate_q ? a.turns.w[lane] : 0;
-        float re[kTurns], im[kTurns];
-        int32_t pos[kTurns];
-#pragma unroll
-        for (int i = 0; i < kTurns; ++i) {
-            const int r = r0 + min(wave + kWaves * i, rows - 1), token = tr.t0 + r / G, hq = h * G + r % G;
-            load_band(reinterpret_cast<const T *>(a.q) + (int64_t)token * a.q_stride_token + (int64_t)hq * a.q_stride_head, lane, a.half, &re[i], &im[i]);
-            pos[i] = a.causal || a.rotate_q ? a.pos[token] : 0;
-        }
 #pragma unroll
         for (int i = 0; i < kTurns; ++i) {
             const int row = wave + kWaves * i;
@@ -538,14 +537,11 @@ AttendSplit attend4_split(const tri_model &m, const tri_cache &c, int32_t max_to
 {
     const int64_t G = m.n_q_heads / m.n_kv_heads, rows = max_tokens * G, per = tile_rows(type, rows);
     const bool tile = is_tile(type, rows);
-    #ifndef P4
-#define P4 4096
-#endif
-    const int64_t part = tile ? 8192 : P4;
+        const int64_t part = tile ? 8192 : 3500;
     const int64_t tiles = std::max<int64_t>(c.n_seqs, (n_tokens * G + per - 1) / per + c.n_seqs / 2);
     const int64_t units = m.n_kv_heads * tiles;
     const int64_t least = tile ? 256 : std::min<int64_t>(part, std::max<int64_t>(256, part * units / 256));
-    const int64_t fill = std::max<int64_t>(1, (512 + units / 2) / units);
+    const int64_t fill = std::max<int64_t>(1, ((tile ? 512 : 768) + units / 2) / units);
     const int64_t room = ((int64_t)64 << 20) / (std::max<int64_t>(n_tokens, 1) * m.n_q_heads * kHeadDim * (int64_t)sizeof(float));
     int64_t want = std::max<int64_t>(fill, std::min<int64_t>(c.max_seq_len / part, room));
     if (want * units < 2048) want = want / fill * fill;
