@@ -1,4 +1,6 @@
 // Attention with many rows per KV head (chunks of prompts, batches behind a shared prefix): bf16, contiguous caches and pages of any size.
+#include <type_traits>
+
 #include "tri_attend_common.h"
 #include "tri_serve4.h"
 
@@ -9,6 +11,7 @@ namespace {
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 typedef __attribute__((address_space(3))) void lds_void;
 
@@ -80,11 +83,14 @@ struct TileBuffer {
 // 322, eight waves to a workgroup 382; the loads' issue is a quarter of the time (without them, on stale tiles, 245 of 322).  Without neighbours on one XCD two prompts' 256 sequences take 379 us, with 229.
 // That is with queries and keys as they are.  Two chunks of 1024 over 8192 keys each, contiguous, take 294 us so, 383 with queries turned on the way and 452 with keys too: every row tile turns its keys again, and what
 // does not fit is spilled (6 to 9 registers with queries turned, 11 to 21 with keys).
-// FOUR: keys and values are held in 4 bits.  A lane brings 32 elements of a row, which have one scale, and put() writes what they stand for into LDS: bf16 numbers or, where queries are turned, fp16 ones.
+// FOUR: keys and values are held in 4 bits.  A lane brings 32 elements of a row, which have one scale.  Values are written into LDS as the bf16 numbers that they stand for; keys as they are, with their scales, for
+// v_mfma_scale_f32_32x32x64_f8f6f4, which takes queries as e4m3 numbers: two to an element, four bits each, which is all a bf16 number has, or three where queries are turned (see attend4_rows_kernel).  Keys as bf16 numbers in LDS
+// took four times the reads and as many conversions as values: the two chunks above 291 us over a cache in 4 bits, KEYS_US so.
 template <int PAGES, Keys KEYS, bool HALF, bool FOUR = false>
 __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs a)
 {
-    constexpr bool TURN = KEYS == kTurn, F16 = KEYS != kAsTheyAre;
+    constexpr bool TURN = KEYS == kTurn, F16 = KEYS != kAsTheyAre && !FOUR;
+    constexpr int kParts = KEYS == kAsTheyAre ? 2 : 3;   // FOUR: e4m3 numbers to an element of q
     constexpr int kLanes = 64 / kKeys, kPieces = 16 / kLanes;   // F16: lanes to a row of K, pieces to a lane
     __shared__ __align__(16) uint64_t turns[kBands];
     // (two objects and two copies of the loop's body: the compiler then knows that reading one does not have to wait for the loads into the other)
@@ -216,33 +222,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
     auto put = [&](TileBuffer &to) __attribute__((always_inline)) {
         bool scaled = false;
         if constexpr (FOUR) {
+            // (pieces of 16 bytes lie at their number exclusive-or a quarter of the row, so that reads of one piece of sixteen neighbouring rows meet different banks)
             const uint32_t l = lane_again(), row = l >> 2, g = l & 3;
-            uint4 *k = reinterpret_cast<uint4 *>(to.k + (kKeys * wave + row) * kHeadDim), *v = reinterpret_cast<uint4 *>(to.v + (kKeys * wave + row) * kHeadDim);
-            const uint32_t kw[4] = {k_new.x, k_new.y, k_new.z, k_new.w}, vw[4] = {v_new.x, v_new.y, v_new.z, v_new.w};
-            if (F16) {
-                // fp16 as they are from scales of 2^-8 (below 2^-23 bits are lost, 2^-19 of the row's largest at most) to 2^12; else the row's largest scale is its unit
-                const int byte = (k_scale_new >> (8 * g)) & 255;
-                int most = byte == kScaleNaN ? 0 : byte;
-                most = max(most, __builtin_amdgcn_update_dpp(0, most, 0xb1, 0xf, 0xf, false));   // (lane ^ 1, lane ^ 2)
-                most = max(most, __builtin_amdgcn_update_dpp(0, most, 0x4e, 0xf, 0xf, false));
-                scaled = __ballot(most > 127 + 12 || (most < 127 - 8 && most > kScaleLeast));
-                const int unit = scaled && most > kScaleLeast ? most : 127;
-                const float scale = __uint_as_float((uint32_t)(byte == kScaleNaN ? byte : max(byte - unit + 127, 0)) << 23);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    uint4 x;
-                    x.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(kw[j], scale, 0));
-                    x.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(kw[j], scale, 1));
-                    x.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(kw[j], scale, 2));
-                    x.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(kw[j], scale, 3));
-                    k[(4 * g + j) ^ row] = x;
-                }
-                if (g == 0) to.unit[kKeys * wave + row] = __uint_as_float((uint32_t)unit << 23);
-            } else {
-                const float scale = scale_at(k_scale_new, g);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) k[(4 * g + j) ^ row] = read8(kw[j], scale);
-            }
+            uint4 *k = reinterpret_cast<uint4 *>(to.k) + (kKeys * wave + row) * 4, *v = reinterpret_cast<uint4 *>(to.v + (kKeys * wave + row) * kHeadDim);
+            const uint32_t vw[4] = {v_new.x, v_new.y, v_new.z, v_new.w};
+            k[g ^ ((row >> 2) & 3)] = k_new;
+            if (g == 0) to.unit[kKeys * wave + row] = __uint_as_float(k_scale_new);
             const float scale = scale_at(v_scale_new, g);
 #pragma unroll
             for (int j = 0; j < 4; ++j) v[(4 * g + j) ^ (2 * (row & 7))] = read8(vw[j], scale);
@@ -317,8 +302,66 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
     const int32_t t_pos = a.causal ? a.pos[t] : 0x7fffffff;
     int32_t first_pos = t_pos, last_pos = real ? t_pos : -0x7fffffff - 1;
     bf16x8 q[8];
+    i32x8 q8[FOUR ? kParts : 1][2];   // FOUR: the first and the last 64 dimensions, each 16 h to 16 h + 15 and those 32 further on
+    uint32_t q_scale = 0;             // FOUR: a byte for every part
     float unit = 1.f;   // of the row's q
-    {
+    if constexpr (FOUR) {
+        const char *p = a.q + ((int64_t)t * a.q_stride_token + (int64_t)hq * a.q_stride_head) * 2 + 32 * h;
+        float x[2][32], most = 0.f;   // x[i]: of the i-th 64 dimensions
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) widen8(*reinterpret_cast<const uint4 *>(p + 128 * i + 64 * (j / 2) + 16 * (j % 2)), x[i] + 8 * j);
+        if (a.rotate_q) {
+            const int32_t turn_pos = a.pos[t];
+            const auto turn = [&](int f, float &re, float &im) {
+                const uint64_t w = turns[f];
+                float cs, sn;
+                turn_fast(phase_of(turn_pos, (uint32_t)w, (uint32_t)(w >> 32)), &cs, &sn);
+                const float x0 = re, y0 = im;
+                re = fmaf(x0, cs, -(y0 * sn));
+                im = fmaf(x0, sn, y0 * cs);
+            };
+            if (a.half) {
+#pragma unroll
+                for (int e = 0; e < 32; ++e) turn(32 * (e / 16) + 16 * h + e % 16, x[0][e], x[1][e]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) turn(32 * i + 16 * (e / 8) + 8 * h + e % 8, x[i][2 * e], x[i][2 * e + 1]);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int e = 0; e < 32; ++e) most = fmaxf(most, fabsf(x[i][e]));
+        most = fmaxf(most, __shfl_xor(most, 32));
+        // the first part of the row's largest is in [128, 256); a part's scale is 2^-4 of the last one's
+        const int power = max((int)(__float_as_uint(most) >> 23), 127 - 99);
+        const float by = __uint_as_float((uint32_t)(261 - power) << 23);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int e = 0; e < 32; ++e) x[i][e] *= by;
+#pragma unroll
+        for (int n = 0; n < kParts; ++n) {
+            q_scale |= (uint32_t)(power - 7 - 4 * n) << (8 * n);
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    float *y = x[i] + 4 * j;
+                    int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+                    w = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true);
+                    q8[n][i][j] = w;
+                    y[0] = (y[0] - __builtin_amdgcn_cvt_f32_fp8(w, 0)) * 16.f;
+                    y[1] = (y[1] - __builtin_amdgcn_cvt_f32_fp8(w, 1)) * 16.f;
+                    y[2] = (y[2] - __builtin_amdgcn_cvt_f32_fp8(w, 2)) * 16.f;
+                    y[3] = (y[3] - __builtin_amdgcn_cvt_f32_fp8(w, 3)) * 16.f;
+                }
+        }
+    } else {
         const char *p = a.q + ((int64_t)t * a.q_stride_token + (int64_t)hq * a.q_stride_head) * 2 + 16 * h;
         if (F16) {
             float v[8][8], most = 0.f;
@@ -401,7 +444,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
         for (int u = 0; u < 2; ++u)
 #pragma unroll
             for (int i = 0; i < 16; ++i) sc[u][i] = 0.f;
-        bf16x8 k[2][8], v[2][4];   // v[u][j]: dimensions 32 j + col, the keys of weight[u]
+        bf16x8 k[FOUR ? 1 : 2][8], v[2][4];   // v[u][j]: dimensions 32 j + col, the keys of weight[u]
         auto values = [&](int U) __attribute__((always_inline)) {
 #pragma unroll
             for (int u = 0; u < 2; ++u)
@@ -413,6 +456,39 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
                     v[u][j] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
                 }
         };
+        if constexpr (FOUR) {
+            uint4 k4[2][2];   // [u][i]: the i-th 64 dimensions
+            uint32_t k_scale[2];
+            const uint32_t row = lane_again() & 31, half = lane_again() >> 5;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) k4[u][i] = reinterpret_cast<const uint4 *>(from.k)[(32 * u + row) * 4 + ((2 * i + half) ^ ((row >> 2) & 3))];
+                k_scale[u] = __float_as_uint(from.unit[32 * u + row]) >> (8 * half);   // bytes 0 and 2
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const i32x8 x{(int)k4[u][i].x, (int)k4[u][i].y, (int)k4[u][i].z, (int)k4[u][i].w, 0, 0, 0, 0};
+                    const auto product = [&](auto part) {
+                        constexpr int n = decltype(part)::value;
+                        if constexpr (n < kParts) {
+                            if (i == 0) sc[u] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, q8[n][0], sc[u], 4, 0, 0, k_scale[u], n, q_scale);
+                            else sc[u] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, q8[n][1], sc[u], 4, 0, 2, k_scale[u], n, q_scale);
+                        }
+                    };
+                    product(std::integral_constant<int, 2>()), product(std::integral_constant<int, 1>()), product(std::integral_constant<int, 0>());
+                }
+                if (u == 0) {
+                    values(0);   // asked for ahead of the softmax
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            __builtin_amdgcn_s_setprio(0);
+        } else {
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -426,6 +502,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
 #pragma unroll
         for (int j = 0; j < 8; ++j) sc[1] = scores<F16>(k[1][j], q[j], sc[1]);
         __builtin_amdgcn_s_setprio(0);
+        }
         if (F16 && scaled) {
 #pragma unroll
             for (int u = 0; u < 2; ++u)
