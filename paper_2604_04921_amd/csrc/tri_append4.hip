@@ -8,32 +8,77 @@ namespace tri {
 namespace {
 
 constexpr int kPackThreads = 256, kLanes = 8, kPackRows = kPackThreads / kLanes;   // threads to a row, rows of a workgroup
-constexpr int kReadPasses = 4, kReadRows = kReadPasses * kPackThreads / 16;
+constexpr int kReadPasses = 2, kReadRows = kReadPasses * kPackThreads / 16;
 
+// Eight elements of a row as they come.
 template <typename T>
-__device__ __forceinline__ void load8(const char *p, float *x);
+struct Eight;
 template <>
-__device__ __forceinline__ void load8<float>(const char *p, float *x)
-{
-    const uint4 a = load_stream16(p), b = load_stream16(p + 16);
-    const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+struct Eight<float> {
+    uint32_t w[8];
+    __device__ __forceinline__ void load(const float *p)
+    {
+        // (not non-temporal: a lane's two pieces are halves of one line with its neighbour's; three fp32 caches packed and read back 21 us, 25 with that hint)
+        const uint4 a = *reinterpret_cast<const uint4 *>(p), b = *reinterpret_cast<const uint4 *>(p + 4);
+        w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w, w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
+    }
+    __device__ __forceinline__ void widen(float *x) const
+    {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(w[i]);
-}
+        for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(w[i]);
+    }
+    __device__ __forceinline__ uint32_t most() const   // bits of the largest magnitude, that of what is no number being the largest
+    {
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = max(m, w[i] & 0x7fffffffu);
+        return m;
+    }
+    __device__ __forceinline__ uint32_t codes(float scale) const
+    {
+        uint32_t r = 0;
+        r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, __uint_as_float(w[0]), __uint_as_float(w[1]), scale, 0);
+        r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, __uint_as_float(w[2]), __uint_as_float(w[3]), scale, 1);
+        r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, __uint_as_float(w[4]), __uint_as_float(w[5]), scale, 2);
+        return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, __uint_as_float(w[6]), __uint_as_float(w[7]), scale, 3);
+    }
+};
 template <>
-__device__ __forceinline__ void load8<__bf16>(const char *p, float *x)
-{
-    const uint4 a = load_stream16(p);
-    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+struct Eight<__bf16> {
+    uint32_t w[4];
+    __device__ __forceinline__ void load(const __bf16 *p)
+    {
+        const uint4 a = load_stream16((const char *)p);
+        w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w;
+    }
+    __device__ __forceinline__ void widen(float *x) const
+    {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(w[i] << 16), x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-}
+        for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(w[i] << 16), x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+    __device__ __forceinline__ uint32_t most() const
+    {
+        typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+        u16x2 m{0, 0};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, w[i] & 0x7fff7fffu));
+        return (uint32_t)max(m[0], m[1]) << 16;
+    }
+    __device__ __forceinline__ uint32_t codes(float scale) const
+    {
+        uint32_t r = 0;
+        r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(bf16x2, w[0]), scale, 0);
+        r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(bf16x2, w[1]), scale, 1);
+        r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(bf16x2, w[2]), scale, 2);
+        return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(bf16x2, w[3]), scale, 3);
+    }
+};
 
 // The four lanes of 32 elements.
 __device__ __forceinline__ uint32_t most_of_4(uint32_t x)
 {
-    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xb1, 0xf, 0xf, false));          // lane ^ 1
-    return max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x4e, 0xf, 0xf, false));       // lane ^ 2
+    x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0xb1, 0xf, 0xf, true));          // lane ^ 1
+    return max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x4e, 0xf, 0xf, true));       // lane ^ 2
 }
 __device__ __forceinline__ double most_of_4(double x)
 {
@@ -50,15 +95,26 @@ __device__ __forceinline__ uint32_t codes8(const float *x, float scale)
     return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], scale, 3);
 }
 
-// Element d of a row rotated in double precision: the angle is the position's product with the band's frequency modulo one revolution, off by |pos| 2^-62 revolutions at most.
+// Element d of a row rotated in double precision: the angle is the position's product with the band's frequency modulo one revolution, off by |pos| 2^-62 revolutions at most; less the nearest quarter turn it is
+// at most pi / 4, where the Taylor polynomials of degree 17 and 16 are off by less than 2^-58.
 template <typename T, bool HALF>
 __device__ double rotated(const T *row, int d, int32_t pos, const BandTurns &turns)
 {
     const int f = HALF ? d & 63 : d >> 1;
     const double re = (double)row[HALF ? f : 2 * f], im = (double)row[HALF ? f + 64 : 2 * f + 1];
-    const int64_t phase = (int64_t)((uint64_t)(int64_t)pos * turns.w[f]);
-    double s, c;
-    sincospi((double)phase * 0x1p-63, &s, &c);
+    const uint64_t phase = (uint64_t)(int64_t)pos * turns.w[f], quarter = (phase + (1ull << 61)) >> 62;
+    const double x = (double)(int64_t)(phase - (quarter << 62)) * (6.283185307179586476925 * 0x1p-64), z = x * x;
+    double sn = 1.0 / 355687428096000.0, cs = 1.0 / 20922789888000.0;   // 1 / 17!, 1 / 16!
+    sn = fma(sn, z, -1.0 / 1307674368000.0), cs = fma(cs, z, -1.0 / 87178291200.0);
+    sn = fma(sn, z, 1.0 / 6227020800.0), cs = fma(cs, z, 1.0 / 479001600.0);
+    sn = fma(sn, z, -1.0 / 39916800.0), cs = fma(cs, z, -1.0 / 3628800.0);
+    sn = fma(sn, z, 1.0 / 362880.0), cs = fma(cs, z, 1.0 / 40320.0);
+    sn = fma(sn, z, -1.0 / 5040.0), cs = fma(cs, z, -1.0 / 720.0);
+    sn = fma(sn, z, 1.0 / 120.0), cs = fma(cs, z, 1.0 / 24.0);
+    sn = fma(sn, z, -1.0 / 6.0), cs = fma(cs, z, -0.5);
+    sn = fma(sn * z, x, x), cs = fma(cs, z, 1.0);
+    const double a = quarter & 1 ? sn : cs, b = quarter & 1 ? cs : sn;
+    const double c = (quarter + 1) & 2 ? -a : a, s = quarter & 2 ? -b : b;
     return (HALF ? d < 64 : !(d & 1)) ? fma(re, c, -(im * s)) : fma(re, s, im * c);
 }
 __device__ __forceinline__ uint32_t code_of(double v, uint32_t byte)
@@ -72,68 +128,85 @@ struct Codes {
     uint32_t byte[2];    // their scales
 };
 
-// A lane's sixteen elements x, unrotated, to 4 bits.  TURN: rotated first.  In fp32 a rotated element is off by at most (|re| + |im|) 2^-20 (sine and cosine by 2.2e-7, the products' roundings); where what lies within
-// that of it does not all have one code, or the group's largest not one scale, the element is worked out in double precision: one wave in thirty of Gaussian rows.
-template <typename T, bool TURN, bool HALF>
-__device__ __forceinline__ Codes to_codes(float (*x)[8], const T *row, int32_t pos, const BandTurns &turns, int part)
+// A lane's sixteen elements, as they are, to 4 bits.
+template <typename T>
+__device__ __forceinline__ Codes to_codes(const Eight<T> (&x)[2])
 {
-    float off[2][8];
-    if (TURN) {
+    Codes got;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {   // eight bands
-            float &r = HALF ? x[0][e] : x[e / 4][2 * (e & 3)], &i = HALF ? x[1][e] : x[e / 4][2 * (e & 3) + 1];
-            const uint64_t w = turns.w[HALF ? 8 * part + e : 32 * (e / 4) + 4 * part + (e & 3)];
-            float cs, sn;
-            turn_exact(phase_of(pos, (uint32_t)w, (uint32_t)(w >> 32)), &cs, &sn);
-            const float re = r, im = i;
-            (HALF ? off[0][e] : off[e / 4][2 * (e & 3)]) = (HALF ? off[1][e] : off[e / 4][2 * (e & 3) + 1]) = (fabsf(re) + fabsf(im)) * 0x1p-20f;
-            r = fmaf(re, cs, -(im * sn));
-            i = fmaf(re, sn, im * cs);
-        }
+    for (int p = 0; p < 2; ++p) {
+        got.byte[p] = scale_byte(most_of_4(x[p].most()));
+        got.word[p] = got.byte[p] == kScaleNaN ? 0 : x[p].codes(__uint_as_float(got.byte[p] << 23));
+    }
+    return got;
+}
+
+// Cosine and sine of a lane's eight bands at a position.
+struct Angles {
+    float c[8], s[8];
+};
+template <bool HALF>
+__device__ __forceinline__ Angles angles_of(int32_t pos, const BandTurns &turns, int part)
+{
+    Angles a;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const uint64_t w = turns.w[HALF ? 8 * part + e : 32 * (e / 4) + 4 * part + (e & 3)];
+        turn_fast(phase_of(pos, (uint32_t)w, (uint32_t)(w >> 32)), &a.c[e], &a.s[e]);
+    }
+    return a;
+}
+
+// A lane's sixteen elements to 4 bits, rotated first.  In fp32 a rotated element is off by less than (|re| + |im|) 2^-21: the hardware's cosine and sine by 1.9e-7 (measured over all 2^32 phases), the angle by 5e-9, the
+// products' roundings by 2^-23.  |re| + |im| is at most twice the larger of the pair's rotated elements, of which `apart` below has the largest, its own error being far below the bound's slack.  Where what lies within
+// `apart` of an element does not all have one code, or the group's largest not one scale, the element is worked out in double precision: one or two waves in a hundred of Gaussian rows.
+template <typename T, bool HALF>
+__device__ __forceinline__ Codes to_codes(const Eight<T> (&raw)[2], const Angles &angles, const T *row, int32_t pos, const BandTurns &turns, int part)
+{
+    float x[2][8];
+    raw[0].widen(x[0]);
+    raw[1].widen(x[1]);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        float &r = HALF ? x[0][e] : x[e / 4][2 * (e & 3)], &i = HALF ? x[1][e] : x[e / 4][2 * (e & 3) + 1];
+        const float re = r, im = i;
+        r = fmaf(re, angles.c[e], -(im * angles.s[e]));
+        i = fmaf(re, angles.s[e], im * angles.c[e]);
+    }
+    uint32_t bits_of[2];
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+        bits_of[p] = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) bits_of[p] = max(bits_of[p], __float_as_uint(x[p][e]) & 0x7fffffffu);   // (what is no number is the largest)
+        bits_of[p] = most_of_4(bits_of[p]);
     }
     Codes got;
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
-        uint32_t hi = 0, lo = 0;
-        bool odd = false;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const uint32_t a = __float_as_uint(x[p][e]) & 0x7fffffffu;
-            if (TURN) {
-                odd |= a >= 0x7f800000u;
-                hi = max(hi, min(__float_as_uint(fabsf(x[p][e]) + off[p][e]), 0x7f7fffffu));
-                lo = max(lo, __float_as_uint(fmaxf(fabsf(x[p][e]) - off[p][e], 0.f)));
-            } else {
-                hi = max(hi, a);
-            }
-        }
-        if (TURN && odd) hi = lo = 0xffffffffu;
-        hi = most_of_4(hi);
-        uint32_t byte = scale_byte(hi);
-        if (TURN) {
-            lo = most_of_4(lo);
-            if (hi < 0x7f800000u && scale_byte(lo) != byte) {   // (all four lanes)
-                double most = 0.0;
-                for (int e = 0; e < 8; ++e) most = fmax(most, fabs(rotated<T, HALF>(row, 64 * p + 8 * part + e, pos, turns)));
-                byte = scale_byte(most_of_4(most));
+        const uint32_t bits = bits_of[p];
+        const float most = __uint_as_float(bits), apart = 0x1p-20f * (HALF ? fmaxf(__uint_as_float(bits_of[0]), __uint_as_float(bits_of[1])) : most);   // (half-split pairs lie in both of the lanes' groups)
+        uint32_t byte = scale_byte(bits);
+        if (byte != kScaleNaN) {
+            byte = scale_byte(min(__float_as_uint(most + apart), 0x7f7fffffu));
+            if (scale_byte(__float_as_uint(fmaxf(most - apart, 0.f))) != byte) {   // (all four lanes)
+                double exact = 0.0;
+#pragma unroll 1
+                for (int e = 0; e < 8; ++e) exact = fmax(exact, fabs(rotated<T, HALF>(row, 64 * p + 8 * part + e, pos, turns)));
+                byte = scale_byte(most_of_4(exact));
             }
         }
         const float scale = __uint_as_float(byte << 23);
-        uint32_t word;
-        if (TURN) {
-            float below[8], above[8];
+        float below[8], above[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) below[e] = x[p][e] - off[p][e], above[e] = x[p][e] + off[p][e];
-            word = codes8(below, scale);
-            uint32_t open = byte == kScaleNaN ? 0 : word ^ codes8(above, scale);
-            while (open) {
-                const int at = (__ffs(open) - 1) & ~3;
-                const uint32_t code = code_of(rotated<T, HALF>(row, 64 * p + 8 * part + at / 4, pos, turns), byte);
-                word = (word & ~(15u << at)) | code << at;
-                open &= ~(15u << at);
-            }
-        } else {
-            word = codes8(x[p], scale);
+        for (int e = 0; e < 8; ++e) below[e] = x[p][e] - apart, above[e] = x[p][e] + apart;
+        uint32_t word = codes8(below, scale), open = byte == kScaleNaN ? 0 : word ^ codes8(above, scale);
+#pragma unroll 1
+        while (open) {
+            const int at = (__ffs(open) - 1) & ~3;
+            const uint32_t code = code_of(rotated<T, HALF>(row, 64 * p + 8 * part + at / 4, pos, turns), byte);
+            word = (word & ~(15u << at)) | code << at;
+            open &= ~(15u << at);
         }
         got.word[p] = byte == kScaleNaN ? 0 : word;
         got.byte[p] = byte;
@@ -153,9 +226,9 @@ __device__ __forceinline__ void put_row(void *rows, uint32_t *scales, const Code
     if (part == 0) scales[at_word] = word;
 }
 
-// A workgroup takes 32 neighbouring tokens of a KV head, eight threads to a row of K and of V, each with two pieces of eight elements half a row apart: both parts of its bands lie in them in either pair layout, and
-// four lanes hold the 32 elements of a scale.  Neighbouring rows are neighbouring slots: 64 bytes each, a wave writes 512 side by side.
-template <typename T, bool TURN, bool HALF>
+// A workgroup takes 32 neighbouring tokens of HEADS KV heads, eight threads to a row of K and of V, each with two pieces of eight elements half a row apart: both parts of its bands lie in them in either pair layout, and
+// four lanes hold the 32 elements of a scale.  Neighbouring rows are neighbouring slots: 64 bytes each, a wave writes 512 side by side.  The heads of a token have its angles in common.
+template <typename T, bool TURN, bool HALF, int HEADS>
 __global__ __launch_bounds__(kPackThreads) void append4_kernel(Append4Args args)
 {
     const AppendArgs &a = args.a;
@@ -169,19 +242,23 @@ __global__ __launch_bounds__(kPackThreads) void append4_kernel(Append4Args args)
         if (a.start) got = max(clamp_to(a.start[s + 1], a.n_tokens) - clamp_to(a.start[s], a.n_tokens), 0);
         a.new_seq_len[s] = (int)min((int64_t)n + got, (int64_t)c.max_seq_len);
     }
-    const int h = blockIdx.x % H, part = threadIdx.x % kLanes;
-    const int64_t t0 = (int64_t)(blockIdx.x / H) * kPackRows;
+    const uint32_t groups = (uint32_t)(H + HEADS - 1) / HEADS;
+    const int h0 = (int)(blockIdx.x % groups) * HEADS, part = threadIdx.x % kLanes;
+    const int64_t t0 = (int64_t)(blockIdx.x / groups) * kPackRows;
     const int64_t t_wave = t0 + (threadIdx.x & ~63) / kLanes;
     if (t_wave >= a.n_tokens) return;   // (the whole wave)
     const int64_t t_mine = t0 + threadIdx.x / kLanes;
     const int t = (int)min(t_mine, (int64_t)a.n_tokens - 1);
     // the rows are asked for before their place is known
-    const int64_t from = ((int64_t)t * a.stride_token + (int64_t)h * a.stride_head) * (int64_t)sizeof(T);
-    float k[2][8], v[2][8];
+    const T *k_row = reinterpret_cast<const T *>(a.k_new) + (int64_t)t * a.stride_token + (int64_t)h0 * a.stride_head;
+    const T *v_row = reinterpret_cast<const T *>(a.v_new) + (int64_t)t * a.stride_token + (int64_t)h0 * a.stride_head;
+    Eight<T> k[2], v[2];
 #pragma unroll
-    for (int p = 0; p < 2; ++p) load8<T>(a.k_new + from + (64 * p + 8 * part) * sizeof(T), k[p]), load8<T>(a.v_new + from + (64 * p + 8 * part) * sizeof(T), v[p]);
+    for (int p = 0; p < 2; ++p) k[p].load(k_row + 64 * p + 8 * part), v[p].load(v_row + 64 * p + 8 * part);
     const int32_t pos = a.pos[t];
-    bool there = t_mine < a.n_tokens;
+    Angles angles;
+    if (TURN) angles = angles_of<HALF>(pos, a.turns, part);
+    bool mine = t_mine < a.n_tokens;
     int s = t, first = t;
     if (a.start) {
         s = 0;
@@ -190,43 +267,62 @@ __global__ __launch_bounds__(kPackThreads) void append4_kernel(Append4Args args)
             s += __popcll(__ballot(e < S && a.start[min(e, S - 1) + 1] <= (int)t_wave));
         }
         while (s < S && a.start[s + 1] <= t) ++s;
-        there &= s < S;
+        mine &= s < S;
         s = min(s, S - 1);
         first = a.start[s];
-        there &= t >= first;
+        mine &= t >= first;
     }
-    const int len = clamp_len(a.head_len ? a.head_len[((int64_t)a.layer * S + s) * H + h] : c.seq_len[s], c.max_seq_len);
-    const int64_t slot = (int64_t)len + (t - first);
-    there &= slot < c.max_seq_len;
-    int n = there ? (int)slot : 0;
-    int64_t block = s;
-    if (c.block_shift >= 0) {
-        block = there ? block_of(c, a.n_blocks, s, n) : -1;
-        there &= block >= 0;
-        n &= (1 << c.block_shift) - 1;
+    bool there = false;
+    int n = 0;
+    int64_t block = 0;
+    const auto find = [&](int length) {   // the token's slot behind a length
+        const int64_t slot = (int64_t)clamp_len(length, c.max_seq_len) + (t - first);
+        there = mine & (slot < c.max_seq_len);
+        n = there ? (int)slot : 0;
+        block = s;
+        if (c.block_shift >= 0) {
+            block = there ? block_of(c, a.n_blocks, s, n) : -1;
+            there &= block >= 0;
+            n &= (1 << c.block_shift) - 1;
+        }
+    };
+#pragma unroll
+    for (int j = 0; j < HEADS; ++j) {
+        const int h = h0 + j;
+        if (h >= H) break;
+        if (j == 0 || a.head_len) find(a.head_len ? a.head_len[((int64_t)a.layer * S + s) * H + h] : c.seq_len[s]);
+        const int64_t to = ((int64_t)a.layer * c.stride_layer + (int64_t)h * c.stride_head + block * c.stride_sb + slot_offset(c, n)) / 2;
+        const int64_t word = word_of(c, (int64_t)a.layer * c.pos_stride_layer + (int64_t)h * c.pos_stride_head, block, n);
+        Eight<T> k_here[2] = {k[0], k[1]}, v_here[2] = {v[0], v[1]};
+        const T *row = k_row;
+        if (j + 1 < HEADS && h + 1 < H) {   // the next head's
+            k_row += a.stride_head, v_row += a.stride_head;
+#pragma unroll
+            for (int p = 0; p < 2; ++p) k[p].load(k_row + 64 * p + 8 * part), v[p].load(v_row + 64 * p + 8 * part);
+        }
+        Codes kc;
+        if constexpr (TURN) kc = to_codes<T, HALF>(k_here, angles, row, pos, a.turns, part);
+        else kc = to_codes<T>(k_here);
+        const Codes vc = to_codes<T>(v_here);
+        put_row(const_cast<void *>(c.k), args.k_scale, kc, part, there, to, word);
+        put_row(const_cast<void *>(c.v), args.v_scale, vc, part, there, to, word);
+        if (there && part == 0) const_cast<int32_t *>(c.pos)[word] = pos;
     }
-    const int64_t to = ((int64_t)a.layer * c.stride_layer + (int64_t)h * c.stride_head + block * c.stride_sb + slot_offset(c, n)) / 2;
-    const int64_t word = word_of(c, (int64_t)a.layer * c.pos_stride_layer + (int64_t)h * c.pos_stride_head, block, n);
-    const Codes kc = to_codes<T, TURN, HALF>(k, reinterpret_cast<const T *>(a.k_new + from), pos, a.turns, part);
-    const Codes vc = to_codes<T, false, false>(v, nullptr, 0, a.turns, part);
-    put_row(const_cast<void *>(c.k), args.k_scale, kc, part, there, to, word);
-    put_row(const_cast<void *>(c.v), args.v_scale, vc, part, there, to, word);
-    if (there && part == 0) const_cast<int32_t *>(c.pos)[word] = pos;
 }
 
 // Which slots a workgroup of tri_pack4 / tri_unpack4 moves, and where from.
 struct Instance {
     int l, s, h, count;
-    int64_t inst;
+    uint32_t inst;
 };
-__device__ __forceinline__ Instance instance_of(const Pack4Args &a, int64_t inst)
+__device__ __forceinline__ Instance instance_of(const Pack4Args &a, uint32_t inst)
 {
     Instance x;
     x.inst = inst;
-    x.h = (int)(inst % a.src.n_kv_heads);
-    const int64_t ls = inst / a.src.n_kv_heads;
-    x.s = (int)(ls % a.src.n_seqs);
-    x.l = (int)(ls / a.src.n_seqs);
+    const uint32_t H = a.src.n_kv_heads, S = a.src.n_seqs, ls = inst / H;
+    x.h = (int)(inst - ls * H);
+    x.l = (int)(ls / S);
+    x.s = (int)(ls - x.l * S);
     x.count = clamp_to(a.kept_cnt ? a.kept_cnt[inst] : a.src.seq_len[x.s], a.slots);
     return x;
 }
@@ -247,15 +343,15 @@ __device__ __forceinline__ Place place_of(const CacheView &c, int n_blocks, cons
 }
 __device__ __forceinline__ int slot_to_read(const Pack4Args &a, const Instance &x, int j)
 {
-    return a.kept_idx ? min(max(a.kept_idx[x.inst * a.budget + j], 0), a.src.max_seq_len - 1) : j;
+    return a.kept_idx ? min(max(a.kept_idx[(int64_t)x.inst * a.budget + j], 0), a.src.max_seq_len - 1) : j;
 }
 
 // As append4_kernel, from slots to slots.
 template <typename T, bool TURN, bool HALF>
-__global__ __launch_bounds__(kPackThreads) void pack4_kernel(Pack4Args a)
+__global__ __launch_bounds__(kPackThreads, sizeof(T) == 2 && !HALF ? 6 : 1) void pack4_kernel(Pack4Args a)
 {
-    const int64_t inst = blockIdx.x / (uint32_t)a.row_blocks;
-    const int rb = (int)(blockIdx.x - inst * a.row_blocks), part = threadIdx.x % kLanes;
+    const uint32_t inst = blockIdx.x / (uint32_t)a.row_blocks;
+    const int rb = (int)(blockIdx.x - inst * (uint32_t)a.row_blocks), part = threadIdx.x % kLanes;
     const Instance x = instance_of(a, inst);
     if (a.new_seq_len && x.l == 0 && x.h == 0 && rb == 0 && threadIdx.x == 0) a.new_seq_len[x.s] = x.count;
     const int j = rb * kPackRows + (int)threadIdx.x / kLanes;
@@ -264,54 +360,91 @@ __global__ __launch_bounds__(kPackThreads) void pack4_kernel(Pack4Args a)
     const Place from = place_of(a.src, a.src_blocks, x, slot_to_read(a, x, last)), to = place_of(a.dst, a.dst_blocks, x, last);
     const bool there = j < x.count && from.there && to.there;
     const int64_t at = from.there ? from.row : 0, at_word = from.there ? from.word : 0;
-    const T *row = reinterpret_cast<const T *>(a.src.k) + at;
-    float k[2][8], v[2][8];
+    const T *row = reinterpret_cast<const T *>(a.src.k) + at, *v_row = reinterpret_cast<const T *>(a.src.v) + at;
+    Eight<T> k[2], v[2];
 #pragma unroll
-    for (int p = 0; p < 2; ++p) load8<T>((const char *)(row + 64 * p + 8 * part), k[p]), load8<T>((const char *)(reinterpret_cast<const T *>(a.src.v) + at + 64 * p + 8 * part), v[p]);
+    for (int p = 0; p < 2; ++p) k[p].load(row + 64 * p + 8 * part), v[p].load(v_row + 64 * p + 8 * part);
     const int32_t pos = a.src.pos[at_word];
-    const Codes kc = to_codes<T, TURN, HALF>(k, row, pos, a.turns, part);
-    const Codes vc = to_codes<T, false, false>(v, nullptr, 0, a.turns, part);
+    Codes kc;
+    if constexpr (TURN) kc = to_codes<T, HALF>(k, angles_of<HALF>(pos, a.turns, part), row, pos, a.turns, part);
+    else kc = to_codes<T>(k);
+    const Codes vc = to_codes<T>(v);
     put_row(const_cast<void *>(a.dst.k), a.k_scale, kc, part, there, to.row / 2, to.word);
     put_row(const_cast<void *>(a.dst.v), a.v_scale, vc, part, there, to.row / 2, to.word);
     if (there && part == 0) const_cast<int32_t *>(a.dst.pos)[to.word] = pos;
 }
 
+// A thread's eight numbers of a row: neighbours in bf16, two times four half a row apart in fp32, so that sixteen threads' stores of 16 bytes lie side by side in either (with 32 bytes of its own each, sixteen ragged sequences in two layers took 504 us to read back in fp32, 256 so).
 template <typename T>
-__device__ __forceinline__ void store_read8(T *p, uint32_t word, float scale);
+struct Numbers;
 template <>
-__device__ __forceinline__ void store_read8<__bf16>(__bf16 *p, uint32_t word, float scale) { store_stream16((char *)p, read8(word, scale)); }
+struct Numbers<__bf16> {
+    static __device__ __forceinline__ uint32_t load(const char *row, int part) { return reinterpret_cast<const uint32_t *>(row)[part]; }
+    static __device__ __forceinline__ void store(__bf16 *row, int part, uint32_t word, uint32_t scales) { store_stream16((char *)(row + 8 * part), read8(word, scale_at(scales, part / 4))); }
+};
 template <>
-__device__ __forceinline__ void store_read8<float>(float *p, uint32_t word, float scale)
-{
-    const uint4 b = read8(word, scale);
-    store_stream16((char *)p, make_uint4(b.x << 16, b.x & 0xffff0000u, b.y << 16, b.y & 0xffff0000u));
-    store_stream16((char *)(p + 4), make_uint4(b.z << 16, b.z & 0xffff0000u, b.w << 16, b.w & 0xffff0000u));
-}
+struct Numbers<float> {
+    static __device__ __forceinline__ uint32_t load(const char *row, int part)
+    {
+        const uint16_t *p = reinterpret_cast<const uint16_t *>(row);
+        return (uint32_t)p[part] | (uint32_t)p[16 + part] << 16;
+    }
+    static __device__ __forceinline__ void store(float *row, int part, uint32_t word, uint32_t scales)
+    {
+        const uint4 a = read8(word, scale_at(scales, part / 8)), b = read8(word, scale_at(scales, 2 + part / 8));
+        store_stream16((char *)(row + 4 * part), make_uint4(a.x << 16, a.x & 0xffff0000u, a.y << 16, a.y & 0xffff0000u));
+        store_stream16((char *)(row + 64 + 4 * part), make_uint4(b.z << 16, b.z & 0xffff0000u, b.w << 16, b.w & 0xffff0000u));
+    }
+};
 
 // Sixteen threads to a row, eight numbers each; every bf16 number is exact.
 template <typename T>
 __global__ __launch_bounds__(kPackThreads) void unpack4_kernel(Pack4Args a)
 {
-    const int64_t inst = blockIdx.x / (uint32_t)a.row_blocks;
-    const int rb = (int)(blockIdx.x - inst * a.row_blocks), part = threadIdx.x % 16;
+    const uint32_t inst = blockIdx.x / (uint32_t)a.row_blocks;
+    const int rb = (int)(blockIdx.x - inst * (uint32_t)a.row_blocks), part = threadIdx.x % 16;
     const Instance x = instance_of(a, inst);
     if (a.new_seq_len && x.l == 0 && x.h == 0 && rb == 0 && threadIdx.x == 0) a.new_seq_len[x.s] = x.count;
+    // all rows are asked for before the first is written
+    Place from[kReadPasses], to[kReadPasses];
+    uint32_t k[kReadPasses], v[kReadPasses], k_scale[kReadPasses], v_scale[kReadPasses];
+    int32_t pos[kReadPasses];
+    bool there[kReadPasses];
+    if (rb * kReadRows >= x.count) return;
 #pragma unroll
     for (int i = 0; i < kReadPasses; ++i) {
-        const int j = rb * kReadRows + i * (kPackThreads / 16) + (int)threadIdx.x / 16;
-        if (j >= x.count) continue;
-        const Place from = place_of(a.src, a.src_blocks, x, slot_to_read(a, x, j)), to = place_of(a.dst, a.dst_blocks, x, j);
-        if (!from.there || !to.there) continue;
-        const uint32_t kw = reinterpret_cast<const uint32_t *>((const char *)a.src.k + from.row / 2)[part], vw = reinterpret_cast<const uint32_t *>((const char *)a.src.v + from.row / 2)[part];
-        store_read8<T>((T *)a.dst.k + to.row + 8 * part, kw, scale_at(a.k_scale[from.word], part / 4));
-        store_read8<T>((T *)a.dst.v + to.row + 8 * part, vw, scale_at(a.v_scale[from.word], part / 4));
-        if (part == 0) const_cast<int32_t *>(a.dst.pos)[to.word] = a.src.pos[from.word];
+        const int j = rb * kReadRows + i * (kPackThreads / 16) + (int)threadIdx.x / 16, at = min(j, x.count - 1);
+        from[i] = place_of(a.src, a.src_blocks, x, slot_to_read(a, x, at));
+        to[i] = place_of(a.dst, a.dst_blocks, x, at);
+        there[i] = (j < x.count) & from[i].there & to[i].there;
+    }
+#pragma unroll
+    for (int i = 0; i < kReadPasses; ++i) {
+        const int64_t row = from[i].there ? from[i].row / 2 : 0, word = from[i].there ? from[i].word : 0;
+        k[i] = Numbers<T>::load((const char *)a.src.k + row, part);
+        v[i] = Numbers<T>::load((const char *)a.src.v + row, part);
+        k_scale[i] = a.k_scale[word];
+        v_scale[i] = a.v_scale[word];
+        pos[i] = a.src.pos[word];
+    }
+#pragma unroll
+    for (int i = 0; i < kReadPasses; ++i) {
+        if (!there[i]) continue;
+        Numbers<T>::store((T *)a.dst.k + to[i].row, part, k[i], k_scale[i]);
+        Numbers<T>::store((T *)a.dst.v + to[i].row, part, v[i], v_scale[i]);
+        if (part == 0) const_cast<int32_t *>(a.dst.pos)[to[i].word] = pos[i];
     }
 }
 
 }  // namespace
 
-int64_t append4_groups(int64_t n_tokens, int64_t n_kv_heads) { return (n_tokens + kPackRows - 1) / kPackRows * n_kv_heads; }
+// Heads of a workgroup.
+static int append4_heads(int64_t n_tokens, int64_t n_kv_heads) { return n_tokens * n_kv_heads >= 32768 ? 4 : 1; }
+int64_t append4_groups(int64_t n_tokens, int64_t n_kv_heads)
+{
+    const int64_t heads = append4_heads(n_tokens, n_kv_heads);
+    return (n_tokens + kPackRows - 1) / kPackRows * ((n_kv_heads + heads - 1) / heads);
+}
 int32_t pack4_row_blocks(int32_t slots) { return std::max(1, (int32_t)(((int64_t)slots + kPackRows - 1) / kPackRows)); }
 int32_t unpack4_row_blocks(int32_t slots) { return std::max(1, (int32_t)(((int64_t)slots + kReadRows - 1) / kReadRows)); }
 
@@ -322,8 +455,11 @@ tri_status launch_append4(const Append4Args &a, int32_t rows, hipStream_t st)
     if (blocks == 0) return TRI_OK;
     const auto launch = [&](auto kernel) { kernel<<<blocks, kPackThreads, 0, st>>>(a); };
     const auto of = [&](auto plain, auto half, auto interleaved) { !a.a.rotate ? launch(plain) : a.a.half ? launch(half) : launch(interleaved); };
-    if (rows == TRI_BF16) of(append4_kernel<__bf16, false, false>, append4_kernel<__bf16, true, true>, append4_kernel<__bf16, true, false>);
-    else of(append4_kernel<float, false, false>, append4_kernel<float, true, true>, append4_kernel<float, true, false>);
+    const bool one = append4_heads(a.a.n_tokens, a.a.cache.n_kv_heads) == 1;
+    if (rows == TRI_BF16 && one) of(append4_kernel<__bf16, false, false, 1>, append4_kernel<__bf16, true, true, 1>, append4_kernel<__bf16, true, false, 1>);
+    else if (rows == TRI_BF16) of(append4_kernel<__bf16, false, false, 4>, append4_kernel<__bf16, true, true, 4>, append4_kernel<__bf16, true, false, 4>);
+    else if (one) of(append4_kernel<float, false, false, 1>, append4_kernel<float, true, true, 1>, append4_kernel<float, true, false, 1>);
+    else of(append4_kernel<float, false, false, 4>, append4_kernel<float, true, true, 4>, append4_kernel<float, true, false, 4>);
     return hip_status("append4_kernel");
 }
 
