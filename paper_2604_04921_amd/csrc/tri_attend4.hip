@@ -54,6 +54,32 @@ __device__ __forceinline__ float add_across_8(float x) { return x + __int_as_flo
 // x + that of lane ^ 4
 __device__ __forceinline__ float add_across_4(float x) { return x + __shfl_xor(x, 4); }
 
+// finish_row for N neighbouring dimensions.
+template <typename T, int N>
+__device__ __forceinline__ void finish(const AttendArgs &a, int split, int t, int hq, int Hq, int d0, float best, float total, float (&x)[N])
+{
+    if constexpr (N == 8) {
+        finish_row<T>(a, a.src, split, t, hq, Hq, d0, best, total, x);
+    } else {
+        typedef float Sums __attribute__((ext_vector_type(N)));
+        typedef T Out __attribute__((ext_vector_type(N)));
+        if (a.part_o) {
+            const int64_t at = ((int64_t)(a.src.part0 + split) * a.n_tokens + t) * Hq + hq;
+            if (d0 == 0) a.part_ml[at] = make_float2(best, total);
+            Sums y;
+#pragma unroll
+            for (int e = 0; e < N; ++e) y[e] = x[e];
+            *reinterpret_cast<Sums *>(a.part_o + at * kHeadDim + d0) = y;
+            return;
+        }
+        const float inv = 1.f / total;
+        Out y;
+#pragma unroll
+        for (int e = 0; e < N; ++e) y[e] = (T)(total != 0.f ? x[e] * inv : 0.f);   // (no key: zeros; scores that are no number: NaN)
+        *reinterpret_cast<Out *>(reinterpret_cast<T *>(a.out) + (int64_t)t * a.out_stride_token + (int64_t)hq * a.out_stride_head + d0) = y;
+    }
+}
+
 // NT column tiles of sixteen rows against 64 keys at a time.  S^T[key][row] = K Q^T runs on v_mfma_scale_f32_16x16x128_f8f6f4, which takes the keys as they lie in memory -- a lane (m = lane & 15, kq = lane >> 4) has the
 // 32 dimensions from 32 kq on of its key, and their scale -- and queries as e4m3 numbers: QPARTS of them to an element, each of what rounding left of the one before, four bits each (a part's scale is 2^-4 of the last
 // one's, the first's brings the row's largest to [128, 256)).  O^T[dim][row] = V^T P^T runs on v_mfma_f32_16x16x32_bf16: values become bf16 numbers in registers, exactly (a conversion for two of them, scale and all),
@@ -75,14 +101,20 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
     __shared__ int32_t q_unit[kRows], q_pos[kRows];
     __shared__ float wave_m[kWaves][kRows], wave_l[kWaves][kRows];
     __shared__ __align__(16) float wave_o[kWaves][kRows][kHeadDim + 4];
-    Part(*q_parts)[kRows][kHeadDim] = reinterpret_cast<Part(*)[kRows][kHeadDim]>(wave_o);   // (which is written behind the loop, the parts being read before it)
+    Part(*q_parts)[kRows][kHeadDim] = reinterpret_cast<Part(*)[kRows][kHeadDim]>(wave_o);   // (which is written behind the loop, the parts being read before it and a barrier between)
     static_assert(sizeof(Part[QPARTS][kRows][kHeadDim]) <= sizeof(wave_o), "");
     const AttendSource &src = a.src;
     const CacheView &c = src.cache;
     const int H = c.n_kv_heads, G = a.group_size, Hq = H * G;
+    // All that a workgroup needs of the arguments is asked for at once.  Asked for where it is needed, one wait came after the other: one sequence of 64 keys 6.8 us, 6.3 so, and 0.4 of any call.
+    asm volatile("" ::"s"(c.k), "s"(c.v), "s"(c.pos), "s"(c.stride_sb), "s"(c.stride_layer), "s"(c.stride_head), "s"(c.stride_slot), "s"(c.pos_stride_sb), "s"(c.pos_stride_layer), "s"(c.pos_stride_head), "s"(c.n_seqs),
+                 "s"(c.block_table), "s"(src.head_len), "s"(src.max_tokens), "s"(src.n_split), "s"(src.least_keys), "s"(a.k_scale), "s"(a.v_scale), "s"(a.q), "s"(a.q_stride_token), "s"(a.q_stride_head), "s"(a.pos));
+    asm volatile("" ::"s"(a.layer), "s"(a.causal), "s"(a.rotate_q), "s"(a.half), "s"(a.group_size), "s"(a.part_o), "s"(a.start), "s"(a.row_tiles));
     // Row tiles of the same keys run next to each other on one XCD; a head's parts next to each other, which part comes first going round the heads (see attend_rows_kernel).
     const uint32_t x8 = blockIdx.x & 7, y8 = blockIdx.x >> 3;
-    const uint32_t row_tile = y8 % (uint32_t)a.row_tiles, w = y8 / (uint32_t)a.row_tiles * 8 + x8;
+    uint32_t in_eight = y8, row_tile = 0;
+    if (a.row_tiles > 1) in_eight = y8 / (uint32_t)a.row_tiles, row_tile = y8 - in_eight * (uint32_t)a.row_tiles;
+    const uint32_t w = in_eight * 8 + x8;
     const uint32_t n = src.n_split, head = w / n, even = min(n & -n, 32u);
     if (head >= (uint32_t)(H * c.n_seqs)) return;
     const uint32_t turned = w - head * n + ((head * even / 32) & (even - 1));
@@ -280,6 +312,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
         }
     }
     first_pos = __builtin_amdgcn_readfirstlane(over_16(first_pos, [](int x, int y) { return min(x, y); }));
+    __syncthreads();
 
     // (QUAD) bytes 1, 0 below zeros or above them; of the upper half
     const uint32_t pick = m < 8 ? 0x0c0c0100u : 0x01000c0cu, pick_next = m < 8 ? 0x0202u : 0x02020000u;
@@ -467,57 +500,56 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
         block = block_next;
         there = there_next;
     }
-    // join the waves: O's lane has dimensions 32 kq + 8 d + e of its row
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        sum[t] += __shfl_xor(sum[t], 16);
-        sum[t] += __shfl_xor(sum[t], 32);
-        if (kq == 0 && m < COLS) wave_m[wave][t * COLS + m] = top[t], wave_l[wave][t * COLS + m] = sum[t];
-    }
-    __syncthreads();
+    // Join the waves: O's lane has dimensions 32 kq + 8 d + e of its row (QUAD: 32 kq + 8 d + 2 e, and those after them in the lanes of m >= 8).  Where lanes hold the same sums, each writes half of them.
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         const int at = t * COLS + (m & (COLS - 1));
-        float all = kNoScore;
+        sum[t] += __shfl_xor(sum[t], 16);
+        sum[t] += __shfl_xor(sum[t], 32);
+        if (kq == 0 && m < COLS) wave_m[wave][at] = top[t], wave_l[wave][at] = sum[t];
+        const bool other = LO && (m & (QUAD ? 4 : 8));
 #pragma unroll
-        for (int j = 0; j < kWaves; ++j) all = fmaxf(all, wave_m[j][at]);
-        const float mine = __builtin_amdgcn_exp2f((top[t] - (all == kNoScore ? 0.f : all)) * a.scale_log2);
-        const bool none = (not_numbers[t] >> (8 * kq + 7)) & 1;
+        for (int i = 0; i < (LO ? 2 : 4); ++i) {
+            const int d = LO ? 2 * other + i : i;
 #pragma unroll
-        for (int e = 0; e < kSums; ++e)
+            for (int e = 0; e < kSums; e += 4) {
+                f32x4 y;
 #pragma unroll
-            for (int d = 0; d < 4; ++d) o[t][e][d] = none ? __builtin_nanf("") : (QUAD ? add_across_4(o[t][e][d]) : LO ? add_across_8(o[t][e][d]) : o[t][e][d]) * mine;
-#pragma unroll
-        for (int d = 0; d < 4; ++d) {
-            if (QUAD) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (!(m & 4)) wave_o[wave][at][32 * kq + 8 * d + 2 * e + (m >> 3)] = o[t][e % kSums][d];
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; e += 4)
-                    if (m < COLS)
-                        *reinterpret_cast<f32x4 *>(&wave_o[wave][at][32 * kq + 8 * d + e]) = f32x4{o[t][e % kSums][d], o[t][(e + 1) % kSums][d], o[t][(e + 2) % kSums][d], o[t][(e + 3) % kSums][d]};
+                for (int n = 0; n < 4; ++n) {
+                    const float first = o[t][e + n][i], later = o[t][e + n][LO ? 2 + i : i];
+                    const float here = QUAD ? add_across_4(first) : LO ? add_across_8(first) : first, there = QUAD ? add_across_4(later) : LO ? add_across_8(later) : later;
+                    y[n] = other ? there : here;
+                }
+                if (__ballot(not_numbers[t] != 0) && (not_numbers[t] >> (8 * kq + 7)) & 1) y = __builtin_nanf("");
+                *reinterpret_cast<f32x4 *>(&wave_o[wave][at][32 * kq + 8 * d + (QUAD ? 4 * (m >> 3) : e)]) = y;
             }
         }
     }
     __syncthreads();
+    constexpr int kOut = std::min(8, kRows * kHeadDim / kThreads), kLanesOut = kHeadDim / kOut;   // dimensions of a thread, threads of a row
 #pragma unroll
-    for (int i = 0; i < (kRows + 15) / 16; ++i) {
-        const int row = 16 * i + (tid >> 4), d0 = 8 * (tid & 15);
+    for (int i = 0; i < kRows * kLanesOut / kThreads; ++i) {
+        const int row = (i * kThreads + tid) / kLanesOut, d0 = kOut * (tid % kLanesOut);
         if (row >= rows) break;
-        float best = kNoScore, total = 0.f, x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        float best = kNoScore, total = 0.f, x[kOut] = {};
 #pragma unroll
         for (int j = 0; j < kWaves; ++j) best = fmaxf(best, wave_m[j][row]);
         const float ref = best == kNoScore ? 0.f : best;
 #pragma unroll
         for (int j = 0; j < kWaves; ++j) {
-            total += wave_l[j][row] * __builtin_amdgcn_exp2f((wave_m[j][row] - ref) * a.scale_log2);
+            const float by = __builtin_amdgcn_exp2f((wave_m[j][row] - ref) * a.scale_log2);
+            total = fmaf(wave_l[j][row], by, total);
+            const float *y = wave_o[j][row];
+            if (QUAD) {
+                const int lie = (d0 & ~7) + (d0 & 7) / 2;
+                x[0] = fmaf(y[lie], by, x[0]), x[1] = fmaf(y[lie + 4], by, x[1]);
+            } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] += wave_o[j][row][d0 + e];
+                for (int e = 0; e < kOut; ++e) x[e] = fmaf(y[d0 + e], by, x[e]);
+            }
         }
         const int r = r0 + row;
-        finish_row<T>(a, src, split, tr.t0 + r / G, h * G + r % G, Hq, d0, best, total, x);
+        finish<T, kOut>(a, split, tr.t0 + r / G, h * G + r % G, Hq, d0, best, total, x);
     }
 }
 
@@ -537,7 +569,7 @@ AttendSplit attend4_split(const tri_model &m, const tri_cache &c, int32_t max_to
 {
     const int64_t G = m.n_q_heads / m.n_kv_heads, rows = max_tokens * G, per = tile_rows(type, rows);
     const bool tile = is_tile(type, rows);
-        const int64_t part = tile ? 8192 : 3500;
+    const int64_t part = tile ? 8192 : 3500;
     const int64_t tiles = std::max<int64_t>(c.n_seqs, (n_tokens * G + per - 1) / per + c.n_seqs / 2);
     const int64_t units = m.n_kv_heads * tiles;
     const int64_t least = tile ? 256 : std::min<int64_t>(part, std::max<int64_t>(256, part * units / 256));
