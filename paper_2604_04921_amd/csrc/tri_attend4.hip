@@ -230,11 +230,25 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
     const uint64_t turn = a.rotate_q ? a.turns.w[lane] : 0;
     float re[kTurns], im[kTurns];
     int32_t pos[kTurns];
+    // (the last rows' places are whole rows, too: they hold the last row again, and nobody reads them)
+    const int t_first = r0 / G, r_first = r0 - t_first * G;
+    const float of_group = __builtin_amdgcn_rcpf((float)G);
+    const T *q_row[kTurns];
 #pragma unroll
     for (int i = 0; i < kTurns; ++i) {
-        const int r = r0 + min(wave + kWaves * i, rows - 1), token = tr.t0 + r / G, hq = h * G + r % G;
-        load_band(reinterpret_cast<const T *>(a.q) + (int64_t)token * a.q_stride_token + (int64_t)hq * a.q_stride_head, lane, a.half, &re[i], &im[i]);
+        const int r = r_first + min(wave + kWaves * i, rows - 1);   // (below G + 32)
+        int t = (int)((r + 0.5f) * of_group);                       // r / G, or, in groups of tens of thousands, one off
+        t += (r >= (t + 1) * G) - (r < t * G);
+        const int token = tr.t0 + t_first + t, hq = h * G + r - t * G;
+        q_row[i] = reinterpret_cast<const T *>(a.q) + (int64_t)token * a.q_stride_token + (int64_t)hq * a.q_stride_head;
         pos[i] = a.causal || a.rotate_q ? a.pos[token] : 0;
+    }
+    if (a.half) {
+#pragma unroll
+        for (int i = 0; i < kTurns; ++i) load_band(q_row[i], lane, true, &re[i], &im[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kTurns; ++i) load_band(q_row[i], lane, false, &re[i], &im[i]);
     }
     int block = block_at(k0);
     uint64_t there = there_of(k0, block);
@@ -242,45 +256,38 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
     load_k(k0, block, there);
     load_v(k0, block, there);
     int ahead = block_at(k0 + kStep);
-    {
+    const int first = a.half ? lane : 2 * lane, second_at = a.half ? lane + 64 : 2 * lane + 1;   // the dimensions of the band
 #pragma unroll
-        for (int i = 0; i < kTurns; ++i) {
-            const int row = wave + kWaves * i;
-            if (row >= rows) break;
-            float x = re[i], y = im[i];
-            if (a.rotate_q) {
-                float c, s;
-                const uint32_t phase = phase_of(pos[i], (uint32_t)turn, (uint32_t)(turn >> 32));
-                if (DIRECT) turn_fast(phase, &c, &s);
-                else turn_exact(phase, &c, &s);
-                x = fmaf(re[i], c, -(im[i] * s));
-                y = fmaf(re[i], s, im[i] * c);
+    for (int i = 0; i < kTurns; ++i) {
+        const int row = wave + kWaves * i;
+        float c, s;
+        const uint32_t phase = phase_of(pos[i], (uint32_t)turn, (uint32_t)(turn >> 32));
+        if (DIRECT) turn_fast(phase, &c, &s);
+        else turn_exact(phase, &c, &s);
+        float x = a.rotate_q ? fmaf(re[i], c, -(im[i] * s)) : re[i], y = a.rotate_q ? fmaf(re[i], s, im[i] * c) : im[i];
+        if constexpr (DIRECT) {
+            // the power of two of the row's largest, at least what leaves the last part a scale
+            const int unit = max((int)(__float_as_uint(most_of_wave(fmaxf(fabsf(x), fabsf(y)))) >> 23), 127 - 99);
+            const float by = __uint_as_float((uint32_t)(261 - unit) << 23);
+            x *= by, y *= by;
+#pragma unroll
+            for (int p = 0; p < QPARTS; ++p) {
+                const int w = __builtin_amdgcn_cvt_pk_fp8_f32(x, y, 0, false);
+                q_parts[p][row][first] = (uint8_t)w, q_parts[p][row][second_at] = (uint8_t)(w >> 8);
+                x = (x - __builtin_amdgcn_cvt_f32_fp8(w, 0)) * 16.f;
+                y = (y - __builtin_amdgcn_cvt_f32_fp8(w, 1)) * 16.f;
             }
-            if constexpr (DIRECT) {
-                // the power of two of the row's largest, at least what leaves the last part a scale
-                const int unit = max((int)(__float_as_uint(most_of_wave(fmaxf(fabsf(x), fabsf(y)))) >> 23), 127 - 99);
-                const float by = __uint_as_float((uint32_t)(261 - unit) << 23);
-                x *= by, y *= by;
+            if (lane == 0) q_unit[row] = unit;
+        } else {
 #pragma unroll
-                for (int p = 0; p < QPARTS; ++p) {
-                    const int w = __builtin_amdgcn_cvt_pk_fp8_f32(x, y, 0, false);
-                    if (a.half) q_parts[p][row][lane] = (uint8_t)w, q_parts[p][row][lane + 64] = (uint8_t)(w >> 8);
-                    else *reinterpret_cast<uint16_t *>(&q_parts[p][row][2 * lane]) = (uint16_t)w;
-                    x = (x - __builtin_amdgcn_cvt_f32_fp8(w, 0)) * 16.f;
-                    y = (y - __builtin_amdgcn_cvt_f32_fp8(w, 1)) * 16.f;
-                }
-                if (lane == 0) q_unit[row] = unit;
-            } else {
-#pragma unroll
-                for (int p = 0; p < QPARTS; ++p) {
-                    const __bf16 u = (__bf16)x, w = (__bf16)y;
-                    q_parts[p][row][a.half ? lane : 2 * lane] = u;
-                    q_parts[p][row][a.half ? lane + 64 : 2 * lane + 1] = w;
-                    x -= (float)u, y -= (float)w;
-                }
+            for (int p = 0; p < QPARTS; ++p) {
+                const __bf16 u = (__bf16)x, w = (__bf16)y;
+                q_parts[p][row][first] = u;
+                q_parts[p][row][second_at] = w;
+                x -= (float)u, y -= (float)w;
             }
-            if (lane == 0) q_pos[row] = pos[i];
         }
+        if (lane == 0) q_pos[row] = pos[i];
     }
     __syncthreads();
 
