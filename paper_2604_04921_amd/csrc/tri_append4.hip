@@ -234,6 +234,10 @@ __global__ __launch_bounds__(kPackThreads) void append4_kernel(Append4Args args)
     const AppendArgs &a = args.a;
     const CacheView &c = a.cache;
     const int S = c.n_seqs, H = c.n_kv_heads;
+    // All that is needed of the arguments is asked for at once, not where it is needed, one wait after the other: a token 4.4 -> 4.0 us.  (Not so below: sixteen ragged sequences are read back in 154 us, 172 so.)
+    asm volatile("" ::"s"(a.new_seq_len), "s"(a.head_len), "s"(a.start), "s"(a.k_new), "s"(a.v_new), "s"(a.pos), "s"(a.stride_token), "s"(a.stride_head), "s"(a.n_tokens), "s"(a.layer), "s"(a.n_blocks), "s"(c.seq_len),
+                 "s"(c.max_seq_len), "s"(c.n_seqs), "s"(c.n_kv_heads), "s"(c.block_shift), "s"(c.block_table), "s"(c.max_blocks), "s"(c.stride_layer), "s"(c.stride_head));
+    asm volatile("" ::"s"(c.stride_sb), "s"(c.stride_slot), "s"(c.pos_stride_layer), "s"(c.pos_stride_head), "s"(c.pos_stride_sb), "s"(c.k), "s"(c.v), "s"(c.pos), "s"(args.k_scale), "s"(args.v_scale));
     const int64_t i = (int64_t)blockIdx.x * kPackThreads + threadIdx.x;
     if (a.new_seq_len && i < S) {
         const int s = (int)i;
