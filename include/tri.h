@@ -112,7 +112,7 @@ typedef struct tri_cache {
                                      each already rotated by its own position (Section 2.1 Eq. 1), as serving
                                      stacks usually store them; the scores are the same, the rotation of the key
                                      in the score kernel is skipped and pos is read by tri_compact only */
-    int32_t n_blocks;             /* paged, read by tri_append and tri_attend / tri_attend_shared only: block ids outside [0, n_blocks)
+    int32_t n_blocks;             /* paged, read by tri_append, tri_attend / tri_attend_shared and the calls on caches of 4 bits only: block ids outside [0, n_blocks)
                                      name no block; 0: not given, only negative ids name no block */
 } tri_cache;
 
@@ -359,8 +359,9 @@ tri_status tri_unpack4(const tri_model *model, const tri_cache4 *src, const tri_
 /*
  * tri_attend over a cache of 4 bits, q and out being rows of cache->rows; and for sequences with caches of their own in full precision (dtype prefix->rows; what was appended since) behind prefixes in 4 bits, by the
  * rules of tri_attend_shared.  With group 0, 1, 2, ... every sequence has a prefix to itself.
- * Keys and values enter the products as they are read back.  Queries and weights do as in tri_attend: in bf16, up to 32 rows per KV head, with 16 bits of fraction, and beyond, rotated queries as fp16 numbers and weights as bf16
- * numbers; in fp32 with 24 bits.
+ * Keys and values enter the products as they are read back.  In bf16, with up to 64 rows (query heads of the group x max_tokens; x n_tokens for a prefix) per KV head, queries and weights enter them with 16 bits of
+ * fraction.  Beyond, weights are bf16 numbers, queries that are turned on the way are off by at most 2^-12 of an element or 2^-25 of the row's largest, and others by 2^-21 of the row's largest (which most are exact with).
+ * In fp32 both have 24 bits.
  */
 tri_status tri_attend4(const tri_model *model, const tri_cache4 *cache, int32_t layer, const tri_tokens *tokens,
                        const tri_attention *attention, void *workspace, size_t ws_bytes, void *stream);

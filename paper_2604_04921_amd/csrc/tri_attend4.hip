@@ -560,8 +560,9 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
     }
 }
 
-// Rows that a workgroup takes; more than 32 in bf16 are attend_tile_kernel's.
-bool is_tile(int32_t type, int64_t rows) { return type == TRI_BF16 && rows > 32; }
+// Rows that a workgroup takes.  More than 64 in bf16 are attend_tile_kernel's, which takes 128 of them over its tiles of keys where rows kernels take 32: 32 sequences of 16000 keys with 20, 32, 36 and 64 rows per KV head take
+// 148, 149, 286 and 299 us here, 309, 306, 350 and 351 there; a third pass over the keys would not pay.
+bool is_tile(int32_t type, int64_t rows) { return type == TRI_BF16 && rows > 64; }
 int64_t tile_rows(int32_t type, int64_t rows) { return is_tile(type, rows) ? kTileRows : rows <= 8 ? 8 : type == TRI_F32 || rows <= 16 ? 16 : 32; }
 
 int64_t row_tiles_of(int32_t type, int64_t rows)

@@ -29,6 +29,17 @@ def test_no_more_roundings_than_stated(spec):
     assert wrong(call, K.attend(B, c, scale=call.scale, causal=call.causal, tokens=tokens)) == []
 
 
+@pytest.mark.parametrize("tokens, G", [((9, 1), 4), ((16, 3), 4), ((12,), 5), ((8, 8, 8), 8), ((33,), 1)])
+@pytest.mark.parametrize("block, rotated", [(0, False), (4, True), (16, False), (64, True)])
+def test_up_to_64_rows_are_held_as_few_are(monkeypatch, tokens, G, block, rotated):
+    """33 to 64 rows per KV head, against the tolerance of 16 bits for queries and weights."""
+    from paper_2604_04921_amd import binding as B
+    monkeypatch.setattr(X, "kernel_of", lambda c, rows: "few")
+    c = K.Case(31 + len(tokens) + block, (700, 64, 300)[:len(tokens)], tokens, G=G, block=block, given_rotated=rotated, H=3)
+    call = X.Call(c, scale=0.3)
+    assert wrong(call, K.attend(B, c, scale=call.scale)) == []
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
 @pytest.mark.parametrize("tokens", [(1, 1), (9, 30), (70, 200)])
 @pytest.mark.parametrize("block", [0, 4, 16])
