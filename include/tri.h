@@ -332,7 +332,7 @@ size_t tri_attend_workspace_size(const tri_model *model, const tri_cache *prefix
  * Keys are post-RoPE.  Those that come pre-RoPE are rotated by their position first, and the 4-bit numbers are those of the exactly rotated elements: the kernels work out in double precision what fp32 leaves open.
  */
 typedef struct tri_cache4 {
-    tri_cache c;              /* k, v: the 4-bit numbers; dtype TRI_FP4; strides in elements, multiples of 32, slots less than 2^24 apart; k_rotated 1 */
+    tri_cache c;              /* k, v: the 4-bit numbers; dtype TRI_FP4; strides in elements, multiples of 32, slots less than 2^24 apart; k_rotated 1; to be attended to, max_seq_len at most 2^31 - 4097 */
     uint32_t *k_scale, *v_scale; /* device: a slot's word of scale bytes, where pos has its position (the pos_* strides) */
     int32_t rows;             /* tri_dtype of the rows that come and go: k_new, v_new, q, out */
 } tri_cache4;

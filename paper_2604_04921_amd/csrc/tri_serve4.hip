@@ -91,6 +91,10 @@ tri_status check_bounds4(const tri_model *model, const tri_cache4 *x, const tri_
         set_error("%s: dtype %d of a cache of 4 bits, rows of type %d, the sequences' own of type %d", what, x->c.dtype, x->rows, own ? own->dtype : x->rows);
         return TRI_ERR_INVALID_ARG;
     }
+    if (x->c.max_seq_len > 0x7fffffff - 4096) {   // (kernels look a few tiles of keys ahead)
+        set_error("%s: max_seq_len of a cache of 4 bits must be at most 2^31 - 4097", what);
+        return TRI_ERR_UNSUPPORTED;
+    }
     if ((rc = check_row_type(x, what)) != TRI_OK) return rc;
     if ((rc = check_tokens(own ? own : &x->c, tokens, what)) != TRI_OK) return rc;
     for (const tri_cache *c : {&x->c, own})

@@ -81,9 +81,9 @@ CASES = {
     "unpack": BAD_MODEL + BAD_FOUR + BAD_LENGTHS + BAD_FULL + BAD_MOVE + [(dict(frot=0), UNSUPPORTED), (dict(fblock=16, ftable=ANY, fblocks=6, budget=97), INVALID),
                                                                           (dict(layers=60000, seqs=300, budget=1000), UNSUPPORTED)],
     "attend": BAD_MODEL + BAD_FOUR + BAD_LENGTHS + BAD_TOKENS + BAD_ROWS + [(dict(n=1 << 20, ws=0), WORKSPACE), (dict(n=1 << 20, ws=ANY + 64), WORKSPACE), (dict(n=1 << 20, ws_bytes=100), WORKSPACE),
-                                                                            (dict(seqs=40000, tokens=40000), UNSUPPORTED), (dict(tokens=2 ** 31 - 1, most=1), UNSUPPORTED)],
+                                                                            (dict(seqs=40000, tokens=40000), UNSUPPORTED), (dict(tokens=2 ** 31 - 1, most=1), UNSUPPORTED), (dict(n=2 ** 31 - 4096), UNSUPPORTED)],
     "shared": BAD_MODEL + BAD_FOUR + BAD_LENGTHS + BAD_TOKENS + BAD_ROWS + BAD_FULL + [(dict(group=0), INVALID), (dict(fdtype=0), INVALID), (dict(fseqs=0), INVALID), (dict(fn=-1), INVALID), (dict(ws=0), WORKSPACE),
-                                                                                       (dict(rows=0), INVALID), (dict(fseqs=40000), UNSUPPORTED)],
+                                                                                       (dict(rows=0), INVALID), (dict(fseqs=40000), UNSUPPORTED), (dict(n=2 ** 31 - 1), UNSUPPORTED)],
 }
 
 
