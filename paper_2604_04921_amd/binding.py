@@ -225,6 +225,12 @@ class Cache4:
         for t in (seq_len, cur_pos, block_table):
             if t is not None and (t.dtype != torch.int32 or not t.is_contiguous() or t.device != k.device):
                 raise ValueError("seq_len, cur_pos, block_table: int32, contiguous, where k is")
+        if cur_pos.numel() != seq_len.numel():
+            raise ValueError("cur_pos: as many as seq_len's %d, got %d" % (seq_len.numel(), cur_pos.numel()))
+        if block_table is None and (k.shape[1] < seq_len.numel() or k.shape[3] < max_seq_len):
+            raise ValueError("k, v: %d sequences of %d slots, got %s" % (seq_len.numel(), max_seq_len, tuple(k.shape)))
+        if block_table is not None and (block_table.dim() != 2 or block_table.shape[0] < seq_len.numel()):
+            raise ValueError("block_table: two dimensions, %d sequences, got %s" % (seq_len.numel(), tuple(block_table.shape)))
         rows = torch.bfloat16 if rows is None else rows
         if rows not in (torch.bfloat16, torch.float32):
             raise TypeError("rows: float32 or bfloat16, got %s" % rows)

@@ -314,7 +314,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs 
         for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) widen8(*reinterpret_cast<const uint4 *>(p + 128 * i + 64 * (j / 2) + 16 * (j % 2)), x[i] + 8 * j);
-        if (a.rotate_q) {
+        if constexpr (KEYS != kAsTheyAre) {
             const int32_t turn_pos = a.pos[t];
             const auto turn = [&](int f, float &re, float &im) {
                 const uint64_t w = turns[f];

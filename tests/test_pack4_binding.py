@@ -115,6 +115,16 @@ def test_caches():
         cache4(rows=torch.float16)
 
 
+def test_caches_that_are_smaller_than_said():
+    p = parts()
+    arrays = [p[n] for n in ("k", "v", "ks", "vs", "pos")]
+    assert B.Cache4(*arrays, i32(S - 1), i32(S - 1), N - 1).n_seqs == S - 1
+    for n, cur, most, table in ((S, S - 1, N, None), (S + 1, S + 1, N, None), (S, S, N + 1, None), (S, S, N, i32(S - 1, 3)), (S, S, N, i32(3 * S))):
+        with pytest.raises(ValueError):
+            B.Cache4(*arrays, i32(n), i32(cur), most, block_table=table)
+    assert B.Cache4(*arrays, i32(S), i32(S), 3 * N, block_table=i32(S, 3)).c.c.max_seq_len == 3 * N
+
+
 @pytest.mark.parametrize("entry", [append, attend, shared])
 def test_arrays_of_the_step(lib, entry):
     entry(tokens=step(head_len=(L, S, H)))
