@@ -143,7 +143,6 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
     const int in_block = PAGES ? (1 << c.block_shift) - 1 : 0;
     const int my_key = 4 * (m & 3) + (m >> 2);   // of each sixteen, whose row this lane loads
     // A lane has the words of the tile's key 4 m + kq, so that those of keys 16 i + 4 d + kq lie with lane 4 i + d of each sixteen.
-    auto lane_of = [&](int key) { return 16 * (key & 3) + (key >> 2); };
     auto of_my_key = [&](uint32_t x, int i) { return (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (16 * (m >> 2) + (m & 3) + 4 * i), (int)x); };   // of key 16 i + my_key
     const uint32_t blocks = src.n_blocks ? (uint32_t)src.n_blocks : 0x80000000u;
     auto is_block = [&](int b) { return (uint32_t)b < blocks; };
@@ -184,21 +183,23 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
         *keys = left;
         return at;
     };
-    // (PAGES 2: below sixteen slots) the row of the tile's key `key`; keys that are not there bring the pool's first row, with scales of zero
-    auto slot_of = [&](int k0, int key, int block, uint64_t there) {
-        const int from = lane_of(key), b = __shfl(block, from);
-        return (there >> from) & 1 ? base + (int64_t)((uint32_t)b * block_bytes + (uint64_t)(uint32_t)((k0 + key) & in_block) * sb) : base;
+    // (PAGES 2: below sixteen slots) the row of the key that the lane has the words of; keys that are not there bring the pool's first row, with scales of zero.  (Worked out
+    // once and handed round.  By every lane for the rows that it loads, twenty products in 64 bits, it left too few registers: 8 sequences of 4000 keys in pages of 4, eight tokens 92 us, 25 so; four 58 and 20; one 21 and 18.)
+    auto slot_of = [&](int k0, int block, uint64_t there) {
+        return (there >> lane) & 1 ? base + (int64_t)((uint32_t)block * block_bytes + (uint64_t)(uint32_t)((k0 + 4 * m + kq) & in_block) * sb) : base;
     };
+    int64_t my_row = 0;
     uint4 k[4];
     uint32_t v[4][4];
     int64_t at[4];
     int keys[4];
     auto load_k = [&](int k0, int block, uint64_t there) {
+        if (PAGES == 2) my_row = slot_of(k0, block, there);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             typedef uint32_t uint2v __attribute__((ext_vector_type(2)));
             if (PAGES == 2) {
-                const char *p = (const char *)c.k + slot_of(k0, 16 * i + my_key, block, there);
+                const char *p = (const char *)c.k + (int64_t)((uint64_t)of_my_key((uint32_t)(my_row >> 32), i) << 32 | of_my_key((uint32_t)my_row, i));
                 if (DIRECT) {
                     k[i] = load_stream16(p + 16 * kq);
                 } else {
@@ -217,14 +218,22 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
             }
         }
     };
-    auto load_v = [&](int k0, int block, uint64_t there) {
+    auto load_v = [&] {
+        if (PAGES == 2) {
+            const auto some = [&](auto first) {   // (eight at a time: the compiler would have all addresses before the first load)
+                uint32_t low[8], high[8];
+                spread<first.value>((uint32_t)my_row, low, std::make_integer_sequence<int, 8>());
+                spread<first.value>((uint32_t)(my_row >> 32), high, std::make_integer_sequence<int, 8>());
+#pragma unroll
+                for (int n = 0; n < 8; ++n)
+                    v[(first.value + n) / 4][n % 4] = *reinterpret_cast<const uint32_t *>((const char *)c.v + (int64_t)((uint64_t)high[n] << 32 | low[n]) + 4 * m);
+                __builtin_amdgcn_sched_barrier(0);
+            };
+            some(std::integral_constant<int, 0>()), some(std::integral_constant<int, 8>());
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            if (PAGES == 2) {
-#pragma unroll
-                for (int d = 0; d < 4; ++d) v[i][d] = *reinterpret_cast<const uint32_t *>((const char *)c.v + slot_of(k0, 16 * i + 4 * d + kq, block, there) + 4 * m);
-                continue;
-            }
             const auto b = rsrc(c.v, at[i], keys[i]);
 #pragma unroll
             for (int d = 0; d < 4; ++d) v[i][d] = __builtin_amdgcn_raw_buffer_load_b32(b, kq * sb + 4 * m, 4 * d * sb, kNonTemporal);
@@ -261,7 +270,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
     uint64_t there = there_of(k0, block);
     Words words = load_words(k0, block, there);
     load_k(k0, block, there);
-    load_v(k0, block, there);
+    load_v();
     int ahead = block_at(k0 + kStep);
     const int first = a.half ? lane : 2 * lane, second_at = a.half ? lane + 64 : 2 * lane + 1;   // the dimensions of the band
 #pragma unroll
@@ -510,7 +519,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
                     for (int p = kW - 1; p >= 0; --p) o[t][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, weight[t][p], o[t][e], 0, 0, 0);
             }
         }
-        load_v(k0 + kStep, block_next, there_next);
+        load_v();
         block = block_next;
         there = there_next;
     }
