@@ -195,6 +195,27 @@ def test_two_streams_with_a_workspace_each():
     assert all(torch.equal(o, w) for o, w in zip(outs, want))
 
 
+def test_two_graphs_with_one_workspace():
+    """Replayed in turn on one stream, the workspace being anything in between."""
+    from paper_2604_04921_amd import binding as B
+    cases = [K.Case(91, (3000, 50), (2, 1), block=16), K.Case(92, (900,), (70,), block=4)]
+    want = [K.attend(B, c).clone() for c in cases]
+    calls = [(c.model(B), K.descriptor(B, c, c.packed()), c.layer, c.step(B), c.q_gpu, torch.zeros_like(c.q_gpu)) for c in cases]
+    ws = torch.full((max([256] + [B.tri_attend4_workspace_size(a[0], a[1], a[3]) for a in calls]),), 255, dtype=torch.uint8, device="cuda")
+    graphs = [torch.cuda.CUDAGraph() for _ in calls]
+    torch.cuda.synchronize()
+    for g, a in zip(graphs, calls):
+        with torch.cuda.graph(g):
+            B.tri_attend4(*a, workspace=ws)
+    for i in range(6):
+        calls[i % 2][5].fill_(3.0)
+        graphs[i % 2].replay()
+        torch.cuda.synchronize()
+        assert torch.equal(calls[i % 2][5], want[i % 2])
+        if i % 3 == 0:
+            ws.fill_(i)
+
+
 @pytest.mark.parametrize("shared", [False, True])
 def test_graph_of_a_step(shared):
     """An append in 4 bits and the attention over what it wrote (or an append to the sequences' own caches behind a prefix in 4 bits), captured once and replayed with other rows, eager work in between."""
