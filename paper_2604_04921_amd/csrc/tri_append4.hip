@@ -81,10 +81,10 @@ __device__ __forceinline__ uint32_t most_of_4(uint32_t x)
     x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0xb1, 0xf, 0xf, true));          // lane ^ 1
     return max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x4e, 0xf, 0xf, true));       // lane ^ 2
 }
-__device__ __forceinline__ double most_of_4(double x)
+__device__ __forceinline__ uint64_t most_of_4(uint64_t x)
 {
-    x = fmax(x, __shfl_xor(x, 1));
-    return fmax(x, __shfl_xor(x, 2));
+    x = max(x, (uint64_t)__shfl_xor((unsigned long long)x, 1));
+    return max(x, (uint64_t)__shfl_xor((unsigned long long)x, 2));
 }
 
 __device__ __forceinline__ uint32_t codes8(const float *x, float scale)
@@ -160,7 +160,8 @@ __device__ __forceinline__ Angles angles_of(int32_t pos, const BandTurns &turns,
 
 // A lane's sixteen elements to 4 bits, rotated first.  In fp32 a rotated element is off by less than (|re| + |im|) 2^-21: the hardware's cosine and sine by 1.9e-7 (measured over all 2^32 phases), the angle by 5e-9, the
 // products' roundings by 2^-23.  |re| + |im| is at most twice the larger of the pair's rotated elements, of which `apart` below has the largest, its own error being far below the bound's slack.  Where what lies within
-// `apart` of an element does not all have one code, or the group's largest not one scale, the element is worked out in double precision: one or two waves in a hundred of Gaussian rows.
+// `apart` of an element does not all have one code, or the group's largest not one scale (or, next to 2^128, is not on one side of it), the element is worked out in double precision: one or two waves in a hundred of
+// Gaussian rows.
 template <typename T, bool HALF>
 __device__ __forceinline__ Codes to_codes(const Eight<T> (&raw)[2], const Angles &angles, const T *row, int32_t pos, const BandTurns &turns, int part)
 {
@@ -183,17 +184,18 @@ __device__ __forceinline__ Codes to_codes(const Eight<T> (&raw)[2], const Angles
         bits_of[p] = most_of_4(bits_of[p]);
     }
     Codes got;
+    constexpr uint32_t kLargest = 0x7f7fffffu;
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
-        const uint32_t bits = bits_of[p];
-        const float most = __uint_as_float(bits), apart = 0x1p-20f * (HALF ? fmaxf(__uint_as_float(bits_of[0]), __uint_as_float(bits_of[1])) : most);   // (half-split pairs lie in both of the lanes' groups)
-        uint32_t byte = scale_byte(bits);
-        if (byte != kScaleNaN) {
-            byte = scale_byte(min(__float_as_uint(most + apart), 0x7f7fffffu));
+        // (half-split pairs lie in both of the lanes' groups; infinities may be roundings of numbers: as the largest number)
+        const float most = __uint_as_float(min(bits_of[p], kLargest)), apart = 0x1p-20f * (HALF ? __uint_as_float(min(max(bits_of[0], bits_of[1]), kLargest)) : most);
+        uint32_t byte = kScaleNaN;
+        if (bits_of[p] <= 0x7f800000u) {   // (beyond: what came was no number)
+            byte = scale_byte(__float_as_uint(most + apart));
             if (scale_byte(__float_as_uint(fmaxf(most - apart, 0.f))) != byte) {   // (all four lanes)
-                double exact = 0.0;
+                uint64_t exact = 0;   // (the bits: what is no number is the largest)
 #pragma unroll 1
-                for (int e = 0; e < 8; ++e) exact = fmax(exact, fabs(rotated<T, HALF>(row, 64 * p + 8 * part + e, pos, turns)));
+                for (int e = 0; e < 8; ++e) exact = max(exact, (uint64_t)__double_as_longlong(fabs(rotated<T, HALF>(row, 64 * p + 8 * part + e, pos, turns))));
                 byte = scale_byte(most_of_4(exact));
             }
         }

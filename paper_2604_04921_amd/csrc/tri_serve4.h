@@ -17,9 +17,9 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t bits)
     const int b = (int)(bits >> 23) - 2 + ((bits & 0x7fffffu) > 0x600000u);
     return (uint32_t)min(max(b, kScaleLeast), kScaleMost);
 }
-__device__ __forceinline__ uint32_t scale_byte(double a)
+__device__ __forceinline__ uint32_t scale_byte(uint64_t bits)   // (a double's; NaN is beyond 2^128, too)
 {
-    const uint64_t bits = (uint64_t)__double_as_longlong(a);
+    if (bits >= (uint64_t)(1023 + 128) << 52) return kScaleNaN;
     const int b = (int)(bits >> 52) - 1023 + 127 - 2 + ((bits & 0xfffffffffffffull) > 0xc000000000000ull);
     return (uint32_t)min(max(b, kScaleLeast), kScaleMost);
 }
