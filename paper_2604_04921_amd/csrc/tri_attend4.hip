@@ -236,7 +236,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
         for (int i = 0; i < 4; ++i) {
             const auto b = rsrc(c.v, at[i], keys[i]);
 #pragma unroll
-            for (int d = 0; d < 4; ++d) v[i][d] = __builtin_amdgcn_raw_buffer_load_b32(b, kq * sb + 4 * m, 4 * d * sb, kNonTemporal);
+            for (int d = 0; d < 4; ++d) v[i][d] = __builtin_amdgcn_raw_buffer_load_b32(b, (kq + 4 * d) * sb + 4 * m, 0, kNonTemporal);   // (the scalar offset would not be checked against the size)
         }
     };
     constexpr int kStep = kWaves * kTile;
