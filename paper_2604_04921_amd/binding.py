@@ -191,6 +191,8 @@ class Cache:
         assert pos.dtype == torch.int32 and seq_len.dtype == torch.int32 and cur_pos.dtype == torch.int32
         self.tensors = (k, v, pos, seq_len, cur_pos, block_table)
         self.n_seqs, self.dtype, self.device = seq_len.numel(), k.dtype, k.device
+        self.sizes = tuple(min(n) for n in zip(k.shape[:4], pos.shape, (k if v is None else v).shape))
+        self.layers, self.heads = self.sizes[0], self.sizes[2]
         bs = 0 if block_table is None else k.shape[3]
         self.c = TriCache(k.data_ptr(), 0 if v is None else v.data_ptr(), pos.data_ptr(), _dtype(k),
                           seq_len.numel(), seq_len.data_ptr(), cur_pos.data_ptr(), int(max_seq_len), bs,
@@ -236,6 +238,8 @@ class Cache4:
             raise TypeError("rows: float32 or bfloat16, got %s" % rows)
         self.tensors = (k, v, k_scale, v_scale, pos, seq_len, cur_pos, block_table)
         self.n_seqs, self.dtype, self.device = seq_len.numel(), rows, k.device
+        self.sizes = tuple(k.shape[:4])
+        self.layers, self.heads = self.sizes[0], self.sizes[2]
         table = (0, 0, 0, 0) if block_table is None else (k.shape[3], block_table.data_ptr(), block_table.shape[1], k.shape[1])
         c = TriCache(k.data_ptr(), v.data_ptr(), pos.data_ptr(), TRI_FP4, seq_len.numel(), seq_len.data_ptr(), cur_pos.data_ptr(), int(max_seq_len), table[0], table[1], table[2],
                      *(2 * k.stride(i) for i in range(4)), pos.stride(0), pos.stride(1), pos.stride(2), 1, table[3])
@@ -282,6 +286,24 @@ def _rows(t, heads, tokens, cache, name):
     return strides
 
 
+def _covers(model, cache, layer, name="the cache"):
+    """That a layer's call stays inside the cache's arrays."""
+    if cache.layers <= layer or cache.heads < model.n_kv_heads:
+        raise ValueError("%s: %d layers of %d heads, not layer %d of %d heads" % (name, cache.layers, cache.heads, layer, model.n_kv_heads))
+
+
+def _room(model, cache, seqs, slots, name):
+    """That the cache's arrays have all layers and heads of the model, and `slots` slots of `seqs` sequences; paged, that a table has these sequences, and the arrays all blocks that ids can name."""
+    layers, many, heads, most = cache.sizes
+    k, table = cache.tensors[0], cache.tensors[-1]
+    if layers < model.n_layers or heads < model.n_kv_heads:
+        raise ValueError("%s: %d layers of %d heads, the model's %d of %d" % (name, layers, heads, model.n_layers, model.n_kv_heads))
+    if table is None and (many < seqs or most < slots):
+        raise ValueError("%s: room for %d sequences of %d slots, not %d of %d" % (name, many, most, seqs, slots))
+    if table is not None and (table.dim() != 2 or table.shape[0] < seqs or (many, most) != (k.shape[1], k.shape[3])):
+        raise ValueError("%s: a table %s of %d blocks of %d for %d sequences, k's blocks being %d of %d" % (name, tuple(table.shape), many, most, seqs, k.shape[1], k.shape[3]))
+
+
 def _fits(model, cache, tokens):
     """What the kernels take on trust of the step's arrays: their sizes, and that they lie where the cache does."""
     if tokens.starts is not None and tokens.starts <= cache.n_seqs:
@@ -307,6 +329,7 @@ def _append(entry, model, cache, layer, tokens, k_new, v_new, new_seq_len, strea
     strides = _rows(k_new, model.n_kv_heads, tokens, cache, "k_new")
     if _rows(v_new, model.n_kv_heads, tokens, cache, "v_new") != strides:
         raise ValueError("k_new and v_new must have the same strides")
+    _covers(model, cache, layer)
     _fits(model, cache, tokens)
     _lengths(new_seq_len, cache)
     _check(entry(model.ref, cache.ref, layer, tokens.ref, k_new.data_ptr(), v_new.data_ptr(), strides[0], strides[1],
@@ -334,6 +357,9 @@ def tri_append4(model, cache, layer, tokens, k_new, v_new, new_seq_len=None, str
 
 def _move(entry, model, src, dst, budget, kept_idx, kept_cnt, new_seq_len, stream):
     _here(dst, src, "dst")
+    most = (src.c.c if isinstance(src, Cache4) else src.c).max_seq_len
+    _room(model, src, src.n_seqs, most, "src")
+    _room(model, dst, src.n_seqs, min(int(budget), most), "dst")
     inst = model.n_layers * src.n_seqs * model.n_kv_heads
     for t, n, name in ((kept_idx, inst * int(budget), "kept_idx"), (kept_cnt, inst, "kept_cnt")):
         if t is not None:
@@ -345,7 +371,8 @@ def _move(entry, model, src, dst, budget, kept_idx, kept_cnt, new_seq_len, strea
 
 
 def tri_pack4(model, src, dst, budget, kept_idx=None, kept_cnt=None, new_seq_len=None, stream=None):
-    """Slots of a Cache into a Cache4, all layers: those that kept_idx [L][S][Hkv][budget] and kept_cnt [L][S][Hkv] name, or the first min(length, budget)."""
+    """Slots of a Cache into a Cache4, all layers: those that kept_idx [L][S][Hkv][budget] and kept_cnt [L][S][Hkv] name, or the first min(length, budget).  dst has arrays for src's
+    sequences and min(budget, src's max_seq_len) slots of each; its own lengths and max_seq_len are not read."""
     _move(lib().tri_pack4, model, src, dst, budget, kept_idx, kept_cnt, new_seq_len, stream)
 
 
@@ -354,7 +381,8 @@ def tri_unpack4(model, src, dst, budget, kept_idx=None, kept_cnt=None, new_seq_l
     _move(lib().tri_unpack4, model, src, dst, budget, kept_idx, kept_cnt, new_seq_len, stream)
 
 
-def _attention(model, cache, tokens, q, out, scale, causal):
+def _attention(model, cache, layer, tokens, q, out, scale, causal):
+    _covers(model, cache, layer)
     _fits(model, cache, tokens)
     heads = model.n_q_heads
     qs, os_ = _rows(q, heads, tokens, cache, "q"), _rows(out, heads, tokens, cache, "out")
@@ -364,15 +392,16 @@ def _attention(model, cache, tokens, q, out, scale, causal):
 
 def tri_attend(model, cache, layer, tokens, q, out, scale=None, causal=True, workspace=None, stream=None):
     """out [T][Hq][d] <- attention of q [T][Hq][d] over layer `layer` of the cache.  scale None: 1 / sqrt(d)."""
-    at = _attention(model, cache, tokens, q, out, scale, causal)
+    at = _attention(model, cache, layer, tokens, q, out, scale, causal)
     _check(lib().tri_attend(model.ref, cache.ref, layer, tokens.ref, ctypes.byref(at), _p(workspace), _bytes(workspace, cache), _stream(stream)))
 
 
 def tri_attend_shared(model, prefix, group, cache, layer, tokens, q, out, scale=None, causal=True, workspace=None, stream=None):
     """tri_attend with the keys of shared prefixes: group int32 [P + 1] (first sequence of every prefix's), None for one prefix."""
     assert group is None or (group.dtype == torch.int32 and group.is_contiguous() and group.numel() == prefix.c.n_seqs + 1)
-    at = _attention(model, cache, tokens, q, out, scale, causal)
+    at = _attention(model, cache, layer, tokens, q, out, scale, causal)
     _here(prefix, cache, "prefix")
+    _covers(model, prefix, layer, "prefix")
     if group is not None:
         _here(group, cache, "group")
     _check(lib().tri_attend_shared(model.ref, prefix.ref, _p(group), cache.ref, layer, tokens.ref, ctypes.byref(at), _p(workspace),
@@ -388,7 +417,7 @@ def tri_attend_workspace_size(model, cache, tokens, prefix=None):
 
 def tri_attend4(model, cache, layer, tokens, q, out, scale=None, causal=True, workspace=None, stream=None):
     """tri_attend over a Cache4; q and out of its `rows` type."""
-    at = _attention(model, cache, tokens, q, out, scale, causal)
+    at = _attention(model, cache, layer, tokens, q, out, scale, causal)
     _check(lib().tri_attend4(model.ref, cache.ref, layer, tokens.ref, ctypes.byref(at), _p(workspace), _bytes(workspace, cache), _stream(stream)))
 
 
@@ -396,8 +425,9 @@ def tri_attend4_shared(model, prefix, group, cache, layer, tokens, q, out, scale
     """tri_attend_shared with the prefixes in a Cache4, the sequences' own keys in a Cache of the prefix's `rows` type."""
     if group is not None and (group.dtype != torch.int32 or not group.is_contiguous() or group.numel() != prefix.n_seqs + 1):
         raise ValueError("group: int32, %d entries side by side" % (prefix.n_seqs + 1))
-    at = _attention(model, cache, tokens, q, out, scale, causal)
+    at = _attention(model, cache, layer, tokens, q, out, scale, causal)
     _here(prefix, cache, "prefix")
+    _covers(model, prefix, layer, "prefix")
     if group is not None:
         _here(group, cache, "group")
     _check(lib().tri_attend4_shared(model.ref, prefix.ref, _p(group), cache.ref, layer, tokens.ref, ctypes.byref(at), _p(workspace),
