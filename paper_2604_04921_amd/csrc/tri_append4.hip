@@ -158,7 +158,7 @@ __device__ __forceinline__ Angles angles_of(int32_t pos, const BandTurns &turns,
     return a;
 }
 
-// A lane's sixteen elements to 4 bits, rotated first.  In fp32 a rotated element is off by less than (|re| + |im|) 2^-21: the hardware's cosine and sine by 1.9e-7 (measured over all 2^32 phases), the angle by 5e-9, the
+// A lane's sixteen elements to 4 bits, rotated first.  In fp32 a rotated element is off by less than (|re| + |im|) 2^-21: the hardware's cosine and sine by 1.9e-7 (measured over all 2^32 phases, as a test does again), the angle by 5e-9, the
 // products' roundings by 2^-23.  |re| + |im| is at most twice the larger of the pair's rotated elements, of which `apart` below has the largest, its own error being far below the bound's slack.  Where what lies within
 // `apart` of an element does not all have one code, or the group's largest not one scale (or, next to 2^128, is not on one side of it), the element is worked out in double precision: one or two waves in a hundred of
 // Gaussian rows.

@@ -20,8 +20,8 @@ __device__ __forceinline__ uint32_t phase_of(int32_t pos, uint32_t w_lo, uint32_
     return p * w_hi + __umulhi(p, w_lo) - (pos < 0 ? w_lo : 0u);
 }
 
-// cos and sin of a phase.  bf16: the hardware's, whose argument is in revolutions (absolute error about 2^-20, a rounding to
-// bf16 being 2^-9).  fp32: the nearest quarter turn is taken off in integers, which leaves |x| <= pi/4 with a relative error of 2^-24, and the
+// cos and sin of a phase.  bf16: the hardware's, whose argument is in revolutions (off by at most 1.9e-7, 2^-22.3, over all 2^32 phases, its own rounding to fp32 among it; a rounding to
+// bf16 is 2^-9).  fp32: the nearest quarter turn is taken off in integers, which leaves |x| <= pi/4 with a relative error of 2^-24, and the
 // Taylor polynomials of degree 9 and 10 are off by less than 2e-9 there.
 __device__ __forceinline__ void turn_fast(uint32_t phase, float *c, float *s)
 {

@@ -25,7 +25,9 @@ def build(verbose=False):
     """The generator's library and the instruction-rate probe (a stand-alone program)."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     flags = ["--offload-arch=gfx950", "-std=c++17", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
-    for cmd in ([hipcc, *flags, "-O3", "-fPIC", "-shared", _SRC, "-o", LIB_PATH],
+    root = os.path.dirname(_HERE)
+    include = ["-I", os.path.join(root, "include"), "-I", os.path.join(root, "paper_2604_04921_amd", "csrc")]
+    for cmd in ([hipcc, *flags, *include, "-O3", "-fPIC", "-shared", _SRC, "-o", LIB_PATH],
                 [hipcc, *flags, "-O2", PROBE_SRC, "-o", PROBE_PATH]):
         res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
         if res.returncode != 0:
@@ -57,6 +59,8 @@ def lib():
         L.wl_fill_samples.argtypes = [vp, i32, vp, i64, i64, i64, i64, f32, f32, f32, u64, u64, vp]
         L.wl_fill_normal.restype = i32
         L.wl_fill_normal.argtypes = [vp, i32, i64, u64, u64, vp]
+        L.wl_turn_error.restype = i32
+        L.wl_turn_error.argtypes = [vp, vp]
         L.wl_stream_probe.restype = i64
         L.wl_stream_probe.argtypes = [vp, i64, vp, i32, i32, vp]
         _lib = L
@@ -151,6 +155,13 @@ def generate(cfg, positions=None, layers=None, layer0=0):
     out["k"], out["v"], out["pos"] = k, v, pos
     torch.cuda.synchronize()
     return out
+
+
+def turn_error():
+    """The largest errors of the rotation's hardware cosine and sine, over all 2^32 phases."""
+    worst = torch.zeros(2, dtype=torch.float32, device="cuda")
+    assert lib().wl_turn_error(worst.data_ptr(), _stream()) == 0
+    return worst.tolist()
 
 
 def hbm_probe(gib=16, reps=5):

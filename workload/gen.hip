@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "tri_serve.h"
+
 namespace {
 
 __device__ __forceinline__ uint64_t mix64(uint64_t z)
@@ -150,6 +152,24 @@ __global__ __launch_bounds__(512) void stream_probe_kernel(const uint4 *__restri
     if (acc == 0x12345678u) sink[0] = acc;
 }
 
+// How far the rotation's cosine and sine (tri_serve.h) are off, over all 2^32 phases: the largest difference to double precision's, as the bits of a float (which are in the order of the numbers).
+__global__ __launch_bounds__(256) void turn_error_kernel(uint32_t *worst)
+{
+    const uint32_t threads = gridDim.x * 256u;   // (divides 2^32)
+    float off_c = 0.f, off_s = 0.f;
+    uint32_t phase = blockIdx.x * 256u + threadIdx.x;
+    for (uint64_t i = 0; i < (1ull << 32) / threads; ++i, phase += threads) {
+        float c, s;
+        tri::turn_fast(phase, &c, &s);
+        double cd, sd;
+        sincospi((double)(int32_t)phase * 0x1p-31, &sd, &cd);
+        off_c = fmaxf(off_c, (float)fabs((double)c - cd));
+        off_s = fmaxf(off_s, (float)fabs((double)s - sd));
+    }
+    atomicMax(worst, __float_as_uint(off_c));
+    atomicMax(worst + 1, __float_as_uint(off_s));
+}
+
 }  // namespace
 
 extern "C" {
@@ -170,6 +190,14 @@ int64_t wl_stream_probe(const void *in, int64_t bytes, void *out, int write_ever
         hipLaunchKernelGGL(stream_probe_kernel<false>, dim3(wgs), dim3(512), 0, (hipStream_t)stream,
                            reinterpret_cast<const uint4 *>(in), o, o + bytes / 64, per, write_every);
     return hipGetLastError() == hipSuccess ? per * waves * 16 : -4;
+}
+
+// worst (device, two words that are zero): the largest errors of cosine and sine over all phases, as bits of floats.
+int wl_turn_error(void *worst, void *stream)
+{
+    if (!worst) return -1;
+    hipLaunchKernelGGL(turn_error_kernel, dim3(2048), dim3(256), 0, (hipStream_t)stream, reinterpret_cast<uint32_t *>(worst));
+    return hipGetLastError() == hipSuccess ? 0 : -4;
 }
 
 // Samples around per-head centres (keys, calibration queries).  All pointers are device pointers.
