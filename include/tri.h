@@ -359,9 +359,9 @@ tri_status tri_unpack4(const tri_model *model, const tri_cache4 *src, const tri_
 /*
  * tri_attend over a cache of 4 bits, q and out being rows of cache->rows; and for sequences with caches of their own in full precision (dtype prefix->rows; what was appended since) behind prefixes in 4 bits, by the
  * rules of tri_attend_shared.  With group 0, 1, 2, ... every sequence has a prefix to itself.
- * Keys and values enter the products as they are read back.  In bf16, with up to 64 rows (query heads of the group x max_tokens; x n_tokens for a prefix) per KV head, queries and weights enter them with 16 bits of
- * fraction.  Beyond, weights are bf16 numbers, queries that are turned on the way are off by at most 2^-12 of an element or 2^-25 of the row's largest, and others by 2^-21 of the row's largest (most are exact).  Of the
- * products of a query's and a key's dimensions, what is below 2^-13 of the largest of the eight 8 n to 8 n + 7 is cut off each; the eight's sums are added in fp32.  In fp32 both have 24 bits, and all is added in fp32.
+ * Keys and values enter the products as they are read back.  In bf16, with up to 64 rows (query heads of the group x max_tokens; for a prefix x n_tokens, all of the step's, whichever prefix they are behind: what
+ * a sequence's result is rounded to depends on the step's size) per KV head, queries and weights enter them with 16 bits of fraction.  Beyond, weights are bf16 numbers, queries that are turned on the way are off by
+ * at most 2^-12 of an element or 2^-25 of the row's largest, and others by 2^-21 of the row's largest (most are exact).  Of the products of a query's and a key's dimensions, what is below 2^-13 of the largest of the eight 8 n to 8 n + 7 is cut off each; the eight's sums are added in fp32.  In fp32 both have 24 bits, and all is added in fp32.
  */
 tri_status tri_attend4(const tri_model *model, const tri_cache4 *cache, int32_t layer, const tri_tokens *tokens,
                        const tri_attention *attention, void *workspace, size_t ws_bytes, void *stream);

@@ -356,7 +356,7 @@ __device__ __forceinline__ int slot_to_read(const Pack4Args &a, const Instance &
 }
 
 // As append4_kernel, from slots to slots; a slot's row and its place are each found by the lane (slots kept are in any order).  Bound by bytes: 2048 kept slots in four layers of eight sequences, 344 MB, take 76 us (4.5 TB/s; a large copy 4.8),
-// pre-RoPE and scattered.  (The bound on registers, six workgroups to a CU: interleaved pairs of sixteen sequences 240 us, 244 without; half-split pairs and fp32 would spill.)
+// pre-RoPE and scattered.  (The bound on registers, six workgroups to a CU, which three registers are spilled for: interleaved pairs of sixteen sequences 240 us, 244 without; half-split pairs and fp32 would spill more.)
 template <typename T, bool TURN, bool HALF>
 __global__ __launch_bounds__(kPackThreads, sizeof(T) == 2 && !HALF ? 6 : 1) void pack4_kernel(Pack4Args a)
 {
@@ -449,7 +449,8 @@ __global__ __launch_bounds__(kPackThreads) void unpack4_kernel(Pack4Args a)
 
 }  // namespace
 
-// Heads of a workgroup: four share their tokens' angles where there are workgroups enough all the same (8192 tokens of 8 heads 14.2 us, 15.4 with one; 4096 tokens 10.5 and 10.0, 2048 9.6 and 6.9, one 6.6 and 4.1).
+// Heads of a workgroup: four share their tokens' angles where there are workgroups enough all the same (8192 tokens of 8 heads 14.2 us, 15.4 with one; 4096 tokens, the border, 10.5 and 10.0, 2048 9.6 and 6.9, one 6.6 and 4.1).
+// Measured with 8 heads alone; with one or two there is little to share, and the rule does not ask for that.
 static int append4_heads(int64_t n_tokens, int64_t n_kv_heads) { return n_tokens * n_kv_heads >= 32768 ? 4 : 1; }
 int64_t append4_groups(int64_t n_tokens, int64_t n_kv_heads)
 {

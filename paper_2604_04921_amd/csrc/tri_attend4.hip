@@ -93,7 +93,9 @@ __device__ __forceinline__ void finish(const AttendArgs &a, int split, int t, in
 // would be too much (22 standard deviations of fp32's roundings): they take three bf16 parts of q and of the weights against keys turned into bf16 numbers, with three times the matrix work.
 // Bound by the cache's bytes where there are many keys: 32 ragged sequences of 1000 to 32768 keys in pages of 16, 622 MB, 116 us (5.3 TB/s; a plain read of as much 6.97 TB/s, 89 us), a sixth of that the prologue and
 // the joining of waves of the last workgroups to begin; by latency where there are few: a token over 2176 keys 6.7 us, half of it the chain of arguments, lengths, rows and keys, then some 1500 instructions of one tile and
-// the joining.  Steps on the way (32 ragged sequences, us): as bf16 numbers in the first product too 159, keys as they are 135, four rows by zeros among the weights 126, a row of q turned once per workgroup 115; turned by
+// the joining; by instructions with 9 to 64 rows: 32 sequences of 16000 keys take 145, 147, 301 and 300 us with 20, 32, 36 and 64 rows (96 with 4, the bytes alone 82), vector instructions being 55 to 61 % of the SIMDs'
+// cycles and the matrix pipe 39 to 43 %.  Four e4m3 parts of a query are multiplied however many it needs, each wave decodes all values for its own rows, and from 33 rows on keys are read and weighed twice.  32 rows spill one
+// register in pages of 16 and more, four in smaller ones.  Steps on the way (32 ragged sequences, us): as bf16 numbers in the first product too 159, keys as they are 135, four rows by zeros among the weights 126, a row of q turned once per workgroup 115; turned by
 // every wave for itself, eight tokens' rows took 31 us of 26.  A third wave per SIMD by launch bounds (4) spills: 124 -> 170.
 template <typename T, int NT, int COLS, int PAGES>
 __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
@@ -577,7 +579,9 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(AttendArgs a)
 }
 
 // Rows that a workgroup takes.  More than 64 in bf16 are attend_tile_kernel's, which takes 128 of them over its tiles of keys where rows kernels take 32: 32 sequences of 16000 keys with 20, 32, 36 and 64 rows per KV head take
-// 148, 149, 286 and 299 us here, 309, 306, 350 and 351 there; a third pass over the keys would not pay.
+// 145, 147, 301 and 300 us here, 309, 306, 350 and 351 there; a third pass over the keys would not pay.
+// A prefix counts as if all of the step's tokens were behind it, as for prefixes in full precision.  Where many prefixes have few tokens each, that is the wrong one of the two: 16 sequences with prefixes of 16000 keys of their
+// own (64 rows in all) take 132 us, 32 take 304, and 256 with 1000 each 722, tri_attend4 over as many caches of that length 96 (32) and 52 (256).
 bool is_tile(int32_t type, int64_t rows) { return type == TRI_BF16 && rows > 64; }
 int64_t tile_rows(int32_t type, int64_t rows) { return is_tile(type, rows) ? kTileRows : rows <= 8 ? 8 : type == TRI_F32 || rows <= 16 ? 16 : 32; }
 

@@ -86,7 +86,8 @@ struct TileBuffer {
 // FOUR: keys and values are held in 4 bits.  A lane brings 32 elements of a row, which have one scale.  Values are written into LDS as the bf16 numbers that they stand for, exactly; keys as they are, with their scales, for
 // v_mfma_scale_f32_32x32x64_f8f6f4, which takes queries as e4m3 numbers: two to an element, four bits each, which is all a bf16 number has, or three where queries are turned, and sums as attend4_rows_kernel says.  Weights are
 // bf16 numbers, as above.  Two chunks of 1024 tokens over 5000 to 7168 keys (227 GF) take 270 us, 840 TFLOP/s, where a large library product in bf16 has 1344; with keys as bf16 numbers in LDS, which is four times the reads and as
-// many conversions as values are, 291.  No unit bounds it (vector instructions 42 % of the time, matrix 31 %, LDS 37 %; waits 37 % of the waves' time): without its exponentials, its first products, its writes to LDS or its
+// many conversions as values are, 291.  That is with queries as they are, where it spills three or four registers; with queries turned on the way it spills 31 to 33, of the third part, and two chunks of 1024 tokens over 8192 keys
+// take 387.  No unit bounds it (vector instructions 42 % of the time, matrix 31 %, LDS 37 %; waits 37 % of the waves' time): without its exponentials, its first products, its writes to LDS or its
 // loads it takes 7, 6, 6 and 12 % less.  Issuing the next tile's first product among the exponentials, with three tiles of keys in LDS, takes as long (266 to 267), and rows straight from memory without LDS 440 and more.
 template <int PAGES, Keys KEYS, bool HALF, bool FOUR = false>
 __global__ __launch_bounds__(64 * kWaves, 2) void attend_tile_kernel(AttendArgs a)
